@@ -90,7 +90,7 @@ KERNEL_GROUPS = {"recurrent_kernel": ["recurrent_fwd", "recurrent_bwd"], "tile_k
                  "tile_kernel<dV>": ["tile_dV"], "tile_kernel<dQ>": ["tile_dQ"], "tile_kernel<dK>": ["tile_dK"],
                  "grads_kernel": ["tile_grads"]}
 OTHER_FAMILIES = ("gates", "gate_bwd_prep", "gate_grads", "state_dot", "recurrent_step", "norm_gate_fwd", "norm_gate_bwd",
-                  "transfer_gain")
+                  "transfer_gain", "rownorm_fwd", "rownorm_bwd", "gemm", "act_bwd")
 
 
 def profiled_traffic():

@@ -63,7 +63,8 @@ extern "C" {
 enum { TFLA_EXP = 0, TFLA_SIG = 1 };           /* variant: exponential / sigmoid input gate */
 enum { TFLA_F32 = 0, TFLA_BF16 = 1 };          /* dtype of q, k, v, H, dH, dq, dk, dv        */
 enum { TFLA_FWD = 0, TFLA_BWD = 1 };           /* direction for tfla_mlstm_workspace_bytes   */
-enum { TFLA_NORM_RMS = 0, TFLA_NORM_LAYER = 1 }; /* norm_kind of the layer entry points      */
+enum { TFLA_NORM_RMS = 0, TFLA_NORM_LAYER = 1 }; /* norm_kind of the layer and norm entry points */
+enum { TFLA_ACT_NONE = 0, TFLA_ACT_SILU = 1, TFLA_ACT_GELU = 2, TFLA_ACT_RELU = 3 }; /* act of the projections */
 
 enum {
     TFLA_OK = 0,
@@ -273,6 +274,65 @@ TFLA_API size_t tfla_mlstm_layer_workspace_bytes(int direction, int B, int NH, i
 TFLA_API int tfla_transfer_gain(const void* h, const void* v, int B, int NH, int T, int dhv,
                        int dtype, int norm_kind, float norm_eps,
                        float* g_before, float* g_after, void* stream);
+
+/*
+ * The rest of a residual block around the cell: the norm over the model's columns, the linear projection (into and out of
+ * the heads) and the gated projection pair of the feed-forward half, forward and backward.
+ *  - M rows (tokens), K input columns, N output columns, D columns of the norm; tensors are dense row-major in `dtype`,
+ *    weights (N, K) as a linear layer keeps them; gamma, beta, biases, row statistics and the gradients of those vectors
+ *    are float.  Sums, statistics and products are accumulated in fp32; every tensor result is rounded once, and so is
+ *    dz / da / du of the backward passes on its way into the matrix products (db is summed from the unrounded values).
+ *  - 0 <= M <= 2^24; 1 <= K, N <= 2^20; 1 <= D <= 16384; M * K, M * N and N * K at most 2^36.  M = 0 is no work: forward
+ *    calls write nothing, backward calls write zeros to the gradients of weights, biases, gamma and beta.
+ *  - Tensors may lie at any address that their element type allows and K, N, D may be odd.  The products work on rows that
+ *    are multiples of 16 bytes at 16-byte addresses; other operands are copied into the workspace first.
+ *  - Results do not depend on the order of execution: the same call gives the same bits.
+ *  - Outputs must not overlap inputs, except that y / dx of the norm may be x, dy or d_residual, and y of the linear
+ *    projection may be its residual.
+ *  - workspace: as for tfla_mlstm_fwd; the *_workspace_bytes queries return 0 for invalid arguments and where none is
+ *    needed (workspace may then be NULL).  `unaligned`: non-zero if a tensor of the call is not at a 16-byte address.
+ *
+ * Norm.  mean = 0 (TFLA_NORM_RMS) or sum_j x_j / D (TFLA_NORM_LAYER);  rstd = 1 / sqrt(sum_j (x_j - mean)^2 / D + norm_eps);
+ *     y = (x - mean) rstd (.) gamma + beta              (beta is ignored by the RMS norm; gamma, beta may be NULL: 1 and 0)
+ * rstd, mean (M): what the backward call needs, each may be NULL (mean is zero for the RMS norm).
+ * Backward, with x^ = (x - mean) rstd and g = dy (.) gamma:
+ *     dx = rstd (g - x^ mean_j(g x^) - [LayerNorm] mean_j(g)) + d_residual;  dgamma = sum_m dy x^;  dbeta = sum_m dy
+ * d_residual (M, D): the gradient that goes round the norm, or NULL; dgamma, dbeta may be NULL (with both NULL no workspace
+ * is needed); mean is read for TFLA_NORM_LAYER only.
+ */
+TFLA_API size_t tfla_norm_workspace_bytes(int direction, int M, int D, int dtype, int norm_kind);
+TFLA_API int tfla_norm_fwd(const void* x, const float* gamma, const float* beta, int M, int D, int dtype, int norm_kind,
+                  float norm_eps, void* y, float* rstd, float* mean, void* stream);
+TFLA_API int tfla_norm_bwd(const void* x, const void* dy, const float* rstd, const float* mean, const float* gamma,
+                  const void* d_residual, int M, int D, int dtype, int norm_kind, void* dx, float* dgamma, float* dbeta,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Linear projection.  z = x W^T + bias;  y = act(z) + residual.  bias (N), residual (M, N) and z (M, N, stored for the
+ * backward call of an activation) may be NULL.  act: silu z sigma(z); gelu z Phi(z) (the error function, no approximation);
+ * relu max(z, 0).
+ * Backward: dz = dy (.) act'(z) (act'(0) = 0 for relu);  dx = dz W;  dw = dz^T x;  db = sum_m dz.  z: as the forward call
+ * stored it, NULL for TFLA_ACT_NONE.  dx, dw, db: each may be NULL = not wanted.
+ */
+TFLA_API size_t tfla_linear_workspace_bytes(int direction, int M, int K, int N, int act, int dtype, int unaligned);
+TFLA_API int tfla_linear_fwd(const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N,
+                    int act, int dtype, void* y, void* z, void* workspace, size_t workspace_bytes, void* stream);
+TFLA_API int tfla_linear_bwd(const void* x, const void* w, const void* dy, const void* z, int M, int K, int N, int act,
+                    int dtype, void* dx, void* dw, float* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gated projection pair.  a = x W_gate^T + b_gate;  u = x W_up^T + b_up;  h = act(a) (.) u, both products and the gate in
+ * one kernel.  a, u (M, N): stored for the backward call, each may be NULL.
+ * Backward: da = dh (.) u (.) act'(a);  du = dh (.) act(a);  dx = da W_gate + du W_up;  dw_gate = da^T x;  dw_up = du^T x;
+ * db_gate = sum_m da;  db_up = sum_m du.  dx, the weights' gradients (both or none) and each bias gradient may be NULL.
+ */
+TFLA_API size_t tfla_gated_workspace_bytes(int direction, int M, int K, int N, int act, int dtype, int unaligned);
+TFLA_API int tfla_gated_fwd(const void* x, const void* w_gate, const void* w_up, const float* b_gate, const float* b_up,
+                   int M, int K, int N, int act, int dtype, void* h, void* a, void* u, void* workspace,
+                   size_t workspace_bytes, void* stream);
+TFLA_API int tfla_gated_bwd(const void* x, const void* w_gate, const void* w_up, const void* a, const void* u,
+                   const void* dh, int M, int K, int N, int act, int dtype, void* dx, void* dw_gate, void* dw_up,
+                   float* db_gate, float* db_up, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Bytes of workspace the call with these arguments needs (host function, launches nothing).

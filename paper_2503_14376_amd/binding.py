@@ -9,6 +9,7 @@ EXP, SIG = 0, 1
 F32, BF16 = 0, 1
 FWD, BWD = 0, 1
 NORM_RMS, NORM_LAYER = 0, 1
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "lib", "libtfla_mlstm.so")
@@ -18,7 +19,9 @@ EXPORTS = ("tfla_mlstm_fwd", "tfla_mlstm_bwd", "tfla_mlstm_step", "tfla_mlstm_wo
            "tfla_status_string", "tfla_version", "tfla_profile_enable", "tfla_profile_read",
            "tfla_profile_kernels", "tfla_mlstm_layer_fwd", "tfla_mlstm_layer_bwd", "tfla_mlstm_layer_workspace_bytes",
            "tfla_transfer_gain", "tfla_mlstm_layer_step", "tfla_tile_width", "tfla_mlstm_fwd_static",
-           "tfla_static_scratch_bytes")
+           "tfla_static_scratch_bytes", "tfla_norm_workspace_bytes", "tfla_norm_fwd", "tfla_norm_bwd",
+           "tfla_linear_workspace_bytes", "tfla_linear_fwd", "tfla_linear_bwd", "tfla_gated_workspace_bytes",
+           "tfla_gated_fwd", "tfla_gated_bwd")
 
 
 class TflaError(RuntimeError):
@@ -83,6 +86,24 @@ def load_library():
     lib.tfla_profile_kernels.restype = ci
     lib.tfla_tile_width.restype = ci
     lib.tfla_tile_width.argtypes = [ci]
+    lib.tfla_norm_workspace_bytes.restype = sz
+    lib.tfla_norm_workspace_bytes.argtypes = [ci] * 5
+    lib.tfla_norm_fwd.restype = ci
+    lib.tfla_norm_fwd.argtypes = [vp, fp, fp, ci, ci, ci, ci, cf, vp, fp, fp, vp]
+    lib.tfla_norm_bwd.restype = ci
+    lib.tfla_norm_bwd.argtypes = [vp, vp, fp, fp, fp, vp, ci, ci, ci, ci, vp, fp, fp, vp, sz, vp]
+    lib.tfla_linear_workspace_bytes.restype = sz
+    lib.tfla_linear_workspace_bytes.argtypes = [ci] * 7
+    lib.tfla_linear_fwd.restype = ci
+    lib.tfla_linear_fwd.argtypes = [vp, vp, fp, vp, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
+    lib.tfla_linear_bwd.restype = ci
+    lib.tfla_linear_bwd.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, fp, vp, sz, vp]
+    lib.tfla_gated_workspace_bytes.restype = sz
+    lib.tfla_gated_workspace_bytes.argtypes = [ci] * 7
+    lib.tfla_gated_fwd.restype = ci
+    lib.tfla_gated_fwd.argtypes = [vp, vp, vp, fp, fp, ci, ci, ci, ci, ci, vp, vp, vp, vp, sz, vp]
+    lib.tfla_gated_bwd.restype = ci
+    lib.tfla_gated_bwd.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, fp, fp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -441,3 +462,195 @@ def transfer_gain(h, v, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None):
     if rc != 0:
         raise TflaError(rc, "tfla_transfer_gain")
     return gb, ga
+
+
+# ---- the rest of a residual block: norm over the model's columns, linear projection, gated projection pair --------------
+# These calls are the shortest of all while generating, so they do little per argument: outputs and the workspace that `out`
+# holds from the call before are taken as they are after a check of shape and type.
+
+def norm_workspace_bytes(direction, M, D, dtype, norm_kind) -> int:
+    return int(load_library().tfla_norm_workspace_bytes(direction, M, D, dtype, norm_kind))
+
+
+def linear_workspace_bytes(direction, M, K, N, act, dtype, unaligned=False) -> int:
+    return int(load_library().tfla_linear_workspace_bytes(direction, M, K, N, act, dtype, int(unaligned)))
+
+
+def gated_workspace_bytes(direction, M, K, N, act, dtype, unaligned=False) -> int:
+    return int(load_library().tfla_gated_workspace_bytes(direction, M, K, N, act, dtype, int(unaligned)))
+
+
+def _rows(x, name):
+    """dtype code and (M, columns) of a dense matrix of rows"""
+    import torch
+    if x.dtype == torch.bfloat16:
+        dtype = BF16
+    elif x.dtype == torch.float32:
+        dtype = F32
+    else:
+        raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, x.dtype))
+    if x.dim() != 2 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor of two dimensions" % name)
+    return dtype, x.shape[0], x.shape[1]
+
+
+def _out(o, name, shape, dtype, like, stream):
+    """o[name], checked, or a new tensor there"""
+    import torch
+    t = o.get(name)
+    if t is None:
+        t = o[name] = torch.empty(shape, dtype=dtype, device=like.device)
+        if stream is not None:
+            t.record_stream(stream)
+    else:
+        _want(t, dtype, shape, name)
+    return t.data_ptr()
+
+
+def _scratch(o, workspace, need, like, stream):
+    """address and size of the workspace: the caller's, the one that the last call with this `out` left, or a new one"""
+    import torch
+    if workspace is None:
+        workspace = o.get("workspace")
+        if need and (workspace is None or workspace.numel() < need):
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+            if stream is not None:
+                workspace.record_stream(stream)
+    o["workspace"] = workspace
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+
+
+def _unaligned(*tensors):
+    bits = 0
+    for t in tensors:
+        if t is not None:
+            bits |= t.data_ptr()
+    return bits & 15
+
+
+def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None, out: Optional[Dict] = None) -> Dict:
+    """tfla_norm_fwd on torch device tensors.  x: (M, D) in bf16 or fp32; gamma, beta: (D,) fp32 or None.  Returns y and the row
+    statistics rstd and (LayerNorm) mean, which norm_bwd needs."""
+    import torch
+    f32 = torch.float32
+    dtype, M, D = _rows(x, "x")
+    _want(gamma, f32, (D,), "gamma"); _want(beta, f32, (D,), "beta")
+    o = out if out is not None else {}
+    y, rstd = _out(o, "y", (M, D), x.dtype, x, stream), _out(o, "rstd", (M,), f32, x, stream)
+    mean = _out(o, "mean", (M,), f32, x, stream) if norm_kind == NORM_LAYER else None
+    rc = load_library().tfla_norm_fwd(x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean,
+                                      _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_norm_fwd")
+    return o
+
+
+def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM_RMS, want_dgamma=True, want_dbeta=False,
+             workspace=None, stream=None, out: Optional[Dict] = None) -> Dict:
+    """tfla_norm_bwd on torch device tensors.  rstd, mean: as norm_fwd returned them; d_residual: (M, D), added to dx, or None.
+    Returns dx, dgamma, dbeta (the last two where wanted)."""
+    import torch
+    f32 = torch.float32
+    dtype, M, D = _rows(x, "x")
+    _want(dy, x.dtype, (M, D), "dy"); _want(d_residual, x.dtype, (M, D), "d_residual"); _want(gamma, f32, (D,), "gamma")
+    _want(rstd, f32, (M,), "rstd"); _want(mean, f32, (M,), "mean")
+    o = out if out is not None else {}
+    dx = _out(o, "dx", (M, D), x.dtype, x, stream)
+    dgamma = _out(o, "dgamma", (D,), f32, x, stream) if want_dgamma else None
+    dbeta = _out(o, "dbeta", (D,), f32, x, stream) if want_dbeta else None
+    need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
+    ws, wsb = _scratch(o, workspace, need, x, stream)
+    rc = load_library().tfla_norm_bwd(x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype,
+                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_norm_bwd")
+    return o
+
+
+def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, workspace=None, stream=None,
+               out: Optional[Dict] = None) -> Dict:
+    """tfla_linear_fwd on torch device tensors.  x: (M, K), w: (N, K), residual: (M, N) in bf16 or fp32; bias: (N,) fp32.  Returns
+    y and, with keep_pre, the pre-activation z, which linear_bwd needs where act is not ACT_NONE."""
+    import torch
+    dtype, M, K = _rows(x, "x")
+    N = w.shape[0]
+    _want(w, x.dtype, (N, K), "w"); _want(bias, torch.float32, (N,), "bias"); _want(residual, x.dtype, (M, N), "residual")
+    o = out if out is not None else {}
+    y = _out(o, "y", (M, N), x.dtype, x, stream)
+    z = _out(o, "z", (M, N), x.dtype, x, stream) if keep_pre else None
+    need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, _unaligned(x, w))
+    ws, wsb = _scratch(o, workspace, need, x, stream)
+    rc = load_library().tfla_linear_fwd(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb,
+                                        _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_linear_fwd")
+    return o
+
+
+def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_db=False, workspace=None, stream=None,
+               out: Optional[Dict] = None) -> Dict:
+    """tfla_linear_bwd on torch device tensors.  dy: (M, N); z: the pre-activation of the forward call where act is not ACT_NONE.
+    Returns dx, dw, db (those that are wanted); the gradient of the residual is dy itself."""
+    import torch
+    dtype, M, K = _rows(x, "x")
+    N = w.shape[0]
+    _want(w, x.dtype, (N, K), "w"); _want(dy, x.dtype, (M, N), "dy"); _want(z, x.dtype, (M, N), "z")
+    o = out if out is not None else {}
+    dx = _out(o, "dx", (M, K), x.dtype, x, stream) if want_dx else None
+    dw = _out(o, "dw", (N, K), x.dtype, x, stream) if want_dw else None
+    db = _out(o, "db", (N,), torch.float32, x, stream) if want_db else None
+    need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, _unaligned(x, w, dy))
+    ws, wsb = _scratch(o, workspace, need, x, stream)
+    rc = load_library().tfla_linear_bwd(x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb,
+                                        _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_linear_bwd")
+    return o
+
+
+def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=False, workspace=None, stream=None,
+              out: Optional[Dict] = None) -> Dict:
+    """tfla_gated_fwd on torch device tensors: h = act(x w_gate^T + b_gate) * (x w_up^T + b_up).  x: (M, K), w_gate, w_up: (N, K) in
+    bf16 or fp32; b_gate, b_up: (N,) fp32.  Returns h and, with keep_pre, a and u, which gated_bwd needs."""
+    import torch
+    f32 = torch.float32
+    dtype, M, K = _rows(x, "x")
+    N = w_gate.shape[0]
+    _want(w_gate, x.dtype, (N, K), "w_gate"); _want(w_up, x.dtype, (N, K), "w_up")
+    _want(b_gate, f32, (N,), "b_gate"); _want(b_up, f32, (N,), "b_up")
+    o = out if out is not None else {}
+    h = _out(o, "h", (M, N), x.dtype, x, stream)
+    a = _out(o, "a", (M, N), x.dtype, x, stream) if keep_pre else None
+    u = _out(o, "u", (M, N), x.dtype, x, stream) if keep_pre else None
+    need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, _unaligned(x, w_gate, w_up))
+    ws, wsb = _scratch(o, workspace, need, x, stream)
+    rc = load_library().tfla_gated_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype,
+                                       h, a, u, ws, wsb, _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_gated_fwd")
+    return o
+
+
+def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=True, want_db=False, workspace=None, stream=None,
+              out: Optional[Dict] = None) -> Dict:
+    """tfla_gated_bwd on torch device tensors.  a, u: as gated_fwd with keep_pre returned them; dh: (M, N).  Returns dx, dw_gate,
+    dw_up, db_gate, db_up (those that are wanted)."""
+    import torch
+    f32 = torch.float32
+    dtype, M, K = _rows(x, "x")
+    N = w_gate.shape[0]
+    _want(w_gate, x.dtype, (N, K), "w_gate"); _want(w_up, x.dtype, (N, K), "w_up")
+    _want(a, x.dtype, (M, N), "a"); _want(u, x.dtype, (M, N), "u"); _want(dh, x.dtype, (M, N), "dh")
+    o = out if out is not None else {}
+    dx = _out(o, "dx", (M, K), x.dtype, x, stream) if want_dx else None
+    dwg = _out(o, "dw_gate", (N, K), x.dtype, x, stream) if want_dw else None
+    dwu = _out(o, "dw_up", (N, K), x.dtype, x, stream) if want_dw else None
+    dbg = _out(o, "db_gate", (N,), f32, x, stream) if want_db else None
+    dbu = _out(o, "db_up", (N,), f32, x, stream) if want_db else None
+    need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, _unaligned(x, w_gate, w_up, dh))
+    ws, wsb = _scratch(o, workspace, need, x, stream)
+    rc = load_library().tfla_gated_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N,
+                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, _stream_handle(stream))
+    if rc != 0:
+        raise TflaError(rc, "tfla_gated_bwd")
+    return o

@@ -18,6 +18,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 # recurrent.hip: MFMA accumulators in ordinary VGPRs (the kernel also scales and stores them with
 # vector ALU instructions, which cannot read accumulation registers)
 UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "step.o", []), ("norm.hip", "norm.o", []),
+         ("block_api.hip", "block_api.o", []), ("block_elem.hip", "block_elem.o", []), ("rownorm.hip", "rownorm.o", []),
          ("recurrent.hip", "recurrent.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"])] + [
     # tile kernels: the start-up loop over X and state slices must unroll completely (its items differ in kind and
     # index registers by compile-time constants); with the widest shapes its body exceeds the default size limit
@@ -25,7 +26,9 @@ UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "s
     ("tile_inst.hip", "tile_mode%d.o" % m, ["-DTFLA_TILE_MODE=%d" % m, "-mllvm", "-pragma-unroll-threshold=200000",
                                             "-mllvm", "-amdgpu-mfma-vgpr-form"]) for m in range(4)] + [
     ("tile_grads.hip", "tile_grads%d.o" % w, ["-DTFLA_GRADS_DQK=%d" % w, "-mllvm", "-pragma-unroll-threshold=200000",
-                                              "-mllvm", "-amdgpu-mfma-vgpr-form"]) for w in (64, 128, 256)]
+                                              "-mllvm", "-amdgpu-mfma-vgpr-form"]) for w in (64, 128, 256)] + [
+    # matrix products: operand layouts 0 - 2, + 4 for fp32
+    ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l, "-mllvm", "-amdgpu-mfma-vgpr-form"]) for l in (0, 1, 2, 4, 5, 6)]
 
 
 def _compile(unit):

@@ -2,6 +2,7 @@
 // the forward and backward pass.  See include/tfla_mlstm.h for the contract.
 #include "../../include/tfla_mlstm.h"
 #include "tfla_internal.h"
+#include "profiler.h"
 
 #include <math.h>
 
@@ -9,7 +10,10 @@
 
 using namespace tfla;
 
-namespace tfla { int tile_width_override = 0; }
+namespace tfla {
+int tile_width_override = 0;
+Profiler g_prof;
+}
 
 namespace {
 
@@ -167,11 +171,6 @@ BwdWs carve_bwd(const Dims& d, void* ws) {
     return w;
 }
 
-#define TFLA_TRY(expr)                         \
-    do {                                       \
-        hipError_t e_ = (expr);                \
-        if (e_ != hipSuccess) return (int)e_;  \
-    } while (0)
 
 // (here, out of sight of the units that define launch_tile_grads(): named in one of them, every width would be built there)
 hipError_t launch_grads(const TileArgs& dv, const TileArgs& dq, const TileArgs& dk, int BH, int dtype, hipStream_t s) {
@@ -182,43 +181,6 @@ hipError_t launch_grads(const TileArgs& dv, const TileArgs& dq, const TileArgs& 
         default: return hipErrorInvalidValue;
     }
 }
-
-// ---- optional per-kernel timing with HIP events on the caller's stream -------------------
-enum { K_GATES = 0, K_BWD_PREP, K_REC_FWD, K_REC_BWD, K_TILE_H, K_TILE_DV, K_TILE_DQ, K_TILE_DK, K_GATE_GRADS,
-       K_STATE_DOT, K_STEP, K_NORM_FWD, K_NORM_BWD, K_GAIN, K_TILE_GRADS, K_COUNT };
-const char* const kKernelNames[K_COUNT] = {"gates", "gate_bwd_prep", "recurrent_fwd", "recurrent_bwd", "tile_H",
-                                           "tile_dV", "tile_dQ", "tile_dK", "gate_grads", "state_dot",
-                                           "recurrent_step", "norm_gate_fwd", "norm_gate_bwd", "transfer_gain", "tile_grads"};
-struct Profiler {
-    bool on = false;
-    int cap = 0, used = 0;
-    hipEvent_t* beg = nullptr;
-    hipEvent_t* end = nullptr;
-    int* slot = nullptr;
-    double total_ms[K_COUNT] = {};
-    long launches[K_COUNT] = {};
-};
-Profiler g_prof;
-
-struct ProfScope {
-    int idx;
-    hipStream_t s;
-    ProfScope(int slot, hipStream_t st) : idx(-1), s(st) {
-        if (g_prof.on && g_prof.used < g_prof.cap) {
-            idx = g_prof.used++;
-            g_prof.slot[idx] = slot;
-            (void)hipEventRecord(g_prof.beg[idx], s);
-        }
-    }
-    ~ProfScope() {
-        if (idx >= 0) (void)hipEventRecord(g_prof.end[idx], s);
-    }
-};
-#define TFLA_LAUNCH(slot, expr)     \
-    do {                            \
-        ProfScope ps_((slot), s);   \
-        TFLA_TRY(expr);             \
-    } while (0)
 
 void prof_collect() {
     for (int i = 0; i < g_prof.used; ++i) {

@@ -1,0 +1,143 @@
+// The passes around the matrix products of the residual block: copies into aligned rows, the activation's backward with the
+// column sums of the bias gradients, and the join of a contraction that was cut into parts.  All memory-bound: eight
+// elements per lane and access.
+#include "gemm_epilogue.h"
+
+namespace tfla {
+
+// one instantiation of the products' launcher per operand layout and type (gemm_inst.hip)
+template <int L> hipError_t launch_gemm_layout(const GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);
+
+namespace {
+
+// rows of `cols` elements at any address -> rows of ldd elements (a multiple of eight), zeros behind the columns
+template <typename DT> __global__ void __launch_bounds__(256) repack_kernel(const void* src, void* dst, long rows, int cols, long ldd) {
+    const int c = (blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+    if (c >= ldd) return;
+    for (long r = (long)blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.y * 4)
+        load8<DT>(src, r * cols + c, cols - c).store(dst, r * ldd + c);
+}
+
+// Workgroups of 4 wavefronts: 512 columns, the rows of a row block in turn over the wavefronts.
+template <typename DT, bool PAIR> __global__ void __launch_bounds__(256) act_bwd_kernel(ActBwdArgs a, int rpb) {
+    __shared__ float red[4][PAIR ? 2 : 1][512];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = (blockIdx.y * 64 + lane) * 8, left = a.N - c;
+    const long r0 = (long)blockIdx.x * rpb, r1 = min(a.M, r0 + rpb);
+    float s0[8], s1[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { s0[e] = 0.0f; s1[e] = 0.0f; }
+    if (c < a.ldd) {
+#pragma unroll 2
+        for (long r = r0 + wave; r < r1; r += 4) {
+            float g[8], z[8], u[8];
+            load8<DT>(a.dy, r * a.N + c, left).get(g);
+            if (a.z) load8<DT>(a.z, r * a.N + c, left).get(z);
+            if constexpr (PAIR) load8<DT>(a.u, r * a.N + c, left).get(u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (PAIR) {
+                    const float da = g[e] * u[e] * act_slope(z[e], a.act);
+                    u[e] = g[e] * act_value(z[e], a.act);
+                    g[e] = da;
+                    s1[e] += u[e];
+                } else if (a.act != ACT_NONE) {
+                    g[e] *= act_slope(z[e], a.act);
+                }
+                s0[e] += g[e];
+            }
+            if (a.dz0) store8<DT>(a.dz0, r * a.ldd + c, 8, g);
+            if constexpr (PAIR) store8<DT>(a.dz1, r * a.ldd + c, 8, u);
+        }
+    }
+    if (!a.part) return;
+    store8<float>(red[wave][0], lane * 8, 8, s0);
+    if constexpr (PAIR) store8<float>(red[wave][1], lane * 8, 8, s1);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += 256) {
+        const int n = blockIdx.y * 512 + i;
+        if (n >= a.N) continue;
+#pragma unroll
+        for (int p = 0; p < (PAIR ? 2 : 1); ++p)
+            a.part[((long)blockIdx.x * (PAIR ? 2 : 1) + p) * a.ldp + n] = ((red[0][p][i] + red[1][p][i]) + red[2][p][i]) + red[3][p][i];
+    }
+}
+
+// adds the parts of a contraction in order and applies the epilogue, eight columns per lane
+template <typename DT, int EPI> __global__ void __launch_bounds__(256) gemm_reduce_kernel(GemmArgs a) {
+    const int n = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8;
+    const long m = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int b = blockIdx.z, planes = a.pair ? 2 : a.batch;
+    if (n >= a.N || m >= a.M) return;
+    float v[8], w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { v[e] = 0.0f; w[e] = 0.0f; }
+#pragma unroll 4
+    for (int p = 0; p < a.split; ++p) {
+        float t[8];
+        load8<float>(a.part, (((long)p * planes + b) * a.M + m) * a.ld_part + n, 8).get(t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += t[e];
+        if constexpr (EPI == EPI_GATED) {
+            load8<float>(a.part, (((long)p * planes + 1) * a.M + m) * a.ld_part + n, 8).get(t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] += t[e];
+        }
+    }
+    epilogue8<DT, EPI>(a, b, m, n, v, w);
+}
+
+// rows of a block of the activation's backward: the partial sums stay a small part of the traffic, and a launch has enough
+// workgroups to stream
+int rows_per_block(long M) { return M <= 1024 ? 16 : 64; }
+
+template <typename DT> hipError_t reduce(const GemmArgs& a, int epi, hipStream_t s) {
+    const dim3 grid((unsigned)((a.M + 3) / 4), (a.N + 511) / 512, a.batch), block(256);
+    if (epi == EPI_GATED) hipLaunchKernelGGL((gemm_reduce_kernel<DT, EPI_GATED>), grid, block, 0, s, a);
+    else if (epi == EPI_LINEAR) hipLaunchKernelGGL((gemm_reduce_kernel<DT, EPI_LINEAR>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((gemm_reduce_kernel<DT, EPI_STORE>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_repack(const void* src, void* dst, long rows, int cols, long ldd, int dtype, hipStream_t s) {
+    const long ny = (rows + 3) / 4;
+    const dim3 grid((unsigned)((ldd + 511) / 512), (unsigned)(ny < 2048 ? ny : 2048));
+    if (dtype == 1) hipLaunchKernelGGL((repack_kernel<bf16_t>), grid, dim3(256), 0, s, src, dst, rows, cols, ldd);
+    else hipLaunchKernelGGL((repack_kernel<float>), grid, dim3(256), 0, s, src, dst, rows, cols, ldd);
+    return hipGetLastError();
+}
+
+int act_bwd_row_blocks(long M, int N) { const int r = rows_per_block(M); return (int)((M + r - 1) / r); }
+
+hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
+    const int rpb = rows_per_block(a.M);
+    const dim3 grid((unsigned)act_bwd_row_blocks(a.M, a.N), (unsigned)((a.ldd + 511) / 512)), block(256);
+    if (a.dtype == 1) {
+        if (a.pair) hipLaunchKernelGGL((act_bwd_kernel<bf16_t, true>), grid, block, 0, s, a, rpb);
+        else hipLaunchKernelGGL((act_bwd_kernel<bf16_t, false>), grid, block, 0, s, a, rpb);
+    } else {
+        if (a.pair) hipLaunchKernelGGL((act_bwd_kernel<float, true>), grid, block, 0, s, a, rpb);
+        else hipLaunchKernelGGL((act_bwd_kernel<float, false>), grid, block, 0, s, a, rpb);
+    }
+    return hipGetLastError();
+}
+
+GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype) {
+    GemmPlan p;
+    p.bm = p.bn = dtype == 1 ? 128 : 64;
+    p.split = 1;
+    return p;
+}
+
+hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s) {
+    const int e = a.split > 1 ? EPI_PART : epi;
+    hipError_t rc;
+    if (a.dtype == 1) rc = !b_tr ? launch_gemm_layout<0>(a, p, e, s) : (!a_tr ? launch_gemm_layout<1>(a, p, e, s) : launch_gemm_layout<2>(a, p, e, s));
+    else rc = !b_tr ? launch_gemm_layout<4>(a, p, e, s) : (!a_tr ? launch_gemm_layout<5>(a, p, e, s) : launch_gemm_layout<6>(a, p, e, s));
+    if (rc != hipSuccess || e != EPI_PART) return rc;
+    return a.dtype == 1 ? reduce<bf16_t>(a, epi, s) : reduce<float>(a, epi, s);
+}
+
+}  // namespace tfla

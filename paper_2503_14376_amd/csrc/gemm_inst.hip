@@ -1,0 +1,42 @@
+// Compiled once per TFLA_GEMM (0: both operands plain, 1: B transposed, 2: both transposed; + 4 for fp32): the product
+// kernels of that layout and their launcher.
+#ifndef TFLA_GEMM
+#error "compile with -DTFLA_GEMM=<0..2, 4..6>"
+#endif
+#include "gemm.h"
+
+namespace tfla {
+
+namespace {
+
+template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipStream_t s) {
+    constexpr int L = TFLA_GEMM & 3;
+    constexpr bool ATR = L == 2, BTR = L >= 1;
+    const int bno = PAIR ? p.bn / 2 : p.bn;
+    const int tms = (a.M + p.bm - 1) / p.bm, tns = (a.N + bno - 1) / bno;
+    const dim3 grid((unsigned)((long)tms * tns * a.split * a.batch));
+#if TFLA_GEMM >= 4
+    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 2, 1, ATR, BTR, PAIR, EPI>), grid, dim3(128), 0, s, a, tms, tns);
+#else
+    hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, ATR, BTR, PAIR, EPI>), grid, dim3(256), 0, s, a, tms, tns);
+#endif
+}
+
+}  // namespace
+
+template <int L> hipError_t launch_gemm_layout(const GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);
+template <> hipError_t launch_gemm_layout<TFLA_GEMM>(const GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s) {
+#if (TFLA_GEMM & 3) == 0
+    if (epi == EPI_PART) {
+        if (a.pair) go<true, EPI_PART>(a, p, s);
+        else go<false, EPI_PART>(a, p, s);
+    } else if (a.pair) go<true, EPI_GATED>(a, p, s);
+    else go<false, EPI_LINEAR>(a, p, s);
+#else
+    if (epi == EPI_PART) go<false, EPI_PART>(a, p, s);
+    else go<false, EPI_STORE>(a, p, s);
+#endif
+    return hipGetLastError();
+}
+
+}  // namespace tfla

@@ -1,0 +1,309 @@
+"""The residual block's operators (norm over the model's columns, linear projection, gated projection pair) against plain
+64-bit forms: every direction, type, activation and optional part, lengths from one token on, odd sizes, tensors at odd
+addresses between values that must not be read, empty calls, other streams, graphs."""
+import itertools
+
+import pytest
+import torch
+
+from tests import block_util as bu
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+ACTS = ("none", "silu", "gelu", "relu")
+
+
+@pytest.fixture(scope="module")
+def tfla():
+    import paper_2503_14376_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def code(tfla, act):
+    return {"none": tfla.ACT_NONE, "silu": tfla.ACT_SILU, "gelu": tfla.ACT_GELU, "relu": tfla.ACT_RELU}[act]
+
+
+def fenced(t, shift=0):
+    """the same tensor inside a larger allocation of NaN: `shift` elements off a 16-byte address, NaN before and behind it"""
+    n = t.numel()
+    buf = torch.full((n + 128,), float("nan"), dtype=t.dtype, device=t.device)
+    at = 64 + shift
+    buf[at:at + n] = t.reshape(-1)
+    return buf[at:at + n].view(t.shape)
+
+
+def normal(gen, *shape, std=1.0, mean=0.0, dtype=F32):
+    return (torch.randn(shape, generator=gen, device="cuda") * std + mean).to(dtype)
+
+
+def generator(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+# ---- norm ----------------------------------------------------------------------------------------------------------
+NORM_SIZES = [(1, 1), (1, 4096), (2, 7), (3, 64), (5, 511), (130, 512), (33, 777), (4, 1024), (7, 1365), (3, 2048), (17, 2049),
+              (6, 4000), (5, 4104), (3, 8191), (2, 10000), (2, 16384), (3000, 100), (600, 2056)]
+
+
+@pytest.mark.parametrize("M,D", NORM_SIZES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layer", [False, True])
+def test_norm(tfla, M, D, dtype, layer):
+    print("norm", M, D, dtype, layer, flush=True)
+    gen = generator(M * 131 + D)
+    kind = tfla.NORM_LAYER if layer else tfla.NORM_RMS
+    shift = (M + D) % 3
+    x = fenced(normal(gen, M, D, mean=0.5, dtype=dtype), shift)
+    dy = fenced(normal(gen, M, D, dtype=dtype), shift)
+    res = fenced(normal(gen, M, D, dtype=dtype), shift) if D % 2 else None
+    gamma = fenced(normal(gen, D, std=0.2, mean=1.0), shift) if D != 64 else None
+    beta = fenced(normal(gen, D, std=0.2), shift) if D != 512 else None
+    f = tfla.norm_fwd(x, gamma, beta, norm_kind=kind, norm_eps=1e-5)
+    mean, rstd, y = bu.norm(x, gamma, beta, layer, 1e-5)
+    if layer:
+        bu.within("mean", f["mean"], *mean)
+    if D > 1 or not layer:        # (a LayerNorm row of one value has no variance: rstd is eps's alone)
+        bu.within("rstd", f["rstd"], *rstd)
+    bu.within("y", f["y"], *y)
+    b = tfla.norm_bwd(x, dy, f["rstd"], f.get("mean"), gamma, res, norm_kind=kind, want_dbeta=True)
+    dx, dg, db = bu.norm_back(x, dy, f["rstd"], f.get("mean"), gamma, res, layer)
+    bu.within("dx", b["dx"], *dx)
+    bu.within("dgamma", b["dgamma"], *dg)
+    bu.within("dbeta", b["dbeta"], *db)
+
+
+def test_norm_in_place_and_many_rows(tfla):
+    gen = generator(3)
+    x, dy = normal(gen, 5000, 1000, dtype=BF16), normal(gen, 5000, 1000, dtype=BF16)
+    gamma = normal(gen, 1000)
+    f = tfla.norm_fwd(x, gamma)
+    y = x.clone()
+    tfla.norm_fwd(y, gamma, out={"y": y})
+    assert torch.equal(y, f["y"])
+    b = tfla.norm_bwd(x, dy, f["rstd"], gamma=gamma, d_residual=dy)
+    d = dy.clone()
+    tfla.norm_bwd(x, d, f["rstd"], gamma=gamma, d_residual=d, out={"dx": d})
+    assert torch.equal(d, b["dx"])
+    again = tfla.norm_bwd(x, dy, f["rstd"], gamma=gamma, d_residual=dy)
+    assert torch.equal(again["dgamma"], b["dgamma"]) and torch.equal(again["dx"], b["dx"])
+
+
+def test_norm_rows_do_not_touch_each_other(tfla):
+    gen = generator(4)
+    x = normal(gen, 40, 3000, dtype=BF16)
+    ok = tfla.norm_fwd(x, norm_kind=tfla.NORM_LAYER)["y"]
+    x[7] = float("nan"); x[20, 5] = float("inf"); x[30] = 0.0
+    y = tfla.norm_fwd(x, norm_kind=tfla.NORM_LAYER)["y"]
+    keep = [r for r in range(40) if r not in (7, 20, 30)]
+    assert torch.equal(y[keep], ok[keep])
+    assert bool(torch.isnan(y[7]).all()) and bool(torch.isnan(y[20]).any()) and bool((y[30] == 0).all())
+
+
+# ---- linear --------------------------------------------------------------------------------------------------------
+LINEAR_SIZES = [(1, 1, 1), (1, 64, 64), (1, 4096, 130), (2, 100, 9), (3, 65, 1000), (4, 1000, 333), (5, 4100, 96), (8, 512, 512),
+                (13, 777, 40), (16, 64, 2000), (17, 333, 257), (31, 1023, 65), (32, 2048, 128), (33, 128, 300), (64, 1000, 64),
+                (65, 72, 1000), (100, 264, 136), (128, 128, 128), (129, 129, 129), (200, 1365, 190), (256, 8, 256), (257, 640, 520),
+                (300, 4096, 72), (513, 1000, 260), (1000, 200, 1365), (2050, 264, 40), (5000, 40, 24), (7, 8200, 16)]
+
+
+def linear_case(tfla, M, K, N, dtype, act, seed, shift=0, bias=True, residual=True):
+    gen = generator(seed)
+    x = fenced(normal(gen, M, K, dtype=dtype), shift)
+    w = fenced(normal(gen, N, K, std=K ** -0.5, dtype=dtype), shift)
+    b = fenced(normal(gen, N, std=0.3), shift) if bias else None
+    r = fenced(normal(gen, M, N, dtype=dtype), shift) if residual else None
+    f = tfla.linear_fwd(x, w, b, r, act=code(tfla, act), keep_pre=True)
+    z, y = bu.linear(x, w, b, r, act)
+    bu.within("z", f["z"], *z)
+    bu.within("y", f["y"], *y)
+    dy = fenced(normal(gen, M, N, dtype=dtype), shift)
+    g = tfla.linear_bwd(x, w, dy, f["z"], act=code(tfla, act), want_db=True)
+    s = bu.act_grad(f["z"].to(bu.F64), act)
+    dz = dy.to(bu.F64) * s
+    edz = torch.zeros_like(dz) if act == "none" else bu.FN * dy.to(bu.F64).abs() * (1 + f["z"].to(bu.F64).abs())
+    dx, dw, db = bu.back([dz], [edz], x, [w], dtype)
+    bu.within("dx", g["dx"], *dx)
+    bu.within("dw", g["dw"], *dw[0])
+    bu.within("db", g["db"], *db[0])
+
+
+@pytest.mark.parametrize("i", range(len(LINEAR_SIZES)))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_linear(tfla, i, dtype):
+    M, K, N = LINEAR_SIZES[i]
+    act = ACTS[i % 4]
+    print("linear", M, K, N, dtype, act, flush=True)
+    linear_case(tfla, M, K, N, dtype, act, seed=i, bias=i % 3 != 1, residual=i % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype,act", list(itertools.product([BF16, F32], ACTS)))
+@pytest.mark.parametrize("M,K,N", [(3, 128, 64), (70, 200, 136), (300, 256, 512)])
+def test_linear_at_odd_addresses(tfla, M, K, N, dtype, act):
+    print("linear odd", M, K, N, dtype, act, flush=True)
+    linear_case(tfla, M, K, N, dtype, act, seed=M, shift=1)
+    linear_case(tfla, M, K, N, dtype, act, seed=M, shift=2)
+
+
+# ---- gated ---------------------------------------------------------------------------------------------------------
+GATED_SIZES = [(1, 1, 1), (1, 1024, 1500), (2, 40, 33), (4, 512, 1365), (7, 777, 72), (16, 128, 64), (20, 65, 200), (33, 1000, 100),
+               (64, 64, 64), (100, 320, 129), (129, 136, 264), (256, 512, 96), (300, 1000, 341), (1030, 264, 520), (3000, 72, 40)]
+
+
+@pytest.mark.parametrize("i", range(len(GATED_SIZES)))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_gated(tfla, i, dtype, shift):
+    M, K, N = GATED_SIZES[i]
+    act, bias = ACTS[(i + 1) % 4], i % 2 == 0
+    print("gated", M, K, N, dtype, act, shift, flush=True)
+    gen = generator(100 + i)
+    x = fenced(normal(gen, M, K, dtype=dtype), shift)
+    wg, wu = (fenced(normal(gen, N, K, std=K ** -0.5, dtype=dtype), shift) for _ in range(2))
+    bg, bb = (fenced(normal(gen, N, std=0.3), shift) if bias else None for _ in range(2))
+    f = tfla.gated_fwd(x, wg, wu, bg, bb, act=code(tfla, act), keep_pre=True)
+    a, u, h = bu.gated(x, wg, wu, bg, bb, act)
+    bu.within("a", f["a"], *a)
+    bu.within("u", f["u"], *u)
+    bu.within("h", f["h"], *h)
+    lean = tfla.gated_fwd(x, wg, wu, bg, bb, act=code(tfla, act))
+    assert "a" not in lean and torch.equal(lean["h"], f["h"])
+    dh = fenced(normal(gen, M, N, dtype=dtype), shift)
+    g = tfla.gated_bwd(x, wg, wu, f["a"], f["u"], dh, act=code(tfla, act), want_db=True)
+    av, uv, d = f["a"].to(bu.F64), f["u"].to(bu.F64), dh.to(bu.F64)
+    da, du = d * uv * bu.act_grad(av, act), d * bu.act(av, act)
+    e = bu.FN * (1 + av.abs()) * d.abs()
+    dx, dw, db = bu.back([da, du], [e * uv.abs() + bu.U * da.abs(), e + bu.U * du.abs()], x, [wg, wu], dtype)
+    bu.within("dx", g["dx"], *dx)
+    for name, r in (("dw_gate", dw[0]), ("dw_up", dw[1]), ("db_gate", db[0]), ("db_up", db[1])):
+        bu.within(name, g[name], *r)
+
+
+# ---- what a caller may leave out, and calls of nothing -------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_parts_that_are_not_wanted(tfla, dtype):
+    gen = generator(9)
+    x, w, w2, dy = (normal(gen, *s, dtype=dtype) for s in ((50, 72), (88, 72), (88, 72), (50, 88)))
+    full = tfla.linear_bwd(x, w, dy, want_db=True)
+    for want in ("dx", "dw", "db"):
+        one = tfla.linear_bwd(x, w, dy, want_dx=want == "dx", want_dw=want == "dw", want_db=want == "db")
+        assert sorted(one) == sorted([want, "workspace"]) and torch.equal(one[want], full[want])
+    f = tfla.gated_fwd(x, w, w2, keep_pre=True)
+    full = tfla.gated_bwd(x, w, w2, f["a"], f["u"], dy, want_db=True)
+    one = tfla.gated_bwd(x, w, w2, f["a"], f["u"], dy, want_dw=False)
+    assert sorted(one) == ["dx", "workspace"] and torch.equal(one["dx"], full["dx"])
+    one = tfla.gated_bwd(x, w, w2, f["a"], f["u"], dy, want_dx=False)
+    assert torch.equal(one["dw_up"], full["dw_up"]) and "dx" not in one
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_no_tokens(tfla, dtype):
+    x, w = torch.empty((0, 40), dtype=dtype, device="cuda"), torch.ones((24, 40), dtype=dtype, device="cuda")
+    dy = torch.empty((0, 24), dtype=dtype, device="cuda")
+    assert tfla.norm_fwd(x)["y"].shape == (0, 40)
+    nan = float("nan")
+    o = {"dgamma": torch.full((40,), nan, device="cuda"), "dbeta": torch.full((40,), nan, device="cuda")}
+    tfla.norm_bwd(x, x, torch.empty(0, device="cuda"), want_dbeta=True, out=o)
+    assert not o["dgamma"].any() and not o["dbeta"].any()
+    assert tfla.linear_fwd(x, w)["y"].shape == (0, 24)
+    o = {"dw": torch.full_like(w, nan), "db": torch.full((24,), nan, device="cuda")}
+    tfla.linear_bwd(x, w, dy, want_db=True, out=o)
+    assert not o["dw"].any() and not o["db"].any()
+    assert tfla.gated_fwd(x, w, w)["h"].shape == (0, 24)
+    o = {"dw_gate": torch.full_like(w, nan), "dw_up": torch.full_like(w, nan)}
+    tfla.gated_bwd(x, w, w, dy, dy, dy, want_db=True, out=o)
+    assert not o["dw_gate"].any() and not o["dw_up"].any() and not o["db_gate"].any() and not o["db_up"].any()
+
+
+@pytest.mark.parametrize("M", [3, 40, 300])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_bad_tokens_stay_in_their_rows(tfla, M, dtype):
+    gen = generator(M)
+    x, w, wu = normal(gen, M, 333, dtype=dtype), normal(gen, 200, 333, std=0.05, dtype=dtype), normal(gen, 200, 333, std=0.05, dtype=dtype)
+    y, h = tfla.linear_fwd(x, w)["y"], tfla.gated_fwd(x, w, wu)["h"]
+    x[1] = float("nan"); x[2, 3] = float("inf")
+    y2, h2 = tfla.linear_fwd(x, w)["y"], tfla.gated_fwd(x, w, wu)["h"]
+    keep = [r for r in range(M) if r not in (1, 2)]
+    assert torch.equal(y[keep], y2[keep]) and torch.equal(h[keep], h2[keep])
+    assert bool(torch.isnan(y2[1]).all()) and bool(torch.isnan(h2[1]).all())
+    assert torch.equal(y2[2].float(), torch.where(w[:, 3] > 0, float("inf"), -float("inf")))
+
+
+# ---- differences ---------------------------------------------------------------------------------------------------
+def test_gradients_against_differences(tfla):
+    """fp32 gradients of the chain norm -> gated -> linear with residual against central differences of the 64-bit forms along
+    random directions.  The step's own error is of its square, 1e-8 of the third derivative; the kernels' errors are a few
+    hundred roundings of 2^-24 in the sums: 1e-4 of the largest of the terms covers both."""
+    gen = generator(77)
+    M, D, N = 23, 72, 52
+    p = {"x": normal(gen, M, D), "gamma": normal(gen, D, mean=1.0, std=0.2), "beta": normal(gen, D, std=0.2),
+         "wg": normal(gen, N, D, std=D ** -0.5), "wu": normal(gen, N, D, std=D ** -0.5), "bg": normal(gen, N, std=0.2),
+         "wo": normal(gen, D, N, std=N ** -0.5), "bo": normal(gen, D, std=0.2)}
+    dy = normal(gen, M, D)
+
+    def value(q):
+        y = bu.norm(q["x"], q["gamma"], q["beta"], True, 1e-5)[2][0]
+        a, u = y @ q["wg"].t() + q["bg"], y @ q["wu"].t()
+        h = bu.act(a, "silu") * u
+        return float(((q["x"] + bu.act(h @ q["wo"].t() + q["bo"], "gelu")) * dy.double()).sum())
+
+    n = tfla.norm_fwd(p["x"], p["gamma"], p["beta"], norm_kind=tfla.NORM_LAYER, norm_eps=1e-5)
+    f = tfla.gated_fwd(n["y"], p["wg"], p["wu"], p["bg"], keep_pre=True)
+    o = tfla.linear_fwd(f["h"], p["wo"], p["bo"], p["x"], act=tfla.ACT_GELU, keep_pre=True)
+    assert o["y"].shape == (M, D)
+    bo = tfla.linear_bwd(f["h"], p["wo"], dy, o["z"], act=tfla.ACT_GELU, want_db=True)
+    bg = tfla.gated_bwd(n["y"], p["wg"], p["wu"], f["a"], f["u"], bo["dx"], want_db=True)
+    bn = tfla.norm_bwd(p["x"], bg["dx"], n["rstd"], n["mean"], p["gamma"], dy, norm_kind=tfla.NORM_LAYER, want_dbeta=True)
+    grads = {"x": bn["dx"], "gamma": bn["dgamma"], "beta": bn["dbeta"], "wg": bg["dw_gate"], "wu": bg["dw_up"], "bg": bg["db_gate"],
+             "wo": bo["dw"], "bo": bo["db"]}
+    p64 = {k: v.double() for k, v in p.items()}
+    for k, g in grads.items():
+        d = normal(gen, *p[k].shape).double()
+        e = 1e-4
+        diff = (value(dict(p64, **{k: p64[k] + e * d})) - value(dict(p64, **{k: p64[k] - e * d}))) / (2 * e)
+        got = float((g.double() * d).sum())
+        assert abs(got - diff) <= 1e-4 * float((g.double() * d).abs().sum()), (k, got, diff)
+
+
+# ---- streams and graphs --------------------------------------------------------------------------------------------
+def _chain(tfla, t, o, stream=None):
+    n = tfla.norm_fwd(t["x"], t["gamma"], out=o["n"], stream=stream)
+    f = tfla.gated_fwd(n["y"], t["wg"], t["wu"], keep_pre=True, out=o["g"], stream=stream)
+    y = tfla.linear_fwd(f["h"], t["wo"], residual=t["x"], out=o["l"], stream=stream)
+    bl = tfla.linear_bwd(f["h"], t["wo"], t["dy"], out=o["bl"], want_db=True, stream=stream)
+    bg = tfla.gated_bwd(n["y"], t["wg"], t["wu"], f["a"], f["u"], bl["dx"], out=o["bg"], stream=stream)
+    bn = tfla.norm_bwd(t["x"], bg["dx"], n["rstd"], gamma=t["gamma"], d_residual=t["dy"], out=o["bn"], stream=stream)
+    return [y["y"], bl["dw"], bl["db"], bg["dw_gate"], bg["dw_up"], bn["dx"], bn["dgamma"]]
+
+
+def _chain_inputs(M, dtype, seed):
+    gen = generator(seed)
+    D, N = 200, 333
+    return {"x": normal(gen, M, D, dtype=dtype), "gamma": normal(gen, D), "wg": normal(gen, N, D, std=0.1, dtype=dtype),
+            "wu": normal(gen, N, D, std=0.1, dtype=dtype), "wo": normal(gen, D, N, std=0.1, dtype=dtype), "dy": normal(gen, M, D, dtype=dtype)}
+
+
+@pytest.mark.parametrize("M,dtype", [(1, BF16), (130, BF16), (77, F32)])
+def test_another_stream_and_a_graph(tfla, M, dtype):
+    names = ("n", "g", "l", "bl", "bg", "bn")
+    t = _chain_inputs(M, dtype, 5)
+    want = [v.clone() for v in _chain(tfla, t, {k: {} for k in names})]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o = {k: {} for k in names}
+    got = _chain(tfla, t, o, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        res = _chain(tfla, t, o)
+    for rep in range(4):
+        fresh = _chain_inputs(M, dtype, 50 + rep)
+        for k in t:
+            t[k].copy_(fresh[k])
+        for r in res:
+            r.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        want = _chain(tfla, fresh, {k: {} for k in names})
+        assert all(torch.equal(a, b) for a, b in zip(want, res)), rep
