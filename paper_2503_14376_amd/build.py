@@ -19,6 +19,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 # vector ALU instructions, which cannot read accumulation registers)
 UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "step.o", []), ("norm.hip", "norm.o", []),
          ("block_api.hip", "block_api.o", []), ("block_elem.hip", "block_elem.o", []), ("rownorm.hip", "rownorm.o", []),
+         ("gemm_rows.hip", "gemm_rows.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
          ("recurrent.hip", "recurrent.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"])] + [
     # tile kernels: the start-up loop over X and state slices must unroll completely (its items differ in kind and
     # index registers by compile-time constants); with the widest shapes its body exceeds the default size limit

@@ -51,6 +51,7 @@ struct FwdLayout {
 };
 FwdLayout fwd_layout(int M, int K, int N, int dtype, bool pair, bool x_off, bool w_off) {
     FwdLayout l{};
+    if (M <= GEMM_ROWS_MAX) return l;      // that kernel reads the tensors where they are
     const size_t e = esize(dtype), Kp = padded(K);
     l.plan = gemm_plan(M, N, K, 1, 1, pair, dtype);
     l.move_x = K % group(dtype) != 0 || x_off;
@@ -125,6 +126,10 @@ int product_fwd(const void* x, const void* const (&w)[2], const float* const (&b
     g.M = M; g.N = N; g.K = K; g.segs = 1; g.batch = 1; g.pair = pair;
     g.bias[0] = bias[0]; g.bias[1] = bias[1]; g.residual = residual; g.out[0] = out; g.z[0] = z[0]; g.z[1] = z[1];
     g.act = act; g.dtype = dtype;
+    if (M <= GEMM_ROWS_MAX) {
+        TFLA_LAUNCH(K_GEMM, launch_gemm_rows(g, s));
+        return TFLA_OK;
+    }
     g.split = l.plan.split; g.part = reinterpret_cast<float*>(ws + l.part); g.ld_part = (N + 7) & ~7;
     TFLA_LAUNCH(K_GEMM, launch_gemm(g, l.plan, false, false, pair ? EPI_GATED : EPI_LINEAR, s));
     return TFLA_OK;

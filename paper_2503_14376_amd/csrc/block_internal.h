@@ -47,6 +47,9 @@ struct GemmArgs {
 // how a product is cut (a rule on its sizes): used for the workspace and by the launcher
 struct GemmPlan { int bm, bn, split; };
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype);
+// Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens)
+constexpr int GEMM_ROWS_MAX = 32;
+hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s);
 
 // ---- elementwise passes around the products ---------------------------------------------------
