@@ -127,6 +127,8 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype) {
     GemmPlan p;
     p.bm = p.bn = dtype == 1 ? 128 : 64;
+    const int bno = pair ? 128 : 256;
+    if (dtype == 1 && (M + 255) / 256 * ((N + bno - 1) / bno) * batch >= 256) p.bm = p.bn = 256;
     p.split = 1;
     return p;
 }

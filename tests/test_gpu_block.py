@@ -145,8 +145,16 @@ def test_linear_at_odd_addresses(tfla, M, K, N, dtype, act):
     linear_case(tfla, M, K, N, dtype, act, seed=M, shift=2)
 
 
+# sizes at which the products take their largest tiles, each one in turn the contraction, with ends inside tiles
+@pytest.mark.parametrize("M,K,N", [(4100, 200, 4111), (4360, 4104, 130), (150, 4100, 4360), (4097, 4097, 64), (9000, 72, 2056)])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_linear_large(tfla, M, K, N, act):
+    print("linear large", M, K, N, act, flush=True)
+    linear_case(tfla, M, K, N, BF16, act, seed=N, residual=act == "none")
+
+
 # ---- gated ---------------------------------------------------------------------------------------------------------
-GATED_SIZES = [(1, 1, 1), (1, 1024, 1500), (2, 40, 33), (4, 512, 1365), (7, 777, 72), (16, 128, 64), (20, 65, 200), (33, 1000, 100),
+GATED_SIZES = [(4100, 136, 2100), (4100, 4100, 40), (136, 4200, 2056), (1, 1, 1), (1, 1024, 1500), (2, 40, 33), (4, 512, 1365), (7, 777, 72), (16, 128, 64), (20, 65, 200), (33, 1000, 100),
                (64, 64, 64), (100, 320, 129), (129, 136, 264), (256, 512, 96), (300, 1000, 341), (1030, 264, 520), (3000, 72, 40)]
 
 
