@@ -57,8 +57,8 @@ __device__ __forceinline__ void wave_epilogue(const GemmArgs& a, const GemmWork&
         for (int nb = 0; nb < NB; ++nb) S::put(area, acc[mb][nb], nb * 32, lane);
         // (the area is this wavefront's own: only its own writes have to have arrived)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-        for (int p = 0; p < 32 / RPP; ++p) {
+#pragma unroll 1
+        for (int p = 0; p < 32 / RPP; ++p) {        // (a loop: unrolled, the activations alone are thousands of instructions)
             const int r = p * RPP + lane / LPR, c = (lane % LPR) * 8;
             float v[8], u[8];
             if constexpr (PAIR) {

@@ -1,34 +1,35 @@
-// bf16 products in tiles of 256 x 256: eight wavefronts, two per SIMD, each with 128 x 64 results in registers.
+// bf16 products in tiles of 256 x 256: four wavefronts, one per SIMD, each with 128 x 128 results in its accumulation registers.
+// (Eight wavefronts of 128 x 64 read half as much again from LDS; under load the clock goes by the power that is drawn.)
 //
-// A step of the contraction is 64 wide.  Each operand's tile is kept as two halves (half h of A: of every wavefront's 128
-// rows the 64 from 64 h on; of B: of its 64 columns the 32 from 32 h on; of a pair: half h is matrix h), in two slots each: 128 KB.
-// A step has two phases of 16 matrix instructions per wavefront, with one barrier each:
+// A step of the contraction is 64 wide.  Each operand's tile is kept as two halves (half h: of every wavefront's 128 rows or
+// columns the 64 from 64 h on; of a pair's columns: matrix h), in two slots each: 128 KB.  A step has two phases of 32 matrix
+// instructions per wavefront, with one barrier each:
 //   X: A0 B0, then A0 B1, while the fragments of B1 and A1 are read;      requests A0, B0 of the step after the next
 //   Y: A1 B0, then A1 B1, while those of the next step's A0 and B0 are;   requests A1, B1 of the step after the next
-// so that fragments are in registers a phase before they are used, a half's memory is requested anew the phase after its last
-// read, and requests have three phases (some 3000 clocks) to arrive: at every phase's start eight requests per wavefront may
-// be under way.  Steps behind the last request nothing (bounds of zero bytes), which keeps the counts.
+// so that a half's memory is requested anew the phase after its last read, and requests have three phases (some 3000 clocks)
+// to arrive: at every phase's start sixteen requests per wavefront may be under way.  Steps behind the last request nothing
+// (bounds of zero bytes), which keeps the counts.  One LDS read or request stands between any two matrix instructions.
 #pragma once
 #include "gemm.h"
 
 namespace tfla {
 
-// One operand's requests.  A half is 128 output rows (or columns) x 64 steps, 16 KB, two requests of each of 512 threads; its
+// One operand's requests.  A half is 128 output rows (or columns) x 64 steps, 16 KB, four requests of each of 256 threads; its
 // local row r stands for row (r / G) 2 G + r % G of the operand behind the half's first row.  The buffer descriptors of both
 // halves are kept ready and moved on by a step at a time; everything else about them is found anew only at the steps where
 // it changes (the last step of a contraction that is no multiple of 64, the second segment, the end).
 template <bool TR, int G, bool PAIR> struct WideOperand {
-    typedef DmaTile<TR ? 64 : 128, TR ? 128 : 64, 512, TR ? SWZ_T : SWZ_K> Shape;
-    static constexpr int CPR = Shape::CPR, N = 2;
+    typedef DmaTile<TR ? 64 : 128, TR ? 128 : 64, 256, TR ? SWZ_T : SWZ_K> Shape;
+    static constexpr int CPR = Shape::CPR, N = 4;
     static constexpr uint32_t BEHIND = 0x40000000u;       // an offset beyond every bound
-    static_assert(Shape::N == N, "two requests per half");
+    static_assert(Shape::N == N, "four requests per half");
     u32x4 d[2];                 // descriptors of the halves at the next step
     uint32_t goff[N], hop;      // byte offsets of this lane; bytes from step to step
     __device__ __forceinline__ void init(long ld, int tid) {
         const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int q = (wave + j * 8) * 64 + lane, r = q / CPR, c = ((q % CPR) ^ swz_mask<TR ? SWZ_T : SWZ_K, CPR>(r)) * 8;
+            const int q = (wave + j * 4) * 64 + lane, r = q / CPR, c = ((q % CPR) ^ swz_mask<TR ? SWZ_T : SWZ_K, CPR>(r)) * 8;
             const int row = TR ? r : (r / G) * 2 * G + r % G, col = TR ? (c / G) * 2 * G + c % G : c;
             goff[j] = (uint32_t)((row * ld + col) * 2);
         }
@@ -52,7 +53,7 @@ template <bool TR, int G, bool PAIR> struct WideOperand {
             const int lane = tid & 63, wave = tid >> 6, left = ((K + 7) & ~7) - k0;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const int q = (wave + j * 8) * 64 + lane, c = ((q % CPR) ^ swz_mask<SWZ_K, CPR>(q / CPR)) * 8;
+                const int q = (wave + j * 4) * 64 + lane, c = ((q % CPR) ^ swz_mask<SWZ_K, CPR>(q / CPR)) * 8;
                 goff[j] = (goff[j] & (BEHIND - 1)) | (c < left ? 0u : BEHIND);
             }
         }
@@ -68,17 +69,17 @@ template <bool TR, int G, bool PAIR> struct WideOperand {
     // request j of half H into the half at LDS address `half` (of this wavefront's part of it)
     template <int H> __device__ __forceinline__ void issue(int j, uint32_t half) const {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     :: "s"(half + j * 8192), "v"(goff[j]), "s"(d[H]) : "m0");
+                     :: "s"(half + j * 4096), "v"(goff[j]), "s"(d[H]) : "m0");
     }
 };
 
 template <bool ATR, bool BTR, bool PAIR, int EPI>
-__global__ void __launch_bounds__(512, 2) gemm_bf16_wide_kernel(GemmArgs a, int tms, int tns) {
+__global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int tms, int tns) {
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     constexpr int HALF = 16384, SLOT = 2 * HALF, OPERAND = 2 * SLOT;
     __shared__ __align__(1024) char lds[2 * OPERAND];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 2, wn = wave & 3;
+    const int wm = wave >> 1, wn = wave & 1;
     const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
     const long row0 = (long)w.tm * 256;
     const int col0 = w.tn * (PAIR ? 128 : 256);
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(512, 2) gemm_bf16_wide_kernel(GemmArgs a, int 
     const int per = (all + a.split - 1) / a.split, k_begin = w.part * per, k_end = min(all, k_begin + per);
 
     WideOperand<ATR, 64, false> oa;
-    WideOperand<BTR, PAIR ? 128 : 32, PAIR> ob;
+    WideOperand<BTR, PAIR ? 128 : 64, PAIR> ob;
     oa.init(a.lda, tid);
     ob.init(a.ldb, tid);
     // the next step to request, and the next at which its descriptors change by more than a step
@@ -109,52 +110,47 @@ __global__ void __launch_bounds__(512, 2) gemm_bf16_wide_kernel(GemmArgs a, int 
         ob.advance();                                      \
         if (rt == change) find();                          \
     } while (0)
-#define TFLA_REQUEST(H)                                    \
-    do {                                                   \
-        oa.template issue<H>(0, la + rslot + (H) * HALF);  \
-        oa.template issue<H>(1, la + rslot + (H) * HALF);  \
-        ob.template issue<H>(0, lb + rslot + (H) * HALF);  \
-        ob.template issue<H>(1, lb + rslot + (H) * HALF);  \
-    } while (0)
+#define TFLA_REQUEST(H)                                                                                  \
+    _Pragma("unroll") for (int j = 0; j < 4; ++j) oa.template issue<H>(j, la + rslot + (H) * HALF);    \
+    _Pragma("unroll") for (int j = 0; j < 4; ++j) ob.template issue<H>(j, lb + rslot + (H) * HALF);
 
     // fragments: per lane offsets into a half
     KFragReader<64> kf;
-    uint32_t ta[2], tb;
+    uint32_t ta[2], tb[2];
     if constexpr (!ATR || !BTR) kf.init(lane & 31, lane >> 5);
-    if constexpr (ATR) { ta[0] = TFragReader<128>::offset_of(lane, 8, wm * 2); ta[1] = TFragReader<128>::offset_of(lane, 8, wm * 2 + 1); }
-    if constexpr (BTR) tb = TFragReader<128>::offset_of(lane, 8, wn);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (ATR) ta[i] = TFragReader<128>::offset_of(lane, 8, wm * 2 + i);
+        if constexpr (BTR) tb[i] = TFragReader<128>::offset_of(lane, 8, wn * 2 + i);
+    }
     const char* la_p = lds + (ATR ? 0 : wm * 64 * 128);
-    const char* lb_p = lds + OPERAND + (BTR ? 0 : wn * 32 * 128);
-    // fragments of contraction steps 16 ks ... of half H in slot offset SO
-#define TFLA_FRAG_A(DST, H, SO, ks)                                                                           \
-    _Pragma("unroll") for (int i = 0; i < 2; ++i) {                                                           \
-        if constexpr (ATR) DST[i][ks] = TFragReader<128>::load_at(la_p + (SO) + (H) * HALF, ta[i], (ks) * 16, (ks) * 16 + 4); \
-        else DST[i][ks] = kf.load(la_p + (SO) + (H) * HALF, ks, i);                                           \
-    }
-#define TFLA_FRAG_B(DST, H, SO, ks)                                                                           \
-    {                                                                                                         \
-        if constexpr (BTR) DST[ks] = TFragReader<128>::load_at(lb_p + (SO) + (H) * HALF, tb, (ks) * 16, (ks) * 16 + 4); \
-        else DST[ks] = kf.load(lb_p + (SO) + (H) * HALF, ks, 0);                                              \
-    }
-    // two matrix instructions, and a line that the scheduler keeps what stands around them on its side of
-#define TFLA_MUL(A, B, HA, HB, ks)                                                                            \
+    const char* lb_p = lds + OPERAND + (BTR ? 0 : wn * 64 * 128);
+    // fragment of block i (32 rows or columns), contraction steps 16 ks ..., of half H in slot offset SO
+#define TFLA_FRAG_A(DST, H, SO, i, ks)                                                                        \
+    if constexpr (ATR) DST[i][ks] = TFragReader<128>::load_at(la_p + (SO) + (H) * HALF, ta[i], (ks) * 16, (ks) * 16 + 4); \
+    else DST[i][ks] = kf.load(la_p + (SO) + (H) * HALF, ks, i);
+#define TFLA_FRAG_B(DST, H, SO, i, ks)                                                                        \
+    if constexpr (BTR) DST[i][ks] = TFragReader<128>::load_at(lb_p + (SO) + (H) * HALF, tb[i], (ks) * 16, (ks) * 16 + 4); \
+    else DST[i][ks] = kf.load(lb_p + (SO) + (H) * HALF, ks, i);
+    // one matrix instruction; the scheduler keeps what stands around it on its side.  (Blocks of a pair alternate.)
+#define TFLA_MUL(A, B, HA, HB, i, j, ks)                                                                      \
     __builtin_amdgcn_sched_barrier(0);                                                                        \
-    _Pragma("unroll") for (int i = 0; i < 2; ++i)                                                             \
-        acc[(HA) * 2 + i][HB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i][ks], B[ks], acc[(HA) * 2 + i][HB], 0, 0, 0);
+    acc[(HA) * 2 + i][PAIR ? (j) * 2 + HB : (HB) * 2 + j] =                                                   \
+        __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i][ks], B[j][ks], acc[(HA) * 2 + i][PAIR ? (j) * 2 + HB : (HB) * 2 + j], 0, 0, 0);
 #define TFLA_PHASE()                                       \
     do {                                                   \
-        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory"); \
+        asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory"); \
         barrier_nofence();                                 \
     } while (0)
 
-    f32x16 acc[4][2];
+    f32x16 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-    bf16x8 a0[2][4], a1[2][4], b0[4], b1[4];
+    bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
     if (k_begin < k_end) {
         find();
         TFLA_REQUEST(0);
@@ -163,59 +159,133 @@ __global__ void __launch_bounds__(512, 2) gemm_bf16_wide_kernel(GemmArgs a, int 
         TFLA_REQUEST(0);
         TFLA_REQUEST(1);
         TFLA_NEXT();
-        wait_vmcnt<12>();
+        wait_vmcnt<24>();
         barrier_nofence();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            TFLA_FRAG_A(a0, 0, 0, ks)
-            TFLA_FRAG_B(b0, 0, 0, ks)
-        }
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                TFLA_FRAG_A(a0, 0, 0, i, ks)
+                TFLA_FRAG_B(b0, 0, 0, i, ks)
+            }
         uint32_t so = 0;
         for (int t = k_begin; t < k_end; ++t) {
             TFLA_PHASE();
-            TFLA_MUL(a0, b0, 0, 0, 0)
-            TFLA_FRAG_B(b1, 1, so, 0)
-            TFLA_FRAG_B(b1, 1, so, 1)
-            TFLA_MUL(a0, b0, 0, 0, 1)
-            TFLA_FRAG_B(b1, 1, so, 2)
-            TFLA_FRAG_B(b1, 1, so, 3)
-            TFLA_MUL(a0, b0, 0, 0, 2)
-            TFLA_FRAG_A(a1, 1, so, 0)
+            TFLA_MUL(a0, b0, 0, 0, 0, 0, 0)
+            TFLA_FRAG_B(b1, 1, so, 0, 0)
+            TFLA_MUL(a0, b0, 0, 0, 0, 1, 0)
+            TFLA_FRAG_B(b1, 1, so, 1, 0)
+            TFLA_MUL(a0, b0, 0, 0, 1, 0, 0)
+            TFLA_FRAG_B(b1, 1, so, 0, 1)
+            TFLA_MUL(a0, b0, 0, 0, 1, 1, 0)
+            TFLA_FRAG_B(b1, 1, so, 1, 1)
+            TFLA_MUL(a0, b0, 0, 0, 0, 0, 1)
+            TFLA_FRAG_B(b1, 1, so, 0, 2)
+            TFLA_MUL(a0, b0, 0, 0, 0, 1, 1)
+            TFLA_FRAG_B(b1, 1, so, 1, 2)
+            TFLA_MUL(a0, b0, 0, 0, 1, 0, 1)
+            TFLA_FRAG_B(b1, 1, so, 0, 3)
+            TFLA_MUL(a0, b0, 0, 0, 1, 1, 1)
+            TFLA_FRAG_B(b1, 1, so, 1, 3)
+            TFLA_MUL(a0, b0, 0, 0, 0, 0, 2)
+            TFLA_FRAG_A(a1, 1, so, 0, 0)
+            TFLA_MUL(a0, b0, 0, 0, 0, 1, 2)
             oa.template issue<0>(0, la + rslot);
-            TFLA_MUL(a0, b0, 0, 0, 3)
-            TFLA_FRAG_A(a1, 1, so, 1)
+            TFLA_MUL(a0, b0, 0, 0, 1, 0, 2)
+            TFLA_FRAG_A(a1, 1, so, 1, 0)
+            TFLA_MUL(a0, b0, 0, 0, 1, 1, 2)
             oa.template issue<0>(1, la + rslot);
-            TFLA_MUL(a0, b1, 0, 1, 0)
-            TFLA_FRAG_A(a1, 1, so, 2)
+            TFLA_MUL(a0, b0, 0, 0, 0, 0, 3)
+            TFLA_FRAG_A(a1, 1, so, 0, 1)
+            TFLA_MUL(a0, b0, 0, 0, 0, 1, 3)
+            oa.template issue<0>(2, la + rslot);
+            TFLA_MUL(a0, b0, 0, 0, 1, 0, 3)
+            TFLA_FRAG_A(a1, 1, so, 1, 1)
+            TFLA_MUL(a0, b0, 0, 0, 1, 1, 3)
+            oa.template issue<0>(3, la + rslot);
+            TFLA_MUL(a0, b1, 0, 1, 0, 0, 0)
+            TFLA_FRAG_A(a1, 1, so, 0, 2)
+            TFLA_MUL(a0, b1, 0, 1, 0, 1, 0)
             ob.template issue<0>(0, lb + rslot);
-            TFLA_MUL(a0, b1, 0, 1, 1)
-            TFLA_FRAG_A(a1, 1, so, 3)
+            TFLA_MUL(a0, b1, 0, 1, 1, 0, 0)
+            TFLA_FRAG_A(a1, 1, so, 1, 2)
+            TFLA_MUL(a0, b1, 0, 1, 1, 1, 0)
             ob.template issue<0>(1, lb + rslot);
-            TFLA_MUL(a0, b1, 0, 1, 2)
-            TFLA_MUL(a0, b1, 0, 1, 3)
+            TFLA_MUL(a0, b1, 0, 1, 0, 0, 1)
+            TFLA_FRAG_A(a1, 1, so, 0, 3)
+            TFLA_MUL(a0, b1, 0, 1, 0, 1, 1)
+            ob.template issue<0>(2, lb + rslot);
+            TFLA_MUL(a0, b1, 0, 1, 1, 0, 1)
+            TFLA_FRAG_A(a1, 1, so, 1, 3)
+            TFLA_MUL(a0, b1, 0, 1, 1, 1, 1)
+            ob.template issue<0>(3, lb + rslot);
+            TFLA_MUL(a0, b1, 0, 1, 0, 0, 2)
+            TFLA_MUL(a0, b1, 0, 1, 0, 1, 2)
+            TFLA_MUL(a0, b1, 0, 1, 1, 0, 2)
+            TFLA_MUL(a0, b1, 0, 1, 1, 1, 2)
+            TFLA_MUL(a0, b1, 0, 1, 0, 0, 3)
+            TFLA_MUL(a0, b1, 0, 1, 0, 1, 3)
+            TFLA_MUL(a0, b1, 0, 1, 1, 0, 3)
+            TFLA_MUL(a0, b1, 0, 1, 1, 1, 3)
             so ^= SLOT;
             TFLA_PHASE();
-            TFLA_MUL(a1, b0, 1, 0, 0)
-            TFLA_FRAG_A(a0, 0, so, 0)
-            TFLA_MUL(a1, b0, 1, 0, 1)
-            TFLA_FRAG_A(a0, 0, so, 1)
-            TFLA_MUL(a1, b0, 1, 0, 2)
-            TFLA_FRAG_A(a0, 0, so, 2)
+            TFLA_MUL(a1, b0, 1, 0, 0, 0, 0)
+            TFLA_FRAG_A(a0, 0, so, 0, 0)
+            TFLA_MUL(a1, b0, 1, 0, 0, 1, 0)
             oa.template issue<1>(0, la + rslot + HALF);
-            TFLA_MUL(a1, b0, 1, 0, 3)
-            TFLA_FRAG_A(a0, 0, so, 3)
+            TFLA_MUL(a1, b0, 1, 0, 1, 0, 0)
+            TFLA_FRAG_A(a0, 0, so, 1, 0)
+            TFLA_MUL(a1, b0, 1, 0, 1, 1, 0)
             oa.template issue<1>(1, la + rslot + HALF);
-            TFLA_MUL(a1, b1, 1, 1, 0)
-            TFLA_FRAG_B(b0, 0, so, 0)
-            TFLA_FRAG_B(b0, 0, so, 1)
+            TFLA_MUL(a1, b0, 1, 0, 0, 0, 1)
+            TFLA_FRAG_A(a0, 0, so, 0, 1)
+            TFLA_MUL(a1, b0, 1, 0, 0, 1, 1)
+            oa.template issue<1>(2, la + rslot + HALF);
+            TFLA_MUL(a1, b0, 1, 0, 1, 0, 1)
+            TFLA_FRAG_A(a0, 0, so, 1, 1)
+            TFLA_MUL(a1, b0, 1, 0, 1, 1, 1)
+            oa.template issue<1>(3, la + rslot + HALF);
+            TFLA_MUL(a1, b0, 1, 0, 0, 0, 2)
+            TFLA_FRAG_A(a0, 0, so, 0, 2)
+            TFLA_MUL(a1, b0, 1, 0, 0, 1, 2)
             ob.template issue<1>(0, lb + rslot + HALF);
-            TFLA_MUL(a1, b1, 1, 1, 1)
-            TFLA_FRAG_B(b0, 0, so, 2)
-            TFLA_FRAG_B(b0, 0, so, 3)
+            TFLA_MUL(a1, b0, 1, 0, 1, 0, 2)
+            TFLA_FRAG_A(a0, 0, so, 1, 2)
+            TFLA_MUL(a1, b0, 1, 0, 1, 1, 2)
             ob.template issue<1>(1, lb + rslot + HALF);
-            TFLA_MUL(a1, b1, 1, 1, 2)
+            TFLA_MUL(a1, b0, 1, 0, 0, 0, 3)
+            TFLA_FRAG_A(a0, 0, so, 0, 3)
+            TFLA_MUL(a1, b0, 1, 0, 0, 1, 3)
+            ob.template issue<1>(2, lb + rslot + HALF);
+            TFLA_MUL(a1, b0, 1, 0, 1, 0, 3)
+            TFLA_FRAG_A(a0, 0, so, 1, 3)
+            TFLA_MUL(a1, b0, 1, 0, 1, 1, 3)
+            ob.template issue<1>(3, lb + rslot + HALF);
+            TFLA_MUL(a1, b1, 1, 1, 0, 0, 0)
+            TFLA_FRAG_B(b0, 0, so, 0, 0)
+            TFLA_MUL(a1, b1, 1, 1, 0, 1, 0)
+            TFLA_FRAG_B(b0, 0, so, 1, 0)
+            TFLA_MUL(a1, b1, 1, 1, 1, 0, 0)
+            TFLA_FRAG_B(b0, 0, so, 0, 1)
+            TFLA_MUL(a1, b1, 1, 1, 1, 1, 0)
+            TFLA_FRAG_B(b0, 0, so, 1, 1)
+            TFLA_MUL(a1, b1, 1, 1, 0, 0, 1)
+            TFLA_FRAG_B(b0, 0, so, 0, 2)
+            TFLA_MUL(a1, b1, 1, 1, 0, 1, 1)
+            TFLA_FRAG_B(b0, 0, so, 1, 2)
+            TFLA_MUL(a1, b1, 1, 1, 1, 0, 1)
+            TFLA_FRAG_B(b0, 0, so, 0, 3)
+            TFLA_MUL(a1, b1, 1, 1, 1, 1, 1)
+            TFLA_FRAG_B(b0, 0, so, 1, 3)
+            TFLA_MUL(a1, b1, 1, 1, 0, 0, 2)
+            TFLA_MUL(a1, b1, 1, 1, 0, 1, 2)
+            TFLA_MUL(a1, b1, 1, 1, 1, 0, 2)
+            TFLA_MUL(a1, b1, 1, 1, 1, 1, 2)
             TFLA_NEXT();
-            TFLA_MUL(a1, b1, 1, 1, 3)
+            TFLA_MUL(a1, b1, 1, 1, 0, 0, 3)
+            TFLA_MUL(a1, b1, 1, 1, 0, 1, 3)
+            TFLA_MUL(a1, b1, 1, 1, 1, 0, 3)
+            TFLA_MUL(a1, b1, 1, 1, 1, 1, 3)
         }
     }
 #undef TFLA_NEXT
@@ -226,8 +296,8 @@ __global__ void __launch_bounds__(512, 2) gemm_bf16_wide_kernel(GemmArgs a, int 
 #undef TFLA_PHASE
     wait_vmcnt<0>();
     __syncthreads();
-    wave_epilogue<bf16_t, EPI, PAIR, 4, 2>(a, w, row0 + wm * 128, col0 + wn * (PAIR ? 32 : 64), acc,
-                                           reinterpret_cast<float*>(lds) + wave * EpiStage<64>::FLOATS, lane);
+    wave_epilogue<bf16_t, EPI, PAIR, 4, 4>(a, w, row0 + wm * 128, col0 + wn * (PAIR ? 64 : 128), acc,
+                                           reinterpret_cast<float*>(lds) + wave * EpiStage<128>::FLOATS, lane);
 }
 
 }  // namespace tfla
