@@ -37,12 +37,15 @@ template <typename DT, bool PAIR> __global__ void __launch_bounds__(256) act_bwd
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if constexpr (PAIR) {
-                    const float da = g[e] * u[e] * act_slope(z[e], a.act);
-                    u[e] = g[e] * act_value(z[e], a.act);
+                    float slope;
+                    const float value = act_both<DT>(z[e], a.act, slope), da = g[e] * u[e] * slope;
+                    u[e] = g[e] * value;
                     g[e] = da;
                     s1[e] += u[e];
                 } else if (a.act != ACT_NONE) {
-                    g[e] *= act_slope(z[e], a.act);
+                    float slope;
+                    act_both<DT>(z[e], a.act, slope);
+                    g[e] *= slope;
                 }
                 s0[e] += g[e];
             }

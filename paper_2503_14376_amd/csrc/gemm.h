@@ -26,58 +26,73 @@ template <int GROUP = 8> __device__ __forceinline__ GemmWork gemm_work(unsigned 
     return w;
 }
 
-// An accumulator block (32 rows x 32 columns per 16 registers) goes through LDS so that the epilogue has eight consecutive
-// columns in a lane.  One wavefront's area: 32 rows of C + 4 floats.
-template <int C> struct EpiStage {
-    static constexpr int LD = C + 4, FLOATS = 32 * LD;
-    static __device__ __forceinline__ void put(float* area, const f32x16& acc, int col0, int lane) {
-        const int c = lane & 31, g = lane >> 5;
+// Results.  The kernels compute the transposed blocks (weights as the first operand), so that lane (c = lane & 31, g = lane >> 5)
+// holds of row c of a block the columns 8 q + 4 g + {0 .. 3} in registers 4 q ... 4 q + 3.  Two exchanges between the halves of
+// a wavefront give lane (c, g) the eight consecutive columns 8 (q + g) ... of row c, for even q: no LDS, 16-byte stores.
+__device__ __forceinline__ void eight_columns(const f32x16& acc, int q, float (&v)[8]) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) area[acc_row(v, g) * LD + col0 + c] = acc[v];
+    for (int e = 0; e < 4; ++e) {
+        const float x = acc[4 * q + e], y = acc[4 * q + 4 + e];     // (a bit cast of a vector's element takes the first one)
+        const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, y), false, false);
+        const unsigned lo = p[0], hi = p[1];
+        v[e] = __builtin_bit_cast(float, lo);
+        v[4 + e] = __builtin_bit_cast(float, hi);
     }
-    static __device__ __forceinline__ void get(const float* area, int row, int col, float (&x)[8]) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(area + row * LD + col), b = *reinterpret_cast<const f32x4*>(area + row * LD + col + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-    }
-};
+}
 
-// One wavefront's MB x NB blocks of 32 x 32 through the epilogue.  row0, col0: first row and (without PAIR) first column;
-// PAIR: blocks 0, 2, ... hold the first matrix's columns col0, col0 + 32, ..., blocks 1, 3, ... the second's.
-template <typename DT, int EPI, bool PAIR, int MB, int NB>
-__device__ __forceinline__ void wave_epilogue(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[MB][NB], float* area,
-                                              int lane) {
-    constexpr int C = NB * 32;
-    typedef EpiStage<C> S;
-    constexpr int OC = PAIR ? C / 2 : C, LPR = OC / 8, RPP = 64 / LPR;      // output columns, lanes per row, rows per pass
-    const int planes = PAIR ? 2 : a.batch;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) S::put(area, acc[mb][nb], nb * 32, lane);
-        // (the area is this wavefront's own: only its own writes have to have arrived)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+// One wavefront's MB x NB blocks of 32 x 32 through the epilogue, 32 rows at a time.  row0, col0: first row and column of the
+// results; PAIR: blocks 0, 2, ... hold the first matrix's columns col0, col0 + 32, ..., blocks 1, 3, ... the second's.
+// The rows go round a loop that picks its registers by a switch: unrolled, the activations alone are 400 KB of code, and a
+// wavefront that runs through it once waits for every line.
+template <typename DT, int EPI, bool PAIR, int MB, int NB, bool FULL>
+__device__ __forceinline__ void wave_epilogue_as(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[MB][NB], int lane) {
+    constexpr int NG = PAIR ? NB : 2 * NB;
+    const int planes = PAIR ? 2 : a.batch, c = lane & 31, g = lane >> 5;
+    int rows = MB;
+    asm("" : "+s"(rows));
 #pragma unroll 1
-        for (int p = 0; p < 32 / RPP; ++p) {        // (a loop: unrolled, the activations alone are thousands of instructions)
-            const int r = p * RPP + lane / LPR, c = (lane % LPR) * 8;
-            float v[8], u[8];
-            if constexpr (PAIR) {
-                const int lc = (c / 32) * 64 + (c % 32);
-                S::get(area, r, lc, v);
-                S::get(area, r, lc + 32, u);
-            } else {
-                S::get(area, r, c, v);
-            }
-            const long m = row0 + mb * 32 + r;
-            if constexpr (EPI == EPI_PART) {
-                partial8(a, planes, w.part, PAIR ? 0 : w.b, m, col0 + c, v);
-                if constexpr (PAIR) partial8(a, planes, w.part, 1, m, col0 + c, u);
-            } else {
-                epilogue8<DT, EPI>(a, w.b, m, col0 + c, v, u);
-            }
+    for (int mb = 0; mb < rows; ++mb) {
+        f32x16 cur[NB];
+#define TFLA_PICK(I)                                            \
+    case I:                                                     \
+        if constexpr (I < MB) {                                 \
+            _Pragma("unroll") for (int j = 0; j < NB; ++j) cur[j] = acc[I][j]; \
+        }                                                       \
+        break;
+        switch (mb) {
+            TFLA_PICK(0) TFLA_PICK(1) TFLA_PICK(2) TFLA_PICK(3)
+            default: __builtin_unreachable();
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#undef TFLA_PICK
+        float v[NG][8], u[NG][8];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            const int nb = PAIR ? (i >> 1) * 2 : i >> 1, q = (i & 1) * 2;
+            eight_columns(cur[nb], q, v[i]);
+            if constexpr (PAIR) eight_columns(cur[nb + 1], q, u[i]);
+        }
+        const long m = row0 + mb * 32 + c;
+        const int n = col0 + 8 * g;
+        auto step = [](int i) { return (i >> 1) * 32 + (i & 1) * 16; };
+        if constexpr (EPI == EPI_PART) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                partial8<FULL>(a, planes, w.part, PAIR ? 0 : w.b, m, n + step(i), v[i]);
+                if constexpr (PAIR) partial8<FULL>(a, planes, w.part, 1, m, n + step(i), u[i]);
+            }
+        } else {
+            epilogue_groups<DT, EPI, NG, FULL>(a, w.b, m, n, step, v, u);
+        }
     }
+}
+// (whole tiles without the checks of every row and column, so that loads and stores are not held up by branches)
+// Returns whether that was so: at least 16 vector memory operations have been issued then.
+template <typename DT, int EPI, bool PAIR, int MB, int NB>
+__device__ __forceinline__ bool wave_epilogue(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[MB][NB], int lane) {
+    const bool full = row0 + MB * 32 <= a.M && col0 + NB * (PAIR ? 16 : 32) <= a.N;
+    if (full) wave_epilogue_as<DT, EPI, PAIR, MB, NB, true>(a, w, row0, col0, acc, lane);
+    else wave_epilogue_as<DT, EPI, PAIR, MB, NB, false>(a, w, row0, col0, acc, lane);
+    return full;
 }
 
 // Bytes of a tile (rows_left x cols_left of the tensor from its first element on, at most ROWS rows) that may be read.
@@ -136,8 +151,7 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int 
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128, STAGE = ABYTES + BBYTES;
-    constexpr int EPIB = WM * WN * EpiStage<TN>::FLOATS * 4, LDS = 2 * STAGE > EPIB ? 2 * STAGE : EPIB;
-    __shared__ __align__(1024) char lds[LDS];
+    __shared__ __align__(1024) char lds[2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
@@ -202,13 +216,10 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int 
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i], bf[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
         }
     }
-    wait_vmcnt<0>();
-    __syncthreads();
-    wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc,
-                                             reinterpret_cast<float*>(lds) + wave * EpiStage<TN>::FLOATS, lane);
+    wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
 
 // fp32 products: tiles through registers into LDS, contraction steps of 32, the contraction index contiguous per LDS row
@@ -235,8 +246,8 @@ template <int BM, int BN, int WM, int WN, bool ATR, bool BTR, bool PAIR, int EPI
 __global__ void __launch_bounds__(WM* WN * 64) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN, LD = 36;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
-    constexpr int STAGE = (BM + BN) * LD, EPIF = WM * WN * EpiStage<TN>::FLOATS;
-    __shared__ __align__(16) float lds[2 * STAGE > EPIF ? 2 * STAGE : EPIF];
+    constexpr int STAGE = (BM + BN) * LD;
+    __shared__ __align__(16) float lds[2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, g = lane >> 5;
     const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
@@ -291,13 +302,12 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_f32_kernel(GemmArgs a, int t
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = Elem<float>::mma(af[i], bf[j], acc[i][j]);
+                for (int j = 0; j < NB; ++j) acc[i][j] = Elem<float>::mma(bf[j], af[i], acc[i][j]);
         }
         if (more) store(stage ^ 1);
         __syncthreads();
     }
-    wave_epilogue<float, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lds + wave * EpiStage<TN>::FLOATS,
-                                            lane);
+    wave_epilogue<float, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
 
 }  // namespace tfla

@@ -9,77 +9,136 @@ namespace tfla {
 enum { ACT_NONE = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
 
 // act(z) and act'(z).  silu: z sigma(z), sigma (1 + z (1 - sigma)); gelu: z Phi(z), Phi + z phi; relu: (z > 0).
-__device__ __forceinline__ float sigmoid_f32(float z) {
+// For bf16 tensors sigma and Phi come from the hardware's exponential and reciprocal (errors of some 2^-22, where the result is
+// rounded to 2^-9), for fp32 from the library's functions.  Phi(-|z|) = 1/2 erfc(|z| / sqrt 2) by the approximation 7.1.26 of
+// Abramowitz and Stegun, Handbook of Mathematical Functions (1.5e-7 absolute), a polynomial in 1 / (1 + p x) times exp(-x^2).
+template <typename DT> __device__ __forceinline__ float sigmoid(float z);
+template <> __device__ __forceinline__ float sigmoid<float>(float z) {
     const float e = expf(-fabsf(z));
     return (z >= 0.0f ? 1.0f : e) / (1.0f + e);
 }
-__device__ __forceinline__ float act_value(float z, int act) {
-    if (act == ACT_SILU) return z * sigmoid_f32(z);
-    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+template <> __device__ __forceinline__ float sigmoid<bf16_t>(float z) {
+    return __builtin_amdgcn_rcpf(1.0f + fast_exp2(-1.44269504f * z));
+}
+// Phi(z), and exp(-z^2 / 2)
+template <typename DT> __device__ __forceinline__ float normal_cdf(float z, float& e);
+template <> __device__ __forceinline__ float normal_cdf<float>(float z, float& e) {
+    e = expf(-0.5f * z * z);
+    return 0.5f * (1.0f + erff(z * 0.70710678f));
+}
+template <> __device__ __forceinline__ float normal_cdf<bf16_t>(float z, float& e) {
+    e = fast_exp2(-0.72134752f * z * z);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+    float p = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+    p = __builtin_fmaf(t, p, 1.421413741f);
+    p = __builtin_fmaf(t, p, -0.284496736f);
+    p = __builtin_fmaf(t, p, 0.254829592f);
+    const float h = 0.5f * t * p * e;
+    return z < 0.0f ? h : 1.0f - h;
+}
+template <typename DT> __device__ __forceinline__ float act_value(float z, int act) {
+    if (act == ACT_SILU) return z * sigmoid<DT>(z);
+    if (act == ACT_GELU) {
+        float e;
+        return z * normal_cdf<DT>(z, e);
+    }
     if (act == ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
     return z;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
+// value and slope
+template <typename DT> __device__ __forceinline__ float act_both(float z, int act, float& slope) {
     if (act == ACT_SILU) {
-        const float g = sigmoid_f32(z);
-        return g * (1.0f + z * (1.0f - g));
+        const float g = sigmoid<DT>(z);
+        slope = g * (1.0f + z * (1.0f - g));
+        return z * g;
     }
-    if (act == ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
-    if (act == ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    return 1.0f;
+    if (act == ACT_GELU) {
+        float e;
+        const float c = normal_cdf<DT>(z, e);
+        slope = __builtin_fmaf(z * 0.39894228f, e, c);
+        return z * c;
+    }
+    if (act == ACT_RELU) {
+        slope = z > 0.0f ? 1.0f : 0.0f;
+        return z > 0.0f ? z : (z != z ? z : 0.0f);
+    }
+    slope = 1.0f;
+    return z;
 }
 
-// Eight columns n, n + 1, ... of row m: the epilogue and the stores.  v: the product (of the first matrix), w: of the second
-// (EPI_GATED).  b: which result of a batch.
-template <typename DT, int EPI>
-__device__ __forceinline__ void epilogue8(const GemmArgs& a, int b, long m, int n, float (&v)[8], float (&w)[8]) {
-    if (m >= a.M || n >= a.N) return;
-    const int left = a.N - n;
+// NG groups of eight columns n + step(i) ... of row m: the epilogue and the stores, part by part over all groups, so that the
+// loads of a part are under way together.  v: the product (of the first matrix), w: of the second (EPI_GATED).  b: which
+// result of a batch.  FULL: all of the row and the columns exist.
+template <typename DT, int EPI, int NG, bool FULL, typename STEP>
+__device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m, int n, STEP step, float (&v)[NG][8], float (&w)[NG][8]) {
+    if (!FULL && m >= a.M) return;
     const long at = m * a.N + n;
-    if constexpr (EPI == EPI_STORE) {
-        store8<DT>(a.out[b], at, left, v);
-    } else if constexpr (EPI == EPI_LINEAR) {
-        if (a.bias[0]) {
-            float t[8];
-            load8<float>(a.bias[0], n, left).get(t);
+    auto left = [&](int i) { return FULL ? 8 : a.N - n - step(i); };
+    auto add = [&](const float* bias, float (&x)[NG][8]) {
+        Vec8<float> t[NG];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += t[e];
+        for (int i = 0; i < NG; ++i) t[i] = load8<float>(bias, n + step(i), left(i));
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] += t[i].v[e];
+    };
+    auto put = [&](void* p, const float (&x)[NG][8]) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) store8<DT>(p, at + step(i), left(i), x[i]);
+    };
+    auto activate = [&](auto kind) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = act_value<DT>(v[i][e], kind());
+    };
+    struct Silu { __device__ constexpr int operator()() const { return ACT_SILU; } };
+    struct Gelu { __device__ constexpr int operator()() const { return ACT_GELU; } };
+    struct Relu { __device__ constexpr int operator()() const { return ACT_RELU; } };
+    if constexpr (EPI != EPI_STORE) {
+        Vec8<DT> r[NG];
+        if (EPI == EPI_LINEAR && a.residual) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) r[i] = load8<DT>(a.residual, at + step(i), left(i));
         }
-        if (a.z[0]) store8<DT>(a.z[0], at, left, v);
-        if (a.act != ACT_NONE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = act_value(v[e], a.act);
+        if (a.bias[0]) add(a.bias[0], v);
+        if (a.z[0]) put(a.z[0], v);
+        if constexpr (EPI == EPI_GATED) {
+            if (a.bias[1]) add(a.bias[1], w);
+            if (a.z[1]) put(a.z[1], w);
         }
-        if (a.residual) {
-            float t[8];
-            load8<DT>(a.residual, at, left).get(t);
+        if (a.act == ACT_SILU) activate(Silu());
+        else if (a.act == ACT_GELU) activate(Gelu());
+        else if (a.act == ACT_RELU) activate(Relu());
+        if constexpr (EPI == EPI_GATED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += t[e];
+            for (int i = 0; i < NG; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] *= w[i][e];
+        } else if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                float t[8];
+                r[i].get(t);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] += t[e];
+            }
         }
-        store8<DT>(a.out[0], at, left, v);
-    } else if constexpr (EPI == EPI_GATED) {
-        if (a.bias[0]) {
-            float t[8];
-            load8<float>(a.bias[0], n, left).get(t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += t[e];
-        }
-        if (a.bias[1]) {
-            float t[8];
-            load8<float>(a.bias[1], n, left).get(t);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] += t[e];
-        }
-        if (a.z[0]) store8<DT>(a.z[0], at, left, v);
-        if (a.z[1]) store8<DT>(a.z[1], at, left, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_value(v[e], a.act) * w[e];
-        store8<DT>(a.out[0], at, left, v);
     }
+    put(a.out[EPI == EPI_STORE ? b : 0], v);
+}
+// one group
+template <typename DT, int EPI> __device__ __forceinline__ void epilogue8(const GemmArgs& a, int b, long m, int n, float (&v)[8], float (&w)[8]) {
+    float v1[1][8], w1[1][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { v1[0][e] = v[e]; w1[0][e] = w[e]; }
+    if (n < a.N) epilogue_groups<DT, EPI, 1, false>(a, b, m, n, [](int) { return 0; }, v1, w1);
 }
 // the partial results of one part of the contraction: plane (part, result) of M rows of ld_part values
+template <bool FULL = false>
 __device__ __forceinline__ void partial8(const GemmArgs& a, int planes, int part, int plane, long m, int n, const float (&v)[8]) {
-    if (m >= a.M || n >= a.N) return;
+    if (!FULL && (m >= a.M || n >= a.N)) return;
     float* p = a.part + (((long)part * planes + plane) * a.M + m) * a.ld_part + n;
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};

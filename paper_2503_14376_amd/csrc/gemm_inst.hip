@@ -18,7 +18,8 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
 #if TFLA_GEMM >= 4
     hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 2, 1, ATR, BTR, PAIR, EPI>), grid, dim3(128), 0, s, a, tms, tns);
 #else
-    if (p.bm == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<ATR, BTR, PAIR, EPI>), grid, dim3(256), 0, s, a, tms, tns);
+    // (one workgroup fits a CU; the 256 of them take the tiles in turn)
+    if (p.bm == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<ATR, BTR, PAIR, EPI>), dim3(grid.x < 256 ? grid.x : 256), dim3(256), 0, s, a, tms, tns);
     else hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, ATR, BTR, PAIR, EPI>), grid, dim3(256), 0, s, a, tms, tns);
 #endif
 }

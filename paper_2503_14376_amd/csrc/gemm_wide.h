@@ -80,18 +80,24 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
     __shared__ __align__(1024) char lds[2 * OPERAND];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
-    const long row0 = (long)w.tm * 256;
-    const int col0 = w.tn * (PAIR ? 128 : 256);
-    const int ksteps = (a.K + 63) / 64, all = ksteps * a.segs;
-    const int per = (all + a.split - 1) / a.split, k_begin = w.part * per, k_end = min(all, k_begin + per);
-
+    const int ksteps = (a.K + 63) / 64, all = ksteps * a.segs, per = (all + a.split - 1) / a.split;
+    const unsigned total = (unsigned)tms * tns * a.split * a.batch;
+    GemmWork w;
+    long row0;
+    int col0, k_begin, k_end;
+    auto take = [&](unsigned id) {
+        w = gemm_work(xcd_range(id, total), tms, tns, a.split);
+        row0 = (long)w.tm * 256;
+        col0 = w.tn * (PAIR ? 128 : 256);
+        k_begin = w.part * per;
+        k_end = min(all, k_begin + per);
+    };
     WideOperand<ATR, 64, false> oa;
     WideOperand<BTR, PAIR ? 128 : 64, PAIR> ob;
     oa.init(a.lda, tid);
     ob.init(a.ldb, tid);
     // the next step to request, and the next at which its descriptors change by more than a step
-    int rt = k_begin, change = k_begin;
+    int rt, change;
     auto find = [&]() {
         const bool on = rt < k_end, second = rt >= ksteps;
         const int k0 = on ? (second ? rt - ksteps : rt) * 64 : 0;
@@ -101,7 +107,7 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
         change = !on ? 0x7fffffff : min(k_end, rt < whole ? whole : seg_end);
     };
     const uint32_t la = lds_addr(lds) + wave * 1024, lb = la + OPERAND;
-    uint32_t rslot = 0;         // slot of the step to request
+    uint32_t rslot;             // slot of the step to request
 #define TFLA_NEXT()                                        \
     do {                                                   \
         ++rt;                                              \
@@ -136,30 +142,39 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
 #define TFLA_MUL(A, B, HA, HB, i, j, ks)                                                                      \
     __builtin_amdgcn_sched_barrier(0);                                                                        \
     acc[(HA) * 2 + i][PAIR ? (j) * 2 + HB : (HB) * 2 + j] =                                                   \
-        __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i][ks], B[j][ks], acc[(HA) * 2 + i][PAIR ? (j) * 2 + HB : (HB) * 2 + j], 0, 0, 0);
-#define TFLA_PHASE()                                       \
-    do {                                                   \
-        asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory"); \
-        barrier_nofence();                                 \
+        __builtin_amdgcn_mfma_f32_32x32x16_bf16(B[j][ks], A[i][ks], acc[(HA) * 2 + i][PAIR ? (j) * 2 + HB : (HB) * 2 + j], 0, 0, 0);
+#define TFLA_PHASE()                                                     \
+    do {                                                                 \
+        if (landed > 0) --landed;                                        \
+        else wait_vmcnt<16>();                                           \
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); \
     } while (0)
 
-    f32x16 acc[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-    bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
-    if (k_begin < k_end) {
+    // the first two steps of a tile
+    auto start = [&]() {
+        rt = k_begin;
+        rslot = 0;
         find();
-        TFLA_REQUEST(0);
-        TFLA_REQUEST(1);
+        TFLA_REQUEST(0)
+        TFLA_REQUEST(1)
         TFLA_NEXT();
-        TFLA_REQUEST(0);
-        TFLA_REQUEST(1);
+        TFLA_REQUEST(0)
+        TFLA_REQUEST(1)
         TFLA_NEXT();
-        wait_vmcnt<24>();
+    };
+    f32x16 acc[4][4];
+    bf16x8 a0[2][4], a1[2][4], b0[2][4], b1[2][4];
+    take(blockIdx.x);
+    start();
+    wait_vmcnt<0>();
+    // One workgroup per CU takes tile after tile; the next one's first steps are requested before the epilogue of the last.
+    for (unsigned id = blockIdx.x;;) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
         barrier_nofence();
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
@@ -169,6 +184,7 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
                 TFLA_FRAG_B(b0, 0, 0, i, ks)
             }
         uint32_t so = 0;
+        int landed = 3;         // phases that need nothing but the first two steps, which have arrived
         for (int t = k_begin; t < k_end; ++t) {
             TFLA_PHASE();
             TFLA_MUL(a0, b0, 0, 0, 0, 0, 0)
@@ -287,6 +303,22 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
             TFLA_MUL(a1, b1, 1, 1, 1, 0, 3)
             TFLA_MUL(a1, b1, 1, 1, 1, 1, 3)
         }
+        // what was requested of steps behind the end has to have arrived before the memory is used anew
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const GemmWork done = w;
+        const long drow = row0 + wm * 128;
+        const int dcol = col0 + wn * (PAIR ? 64 : 128);
+        id += gridDim.x;
+        const bool more = id < total;
+        if (more) {
+            take(id);
+            start();
+        }
+        const bool full = wave_epilogue<bf16_t, EPI, PAIR, 4, 4>(a, done, drow, dcol, acc, lane);
+        if (!more) break;
+        // the requests are older than the epilogue's operations, so its last stores need not have arrived
+        if (full) wait_vmcnt<16>();
+        else wait_vmcnt<0>();
     }
 #undef TFLA_NEXT
 #undef TFLA_REQUEST
@@ -294,10 +326,6 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
 #undef TFLA_FRAG_B
 #undef TFLA_MUL
 #undef TFLA_PHASE
-    wait_vmcnt<0>();
-    __syncthreads();
-    wave_epilogue<bf16_t, EPI, PAIR, 4, 4>(a, w, row0 + wm * 128, col0 + wn * (PAIR ? 64 : 128), acc,
-                                           reinterpret_cast<float*>(lds) + wave * EpiStage<128>::FLOATS, lane);
 }
 
 }  // namespace tfla
