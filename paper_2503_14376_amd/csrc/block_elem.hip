@@ -127,13 +127,42 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// How a product is cut: the tile and the number of parts with the shortest time by a model of the kernels, measured on products
+// of 40 to 8192 rows and columns (forward, both backward layouts; within some 10 % of the best of all choices).  In us, with w
+// workgroups in all, n = ceil(w / 256) of them per CU one after another or side by side, and t steps each:
+//   bf16   256 x 256   8 + n (t (1.0 + 0.45 min(1, w / 256)) + 4)        (the power that all CUs draw lowers the clock)
+//          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
+//          128 x 128   6 + t max(0.63, 0.51 n) + 1.5 max(0, n - 2)
+//          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.27 t n)
+//   joining the parts  4.2 + (bytes written and read again) / 7 MB per us
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype) {
-    GemmPlan p;
-    p.bm = p.bn = dtype == 1 ? 128 : 64;
-    const int bno = pair ? 128 : 256;
-    if (dtype == 1 && (M + 255) / 256 * ((N + bno - 1) / bno) * batch >= 256) p.bm = p.bn = 256;
-    p.split = 1;
-    return p;
+    struct Tile { int bm, bn; };
+    static constexpr Tile bf16_tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}}, f32_tiles[] = {{64, 64}};
+    const bool b16 = dtype == 1;
+    const Tile* tiles = b16 ? bf16_tiles : f32_tiles;
+    const int kinds = b16 ? 4 : 1, step = b16 ? 64 : 32;
+    const int all = (K + step - 1) / step * segs;
+    GemmPlan best{0, 0, 1};
+    double least = 0;
+    for (int i = 0; i < kinds; ++i) {
+        int bm = tiles[i].bm, bn = tiles[i].bn;
+        if (b16 && bm == 64 && pair) bn = 128;
+        const int bno = pair ? bn / 2 : bn;
+        const double cells = (double)((M + bm - 1) / bm) * ((N + bno - 1) / bno) * batch;
+        for (int split = 1; split <= 32 && (split == 1 || (all >= 4 * split && cells * split <= 1024)); split += split < 4 ? 1 : split / 2) {
+            const double w = cells * split, t = (all + split - 1) / split, part = w < 256 ? w / 256 : 1, n = (double)(long)((w + 255) / 256);
+            const double more = n > 2 ? n - 2 : 0;
+            double us;
+            if (!b16) us = 5 + t * (n < 2 ? 1.6 : 0.8 * n);
+            else if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
+            else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
+            else if (bm == 128) us = 6 + t * (0.51 * n > 0.63 ? 0.51 * n : 0.63) + 1.5 * more;
+            else us = 4.8 + (pair ? 0.27 : 0.177) * t * n + 0.9 * more;
+            if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
+            if (best.bm == 0 || us < least) { least = us; best = {bm, bn, split}; }
+        }
+    }
+    return best;
 }
 
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s) {

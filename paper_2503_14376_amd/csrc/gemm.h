@@ -26,18 +26,33 @@ template <int GROUP = 8> __device__ __forceinline__ GemmWork gemm_work(unsigned 
     return w;
 }
 
-// Results.  The kernels compute the transposed blocks (weights as the first operand), so that lane (c = lane & 31, g = lane >> 5)
-// holds of row c of a block the columns 8 q + 4 g + {0 .. 3} in registers 4 q ... 4 q + 3.  Two exchanges between the halves of
-// a wavefront give lane (c, g) the eight consecutive columns 8 (q + g) ... of row c, for even q: no LDS, 16-byte stores.
-__device__ __forceinline__ void eight_columns(const f32x16& acc, int q, float (&v)[8]) {
+// Results.  Partial results are stored as they leave the matrix unit: lane (c = lane & 31, g = lane >> 5) holds of column c of a
+// block the rows acc_row(v, g), so that a store writes whole rows of 32 floats.  For everything else the kernels compute the
+// transposed blocks (the second operand first), so that the lane holds of row c the columns 8 q + 4 g + {0 .. 3} in registers
+// 4 q ... 4 q + 3.  Exchanges between the halves, then between the quarters of a wavefront give it eight consecutive columns:
+// x: row c % 16, y: row c % 16 + 16, columns 16 (c / 16) + 8 g ...; a store writes 64 consecutive bytes of 16 rows in bf16.
+// (Without the second exchange 32 bytes of 32 rows, without any, 16-byte pieces; through LDS the turn took longer than the stores.)
+template <bool WIDE> __device__ __forceinline__ void lane_swap(float& x, float& y) {
+    const unsigned a = __builtin_bit_cast(unsigned, x), b = __builtin_bit_cast(unsigned, y);
+    const auto p = WIDE ? __builtin_amdgcn_permlane32_swap(a, b, false, false) : __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    const unsigned lo = p[0], hi = p[1];
+    x = __builtin_bit_cast(float, lo);
+    y = __builtin_bit_cast(float, hi);
+}
+__device__ __forceinline__ void eight_columns(const f32x16& acc, float (&x)[8], float (&y)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float x = acc[4 * q + e], y = acc[4 * q + 4 + e];     // (a bit cast of a vector's element takes the first one)
-        const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, y), false, false);
-        const unsigned lo = p[0], hi = p[1];
-        v[e] = __builtin_bit_cast(float, lo);
-        v[4 + e] = __builtin_bit_cast(float, hi);
+        x[e] = acc[e]; x[4 + e] = acc[4 + e];
+        y[e] = acc[8 + e]; y[4 + e] = acc[12 + e];
+        lane_swap<true>(x[e], x[4 + e]);
+        lane_swap<true>(y[e], y[4 + e]);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lane_swap<false>(x[e], y[e]);
+}
+// the product of two fragments in the orientation that the epilogue wants
+template <int EPI> __device__ __forceinline__ f32x16 mma_bf16(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+    return EPI == EPI_PART ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0) : __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
 }
 
 // One wavefront's MB x NB blocks of 32 x 32 through the epilogue, 32 rows at a time.  row0, col0: first row and column of the
@@ -47,7 +62,7 @@ __device__ __forceinline__ void eight_columns(const f32x16& acc, int q, float (&
 template <typename DT, int EPI, bool PAIR, int MB, int NB, bool FULL>
 __device__ __forceinline__ void wave_epilogue_as(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[MB][NB], int lane) {
     constexpr int NG = PAIR ? NB : 2 * NB;
-    const int planes = PAIR ? 2 : a.batch, c = lane & 31, g = lane >> 5;
+    const int c = lane & 31, g = lane >> 5;
     int rows = MB;
     asm("" : "+s"(rows));
 #pragma unroll 1
@@ -64,29 +79,34 @@ __device__ __forceinline__ void wave_epilogue_as(const GemmArgs& a, const GemmWo
             default: __builtin_unreachable();
         }
 #undef TFLA_PICK
-        float v[NG][8], u[NG][8];
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-            const int nb = PAIR ? (i >> 1) * 2 : i >> 1, q = (i & 1) * 2;
-            eight_columns(cur[nb], q, v[i]);
-            if constexpr (PAIR) eight_columns(cur[nb + 1], q, u[i]);
-        }
-        const long m = row0 + mb * 32 + c;
-        const int n = col0 + 8 * g;
-        auto step = [](int i) { return (i >> 1) * 32 + (i & 1) * 16; };
+        const long m0 = row0 + mb * 32;
         if constexpr (EPI == EPI_PART) {
+            const int planes = PAIR ? 2 : a.batch;
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                partial8<FULL>(a, planes, w.part, PAIR ? 0 : w.b, m, n + step(i), v[i]);
-                if constexpr (PAIR) partial8<FULL>(a, planes, w.part, 1, m, n + step(i), u[i]);
+            for (int j = 0; j < NB; ++j) {
+                const int n = col0 + (PAIR ? j / 2 : j) * 32 + c;
+                float* p = partial_plane(a, planes, w.part, PAIR ? j & 1 : w.b) + m0 * a.ld_part + n;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int r = acc_row(v, g);
+                    if (FULL || (m0 + r < a.M && n < a.N)) p[r * a.ld_part] = cur[j][v];
+                }
             }
         } else {
-            epilogue_groups<DT, EPI, NG, FULL>(a, w.b, m, n, step, v, u);
+            float v[NG][8], u[NG][8];
+#pragma unroll
+            for (int j = 0; j < NB; j += PAIR ? 2 : 1) {
+                constexpr int F = PAIR ? 1 : 2;
+                eight_columns(cur[j], v[j * F], v[j * F + 1]);
+                if constexpr (PAIR) eight_columns(cur[j + 1], u[j], u[j + 1]);
+            }
+            epilogue_groups<DT, EPI, NG, FULL>(a, w.b, m0 + (c & 15), col0 + (c >> 4) * 16 + 8 * g, [](int i) { return (i & 1) * 16; },
+                                               [](int i) { return (i >> 1) * 32; }, v, u);
         }
     }
 }
 // (whole tiles without the checks of every row and column, so that loads and stores are not held up by branches)
-// Returns whether that was so: at least 16 vector memory operations have been issued then.
+// Returns whether that was so: every lane has stored MB * NB (PAIR: half that) times 32 bytes or more then.
 template <typename DT, int EPI, bool PAIR, int MB, int NB>
 __device__ __forceinline__ bool wave_epilogue(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[MB][NB], int lane) {
     const bool full = row0 + MB * 32 <= a.M && col0 + NB * (PAIR ? 16 : 32) <= a.N;
@@ -95,36 +115,94 @@ __device__ __forceinline__ bool wave_epilogue(const GemmArgs& a, const GemmWork&
     return full;
 }
 
-// Bytes of a tile (rows_left x cols_left of the tensor from its first element on, at most ROWS rows) that may be read.
-template <int ROWS> __device__ __forceinline__ uint32_t tile_bytes(long rows_left, int cols_left, long ld) {
-    const int r = rows_left < ROWS ? (int)rows_left : ROWS;
-    return (r > 0 && cols_left > 0) ? (uint32_t)((r - 1) * ld * 2) + 2u * (uint32_t)cols_left : 0u;
-}
-
-// One operand of a bf16 product: tiles of ROWS output rows (or columns) x 64 contraction steps.  Plain: [ROWS][64] in LDS;
-// transposed: [64][ROWS], read by the transposing LDS reads.
-template <int ROWS, bool TR, int NT> struct OperandTile {
-    typedef DmaTile<TR ? 64 : ROWS, TR ? ROWS : 64, NT, TR ? SWZ_T : SWZ_K> Dma;
-    Dma dma;
-    const bf16_t* base; long ld; long rows_left; int K8; int cols_left;
-    // base: element (row0, 0) or, transposed, (0, row0); extent: rows of the operand; K: contraction length
-    __device__ __forceinline__ void init(const void* p, long ld_, long row0, long extent, int K, int tid) {
-        ld = ld_;
-        base = reinterpret_cast<const bf16_t*>(p) + (TR ? row0 : row0 * ld);
-        // whole groups of eight: what lies behind the extent belongs to the row's padding
-        rows_left = extent - row0; K8 = TR ? K : (K + 7) & ~7;
-        cols_left = TR ? (int)((rows_left + 7) & ~7l) : 0;
-        dma.init(ld, tid);
-        if (TR) dma.bound_columns(cols_left, tid);
-    }
-    __device__ __forceinline__ void issue(int k0, uint32_t lds, int tid) const {
-        if constexpr (TR) {
-            const uint32_t bytes = tile_bytes<64>(K8 - k0, cols_left, ld);
-            dma.template issue_bounded<false>(base + (long)k0 * ld, bytes, ROWS, lds, tid);
-        } else {
-            const uint32_t bytes = tile_bytes<ROWS>(rows_left, K8 - k0, ld);
-            dma.template issue_bounded<false>(base + k0, bytes, K8 - k0, lds, tid);
+// The stream of one operand's tiles into LDS: HALVES parts of ROWS output rows (or columns) x 64 contraction steps each, filled by
+// requests of NT threads.  Plain: [ROWS][64] in LDS; transposed: [64][ROWS], read by the transposing LDS reads.  Local row r of
+// a part stands for row (r / G) 2 G + r % G behind the part's first row (G = ROWS: itself); part h starts at row h G, or with
+// PAIR at the first row of matrix h.  The buffer descriptors are kept ready and moved on by a step at a time; everything else
+// about them is found anew (set) only at the steps where it changes: the last step of a contraction that is no multiple of 64,
+// the second segment, the end, behind which nothing is requested (bounds of zero bytes) and LDS receives zeros.
+template <int ROWS, bool TR, int G, int NT, int HALVES, bool PAIR> struct OperandStream {
+    typedef DmaTile<TR ? 64 : ROWS, TR ? ROWS : 64, NT, TR ? SWZ_T : SWZ_K> Shape;
+    static constexpr int CPR = Shape::CPR, N = Shape::N, NW = NT / 64, BYTES = ROWS * 128;
+    static constexpr long SPAN = G == ROWS ? ROWS : 2 * ROWS;
+    static constexpr uint32_t BEHIND = 0x40000000u;       // an offset beyond every bound
+    u32x4 d[HALVES];            // descriptors of the parts at the next step
+    uint32_t goff[N], hop;      // byte offsets of this lane; bytes from step to step
+    __device__ __forceinline__ void init(long ld, int tid) {
+        const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int q = (wave + j * NW) * 64 + lane, r = q / CPR, c = ((q % CPR) ^ swz_mask<TR ? SWZ_T : SWZ_K, CPR>(r)) * 8;
+            const int row = TR || G == ROWS ? r : (r / G) * 2 * G + r % G, col = TR && G != ROWS ? (c / G) * 2 * G + c % G : c;
+            goff[j] = (uint32_t)((row * ld + col) * 2);
         }
+        hop = (uint32_t)(TR ? 128 * ld : 128);
+    }
+    // p0, p1: the matrices of the parts; first: the operand's first row in the tile, of `extent`; K: contraction length; steps from
+    // k0 on.  Columns behind the end of a transposed operand's rows are other rows' values: they meet results that are not
+    // stored.
+    __device__ __forceinline__ void set(const void* p0, const void* p1, long ld, long first, long extent, int K, int k0, bool exists, int tid) {
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+            const long at = first + (PAIR ? 0 : h * G), left = extent - at;
+            const long rows = TR ? (K - k0 < 64 ? K - k0 : 64) : (left < SPAN ? left : SPAN);
+            // whole groups of eight columns: what lies behind the extent belongs to the row's padding
+            const int K8 = (K + 7) & ~7, cols = TR ? (int)(left < SPAN ? (left + 7) & ~7l : SPAN) : (K8 - k0 < 64 ? K8 - k0 : 64);
+            const uint64_t b = reinterpret_cast<uint64_t>(h ? p1 : p0) + 2 * (TR ? k0 * ld + at : at * ld + k0);
+            d[h][0] = (uint32_t)b;
+            d[h][1] = (uint32_t)(b >> 32) & 0xffffu;
+            d[h][2] = exists && rows > 0 && cols > 0 ? (uint32_t)((rows - 1) * ld * 2) + 2u * (uint32_t)cols : 0u;
+            d[h][3] = 0x00020000u;
+        }
+        if constexpr (!TR) {
+            const int lane = tid & 63, wave = tid >> 6, left = ((K + 7) & ~7) - k0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int q = (wave + j * NW) * 64 + lane, c = ((q % CPR) ^ swz_mask<SWZ_K, CPR>(q / CPR)) * 8;
+                goff[j] = (goff[j] & (BEHIND - 1)) | (c < left ? 0u : BEHIND);
+            }
+        }
+    }
+    template <int STEPS> __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+            const uint64_t b = ((uint64_t)d[h][1] << 32 | d[h][0]) + (uint64_t)hop * STEPS;
+            d[h][0] = (uint32_t)b;
+            d[h][1] = (uint32_t)(b >> 32);
+        }
+    }
+    // request j of part H; lds: LDS address of the part plus 1024 times the wavefront
+    template <int H> __device__ __forceinline__ void issue(int j, uint32_t lds) const {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(lds + j * NW * 1024), "v"(goff[j]), "s"(d[H]) : "m0");
+    }
+    template <int H> __device__ __forceinline__ void issue_all(uint32_t lds) const {
+#pragma unroll
+        for (int j = 0; j < N; ++j) issue<H>(j, lds);
+    }
+};
+
+// Which step of a tile's contraction the operands' streams stand at.
+// STRIDE: steps from one that is requested to the next.
+template <bool PAIR, int STRIDE> struct StepStream {
+    int at, change, k_end, ksteps;      // next step, the first at which the descriptors change by more than a stride
+    template <typename OA, typename OB>
+    __device__ __forceinline__ void find(const GemmArgs& a, const GemmWork& w, long row0, int col0, OA& oa, OB& ob, int tid) {
+        const bool on = at < k_end, second = at >= ksteps;
+        const int k0 = on ? (second ? at - ksteps : at) * 64 : 0;
+        const void* pa = a.A[second ? 1 : w.b];
+        const void* pb = a.B[second && !PAIR ? 1 : 0];
+        oa.set(pa, pa, a.lda, row0, a.M, a.K, k0, on, tid);
+        ob.set(pb, PAIR ? a.B[1] : pb, a.ldb, col0, a.N, a.K, k0, on, tid);
+        const int seg_end = second ? 2 * ksteps : ksteps, whole = seg_end - (a.K % 64 != 0);
+        change = !on ? 0x7fffffff : min(k_end, at < whole ? whole : seg_end);
+    }
+    template <typename OA, typename OB>
+    __device__ __forceinline__ void next(const GemmArgs& a, const GemmWork& w, long row0, int col0, OA& oa, OB& ob, int tid) {
+        at += STRIDE;
+        oa.template advance<STRIDE>();
+        ob.template advance<STRIDE>();
+        if (at >= change) find(a, w, row0, col0, oa, ob, tid);
     }
 };
 
@@ -144,48 +222,45 @@ template <int ROWS> struct OperandFrags<ROWS, true> {
     }
 };
 
-// Tile BM x BN, WM x WN wavefronts, contraction in steps of 64 through two LDS stages filled asynchronously.
-// PAIR: the columns of a tile are BN / 2 of B[0] and the same BN / 2 of B[1], wavefront by wavefront.
-template <int BM, int BN, int WM, int WN, bool ATR, bool BTR, bool PAIR, int EPI>
-__global__ void __launch_bounds__(WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int tms, int tns) {
+// Tile BM x BN, WM x WN wavefronts, contraction in steps of 64 through S LDS stages, S - 1 of them under way.  KG such groups of
+// wavefronts take the steps in turn, each through stages of its own, and meet in LDS at the end: where a launch has no more
+// than one workgroup per CU, a wavefront per SIMD spends a step on issuing its instructions (64 x 64 tiles: 0.29 us, with two
+// wavefronts per SIMD 0.2).  PAIR: the columns of a tile are BN / 2 of B[0] and the same BN / 2 of B[1], wavefront by wavefront.
+template <int BM, int BN, int WM, int WN, int S, int KG, bool ATR, bool BTR, bool PAIR, int EPI>
+__global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int tms, int tns) {
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128, STAGE = ABYTES + BBYTES;
-    __shared__ __align__(1024) char lds[2 * STAGE];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int JOIN = (KG - 1) * WM * WN * MB * NB * 4096;
+    static_assert(JOIN <= KG * S * STAGE, "the groups' results fit the stages");
+    __shared__ __align__(1024) char lds[KG * S * STAGE];
+    const int tid = threadIdx.x % NT, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const int wm = wave / WN, wn = wave % WN;
     const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
     const long row0 = (long)w.tm * BM;
     const int col0 = w.tn * BNO;
 
-    const int ksteps = (a.K + 63) / 64, all = ksteps * a.segs;
-    const int per = (all + a.split - 1) / a.split, k_begin = w.part * per, k_end = min(all, k_begin + per);
-
-    OperandTile<BM, ATR, NT> ta;
-    OperandTile<BNO, BTR, NT> tb, tb2;
-    ta.init(a.A[w.b], a.lda, row0, a.M, a.K, tid);
-    tb.init(a.B[0], a.ldb, col0, a.N, a.K, tid);
-    if constexpr (PAIR) tb2.init(a.B[1], a.ldb, col0, a.N, a.K, tid);
-    // the second segment's operands lie this many bytes away from the first's
-    const uintptr_t hopA = reinterpret_cast<uintptr_t>(a.A[1]) - reinterpret_cast<uintptr_t>(a.A[0]);
-    const uintptr_t hopB = reinterpret_cast<uintptr_t>(a.B[1]) - reinterpret_cast<uintptr_t>(a.B[0]);
-    const uint32_t la = lds_addr(lds);
-    int kt = k_begin;           // next step to request
-    auto request = [&](int stage) {
-        const bool second = kt >= ksteps;
-        const int k0 = (second ? kt - ksteps : kt) * 64;
-        OperandTile<BM, ATR, NT> xa = ta;
-        OperandTile<BNO, BTR, NT> xb = tb;
-        if (second) {
-            xa.base = reinterpret_cast<const bf16_t*>(reinterpret_cast<uintptr_t>(xa.base) + hopA);
-            xb.base = reinterpret_cast<const bf16_t*>(reinterpret_cast<uintptr_t>(xb.base) + hopB);
-        }
-        xa.issue(k0, la + stage * STAGE, tid);
-        xb.issue(k0, la + stage * STAGE + ABYTES, tid);
-        if constexpr (PAIR) tb2.issue(k0, la + stage * STAGE + ABYTES + BBYTES / 2, tid);
-        ++kt;
+    OperandStream<BM, ATR, BM, NT, 1, false> oa;
+    OperandStream<BNO, BTR, BNO, NT, PAIR ? 2 : 1, PAIR> ob;
+    constexpr int LOADS = oa.N + (PAIR ? 2 : 1) * ob.N;     // requests of a wavefront per step
+    StepStream<PAIR, KG> st;
+    oa.init(a.lda, tid);
+    ob.init(a.ldb, tid);
+    st.ksteps = (a.K + 63) / 64;
+    const int all = st.ksteps * a.segs, per = (all + a.split - 1) / a.split;
+    const int k_begin = w.part * per;
+    st.at = k_begin + group;
+    st.k_end = min(all, k_begin + per);
+    st.find(a, w, row0, col0, oa, ob, tid);
+    char* ring = lds + group * S * STAGE;
+    const uint32_t la = lds_addr(ring) + wave * 1024, lb = la + ABYTES;
+    auto request = [&](uint32_t off) {
+        oa.template issue_all<0>(la + off);
+        ob.template issue_all<0>(lb + off);
+        if constexpr (PAIR) ob.template issue_all<1>(lb + BBYTES / 2 + off);
+        st.next(a, w, row0, col0, oa, ob, tid);
     };
-
     f32x16 acc[MB][NB];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -198,12 +273,15 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int 
     fa.init(lane);
     fb.init(lane);
 
-    if (kt < k_end) request(0);
-    for (int k = k_begin, stage = 0; k < k_end; ++k, stage ^= 1) {
-        wait_vmcnt<0>();
-        barrier_nofence();
-        if (kt < k_end) request(stage ^ 1);
-        const char* A = lds + stage * STAGE;
+#pragma unroll
+    for (int q = 0; q < S - 1; ++q) request(q * STAGE);
+    uint32_t off = 0, next = (S - 1) * STAGE;
+    for (int k = k_begin; k < st.k_end; k += KG) {
+        wait_vmcnt<(S - 2) * LOADS>();
+        // (the reads of the stage that is requested next have to be over, not only begun, when the wavefronts meet)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        request(next);
+        const char* A = ring + off;
         const char* B = A + ABYTES;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
@@ -216,8 +294,40 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int 
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NB; ++j) acc[i][j] = mma_bf16<EPI>(af[i], bf[j], acc[i][j]);
         }
+        next = off;
+        off = off == (S - 1) * STAGE ? 0 : off + STAGE;
+    }
+    wait_vmcnt<0>();        // (what was requested of steps behind the end writes LDS too)
+    if constexpr (KG > 1) {
+        // the other groups' sums, in the order of the groups
+        __syncthreads();
+        f32x4* area = reinterpret_cast<f32x4*>(lds);
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        area[((((group - 1) * WM * WN + wave) * MB + i) * NB + j) * 256 + q * 64 + lane] =
+                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int p = 0; p < KG - 1; ++p)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 t = area[(((p * WM * WN + wave) * MB + i) * NB + j) * 256 + q * 64 + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += t[e];
+                    }
     }
     wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
@@ -302,7 +412,7 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_f32_kernel(GemmArgs a, int t
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = Elem<float>::mma(bf[j], af[i], acc[i][j]);
+                for (int j = 0; j < NB; ++j) acc[i][j] = EPI == EPI_PART ? Elem<float>::mma(af[i], bf[j], acc[i][j]) : Elem<float>::mma(bf[j], af[i], acc[i][j]);
         }
         if (more) store(stage ^ 1);
         __syncthreads();

@@ -66,14 +66,13 @@ template <typename DT> __device__ __forceinline__ float act_both(float z, int ac
     return z;
 }
 
-// NG groups of eight columns n + step(i) ... of row m: the epilogue and the stores, part by part over all groups, so that the
-// loads of a part are under way together.  v: the product (of the first matrix), w: of the second (EPI_GATED).  b: which
+// NG groups of eight columns, group i at row m + down(i), columns n + step(i) ...: the epilogue and the stores, part by part over
+// all groups, so that the loads of a part are under way together.  v: the product (of the first matrix), w: of the second (EPI_GATED).  b: which
 // result of a batch.  FULL: all of the row and the columns exist.
-template <typename DT, int EPI, int NG, bool FULL, typename STEP>
-__device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m, int n, STEP step, float (&v)[NG][8], float (&w)[NG][8]) {
-    if (!FULL && m >= a.M) return;
-    const long at = m * a.N + n;
-    auto left = [&](int i) { return FULL ? 8 : a.N - n - step(i); };
+template <typename DT, int EPI, int NG, bool FULL, typename DOWN, typename STEP>
+__device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m, int n, DOWN down, STEP step, float (&v)[NG][8], float (&w)[NG][8]) {
+    auto at = [&](int i) { return (m + down(i)) * a.N + n + step(i); };
+    auto left = [&](int i) { return FULL ? 8 : (m + down(i) < a.M ? a.N - n - step(i) : 0); };
     auto add = [&](const float* bias, float (&x)[NG][8]) {
         Vec8<float> t[NG];
 #pragma unroll
@@ -85,7 +84,7 @@ __device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m
     };
     auto put = [&](void* p, const float (&x)[NG][8]) {
 #pragma unroll
-        for (int i = 0; i < NG; ++i) store8<DT>(p, at + step(i), left(i), x[i]);
+        for (int i = 0; i < NG; ++i) store8<DT>(p, at(i), left(i), x[i]);
     };
     auto activate = [&](auto kind) {
 #pragma unroll
@@ -100,7 +99,7 @@ __device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m
         Vec8<DT> r[NG];
         if (EPI == EPI_LINEAR && a.residual) {
 #pragma unroll
-            for (int i = 0; i < NG; ++i) r[i] = load8<DT>(a.residual, at + step(i), left(i));
+            for (int i = 0; i < NG; ++i) r[i] = load8<DT>(a.residual, at(i), left(i));
         }
         if (a.bias[0]) add(a.bias[0], v);
         if (a.z[0]) put(a.z[0], v);
@@ -133,15 +132,11 @@ template <typename DT, int EPI> __device__ __forceinline__ void epilogue8(const 
     float v1[1][8], w1[1][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { v1[0][e] = v[e]; w1[0][e] = w[e]; }
-    if (n < a.N) epilogue_groups<DT, EPI, 1, false>(a, b, m, n, [](int) { return 0; }, v1, w1);
+    if (n < a.N) epilogue_groups<DT, EPI, 1, false>(a, b, m, n, [](int) { return 0; }, [](int) { return 0; }, v1, w1);
 }
-// the partial results of one part of the contraction: plane (part, result) of M rows of ld_part values
-template <bool FULL = false>
-__device__ __forceinline__ void partial8(const GemmArgs& a, int planes, int part, int plane, long m, int n, const float (&v)[8]) {
-    if (!FULL && (m >= a.M || n >= a.N)) return;
-    float* p = a.part + (((long)part * planes + plane) * a.M + m) * a.ld_part + n;
-    *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+// where the partial results of one part of the contraction lie: plane (part, result) of M rows of ld_part values
+__device__ __forceinline__ float* partial_plane(const GemmArgs& a, int planes, int part, int plane) {
+    return a.part + ((long)part * planes + plane) * a.M * a.ld_part;
 }
 
 }  // namespace tfla

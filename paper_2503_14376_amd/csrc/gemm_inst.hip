@@ -14,13 +14,22 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     constexpr bool ATR = L == 2, BTR = L >= 1;
     const int bno = PAIR ? p.bn / 2 : p.bn;
     const int tms = (a.M + p.bm - 1) / p.bm, tns = (a.N + bno - 1) / bno;
-    const dim3 grid((unsigned)((long)tms * tns * a.split * a.batch));
+    const unsigned n = (unsigned)((long)tms * tns * a.split * a.batch);
 #if TFLA_GEMM >= 4
-    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 2, 1, ATR, BTR, PAIR, EPI>), grid, dim3(128), 0, s, a, tms, tns);
+    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(128), 0, s, a, tms, tns);
 #else
-    // (one workgroup fits a CU; the 256 of them take the tiles in turn)
-    if (p.bm == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<ATR, BTR, PAIR, EPI>), dim3(grid.x < 256 ? grid.x : 256), dim3(256), 0, s, a, tms, tns);
-    else hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, ATR, BTR, PAIR, EPI>), grid, dim3(256), 0, s, a, tms, tns);
+    // (one workgroup of the wide kernels fits a CU; the 256 of them take the tiles in turn)
+    if (p.bn == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<256, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
+    else if (p.bm == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<128, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
+    else if (p.bm == 128) hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    // 64 rows: two groups of wavefronts where no CU gets a second workgroup
+    else if constexpr (PAIR) {
+        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 1, ATR, BTR, true, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        else hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 2, ATR, BTR, true, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
+    } else {
+        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 4, 1, ATR, BTR, false, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        else hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 4, 2, ATR, BTR, false, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
+    }
 #endif
 }
 
