@@ -134,26 +134,29 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
 //          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
 //          128 x 128   6 + t max(0.63, 0.51 n) + 1.5 max(0, n - 2)
 //          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.27 t n)
+//   fp32   128 x 128   7 + max(2.3, 2.1 n) t     (steps of 32)
+//          64 x 64     5.5 + max(0.68, 0.57 n) t (pairs: 64 x 128, twice that)
+//          32 x 32     4.8 + max(0.4, 0.34 n) t  (steps of 64; pairs: 32 x 64, 1.9 times that)
 //   joining the parts  4.2 + (bytes written and read again) / 7 MB per us
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype) {
     struct Tile { int bm, bn; };
-    static constexpr Tile bf16_tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}}, f32_tiles[] = {{64, 64}};
+    static constexpr Tile bf16_tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}}, f32_tiles[] = {{128, 128}, {64, 64}, {32, 32}};
     const bool b16 = dtype == 1;
     const Tile* tiles = b16 ? bf16_tiles : f32_tiles;
-    const int kinds = b16 ? 4 : 1, step = b16 ? 64 : 32;
-    const int all = (K + step - 1) / step * segs;
+    const int kinds = b16 ? 4 : 3;
     GemmPlan best{0, 0, 1};
     double least = 0;
     for (int i = 0; i < kinds; ++i) {
         int bm = tiles[i].bm, bn = tiles[i].bn;
-        if (b16 && bm == 64 && pair) bn = 128;
+        if (pair && bm <= 64 && bn == bm) bn = 2 * bm;
         const int bno = pair ? bn / 2 : bn;
+        const int step = !b16 && bm > 32 ? 32 : 64, all = (K + step - 1) / step * segs;
         const double cells = (double)((M + bm - 1) / bm) * ((N + bno - 1) / bno) * batch;
         for (int split = 1; split <= 32 && (split == 1 || (all >= 4 * split && cells * split <= 1024)); split += split < 4 ? 1 : split / 2) {
             const double w = cells * split, t = (all + split - 1) / split, part = w < 256 ? w / 256 : 1, n = (double)(long)((w + 255) / 256);
             const double more = n > 2 ? n - 2 : 0;
             double us;
-            if (!b16) us = 5 + t * (n < 2 ? 1.6 : 0.8 * n);
+            if (!b16) us = bm == 128 ? 7 + (n < 2 ? 2.3 : 2.1 * n) * t : (bm == 64 ? 5.5 + (n < 2 ? 0.68 : 0.57 * n) * t * (pair ? 2 : 1) : 4.8 + (n < 2 ? 0.4 : 0.34 * n) * t * (pair ? 1.9 : 1));
             else if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
             else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
             else if (bm == 128) us = 6 + t * (0.51 * n > 0.63 ? 0.51 * n : 0.63) + 1.5 * more;

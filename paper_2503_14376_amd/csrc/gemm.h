@@ -222,6 +222,31 @@ template <int ROWS> struct OperandFrags<ROWS, true> {
     }
 };
 
+// Joining the sums of wavefronts that divide a contraction: wavefront `slot` (-1: none) leaves its blocks, another adds them.
+template <int MB, int NB> __device__ __forceinline__ void join_put(f32x4* area, const f32x16 (&acc)[MB][NB], int slot, int lane) {
+    if (slot < 0) return;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                area[((slot * MB + i) * NB + j) * 256 + q * 64 + lane] =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+}
+template <int MB, int NB> __device__ __forceinline__ void join_add(const f32x4* area, f32x16 (&acc)[MB][NB], int slot, int lane) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 t = area[((slot * MB + i) * NB + j) * 256 + q * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += t[e];
+            }
+}
+
 // Tile BM x BN, WM x WN wavefronts, contraction in steps of 64 through S LDS stages, S - 1 of them under way.  KG such groups of
 // wavefronts take the steps in turn, each through stages of its own, and meet in LDS at the end: where a launch has no more
 // than one workgroup per CU, a wavefront per SIMD spends a step on issuing its instructions (64 x 64 tiles: 0.29 us, with two
@@ -304,83 +329,97 @@ __global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_kernel(GemmArgs a, 
         // the other groups' sums, in the order of the groups
         __syncthreads();
         f32x4* area = reinterpret_cast<f32x4*>(lds);
-        if (group > 0) {
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        area[((((group - 1) * WM * WN + wave) * MB + i) * NB + j) * 256 + q * 64 + lane] =
-                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        }
+        join_put<MB, NB>(area, acc, group > 0 ? (group - 1) * WM * WN + wave : -1, lane);
         __syncthreads();
         if (group > 0) return;
 #pragma unroll
-        for (int p = 0; p < KG - 1; ++p)
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x4 t = area[(((p * WM * WN + wave) * MB + i) * NB + j) * 256 + q * 64 + lane];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += t[e];
-                    }
+        for (int p = 0; p < KG - 1; ++p) join_add<MB, NB>(area, acc, p * WM * WN + wave, lane);
     }
     wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
 
-// fp32 products: tiles through registers into LDS, contraction steps of 32, the contraction index contiguous per LDS row
-// (transposed operands are turned on the way).
-template <int ROWS, bool TR, int NT> struct OperandTileF32;
-template <int ROWS, int NT> struct OperandTileF32<ROWS, false, NT> {
-    RowsPrefetch<float, ROWS, 32, NT> r;
-    __device__ __forceinline__ void load(const float* p, long ld, long row0, long extent, int k0, int K, int tid) {
-        const long left = extent - row0;
-        r.template load<true>(p + row0 * ld + k0, ld, tid, left < ROWS ? (int)left : ROWS, K - k0);
+// fp32 products: tiles through registers into two LDS stages, contraction steps of STEP.  The matrix unit takes 64 clocks for
+// 2 x 32 x 32 products of fp32, a sixteenth of its bf16 rate, so LDS never bounds it: what does is how many other instructions
+// its wavefronts have to issue.  So tiles keep the order that they have in memory (plain: rows of STEP, fragments by 16-byte reads;
+// transposed: rows of ROWS, fragments value by value), and loads go through buffer descriptors, whose bounds give the zeros
+// behind the ends.  WM x WN wavefronts with WK each: those divide a step's contraction and meet in LDS at the end, for products
+// of few tiles.
+template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
+    static constexpr int R = TR ? STEP : ROWS, C = TR ? ROWS : STEP, CPR = C / 4, N = R * CPR / NT, LD = C + 4, FLOATS = R * LD;
+    static_assert(R * CPR % NT == 0, "whole loads per thread");
+    u32x4 r[N];
+    uint32_t goff[N];
+    __device__ __forceinline__ void init(long ld, int tid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) goff[i] = (uint32_t)(((tid + i * NT) / CPR * ld + (tid + i * NT) % CPR * 4) * 4);
     }
-    __device__ __forceinline__ void store(float* lds, int tid) const { r.store(lds, 36, tid); }
-};
-template <int ROWS, int NT> struct OperandTileF32<ROWS, true, NT> {
-    TrPrefetch<float, 32, ROWS, NT, false> r;
-    __device__ __forceinline__ void load(const float* p, long ld, long row0, long extent, int k0, int K, int tid) {
-        const long left = extent - row0;
-        r.template load<true>(p + (long)k0 * ld + row0, ld, tid, K - k0, left < ROWS ? (int)left : ROWS);
+    // p: the matrix; first: its first row (column) in the tile, of `extent`; K: contraction length (plain: whole groups of four).
+    // Columns behind the end of a transposed operand's rows are other rows' values: they meet results that are not stored.
+    __device__ __forceinline__ void load(const void* p, long ld, long first, long extent, int k0, int K, int tid) {
+        const long left = extent - first, rows = TR ? (K - k0 < STEP ? K - k0 : STEP) : (left < ROWS ? left : ROWS);
+        const int cols = TR ? (int)(left < ROWS ? (left + 3) & ~3l : ROWS) : (K - k0 < STEP ? K - k0 : STEP);
+        const float* base = reinterpret_cast<const float*>(p) + (TR ? k0 * ld + first : first * ld + k0);
+        const int bytes = rows > 0 && cols > 0 ? (int)((rows - 1) * ld * 4) + 4 * cols : 0;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, bytes, 0x00020000);
+        const bool ends = !TR && cols < STEP;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t at = ends && (tid + i * NT) % CPR * 4 >= cols ? 0x7ffffff0u : goff[i];
+            r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+        }
     }
-    __device__ __forceinline__ void store(float* lds, int tid) const { r.store(lds, 36, tid); }
+    __device__ __forceinline__ void store(float* lds, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + (tid + i * NT) / CPR * LD + (tid + i * NT) % CPR * 4) = r[i];
+    }
+    // the eight values k = k0 + 8 g ... of row `row`
+    static __device__ __forceinline__ Elem<float>::frag frag(const float* lds, int row, int k0, int g) {
+        if constexpr (TR) {
+            Elem<float>::frag f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] = lds[(k0 + 8 * g + e) * LD + row];
+            return f;
+        } else {
+            return Elem<float>::load(lds + row * LD + k0 + 8 * g);
+        }
+    }
 };
 
-template <int BM, int BN, int WM, int WN, bool ATR, bool BTR, bool PAIR, int EPI>
-__global__ void __launch_bounds__(WM* WN * 64) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
-    constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN, LD = 36;
+template <int BM, int BN, int WM, int WN, int WK, int STEP, bool ATR, bool BTR, bool PAIR, int EPI>
+__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
+    constexpr int NW = WM * WN, NT = NW * WK * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
-    constexpr int STAGE = (BM + BN) * LD;
+    typedef OperandTileF32<BM, ATR, STEP, NT> TileA;
+    typedef OperandTileF32<BNO, BTR, STEP, NT> TileB;
+    constexpr int STAGE = TileA::FLOATS + (PAIR ? 2 : 1) * TileB::FLOATS, KS = STEP / 16 / WK;      // 16 contraction steps per fragment
+    static_assert((WK - 1) * NW * MB * NB * 1024 <= 2 * STAGE, "the wavefronts' results fit the stages");
     __shared__ __align__(16) float lds[2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, g = lane >> 5;
+    const int wk = wave / NW, wm = wave % NW / WN, wn = wave % WN, l32 = lane & 31, g = lane >> 5;
     const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
     const long row0 = (long)w.tm * BM;
     const int col0 = w.tn * BNO;
-    const int ksteps = (a.K + 31) / 32, all = ksteps * a.segs;
+    const int ksteps = (a.K + STEP - 1) / STEP, all = ksteps * a.segs;
     const int per = (all + a.split - 1) / a.split, k_begin = w.part * per, k_end = min(all, k_begin + per);
     // (plain operands are read in groups of four: what lies behind K is the row's padding)
     const int K4 = (a.K + 3) & ~3;
 
-    OperandTileF32<BM, ATR, NT> ta;
-    OperandTileF32<BNO, BTR, NT> tb, tb2;
+    TileA ta;
+    TileB tb, tb2;
+    ta.init(a.lda, tid);
+    tb.init(a.ldb, tid);
+    if constexpr (PAIR) tb2.init(a.ldb, tid);
     auto load = [&](int kt) {
-        const int seg = kt >= ksteps ? 1 : 0, k0 = (kt - seg * ksteps) * 32;
-        ta.load(reinterpret_cast<const float*>(seg ? a.A[1] : a.A[w.b]), a.lda, row0, a.M, k0, ATR ? a.K : K4, tid);
-        tb.load(reinterpret_cast<const float*>(a.B[seg]), a.ldb, col0, a.N, k0, BTR ? a.K : K4, tid);
-        if constexpr (PAIR) tb2.load(reinterpret_cast<const float*>(a.B[1]), a.ldb, col0, a.N, k0, K4, tid);
+        const int seg = kt >= ksteps ? 1 : 0, k0 = (kt - seg * ksteps) * STEP;
+        ta.load(seg ? a.A[1] : a.A[w.b], a.lda, row0, a.M, k0, ATR ? a.K : K4, tid);
+        tb.load(a.B[seg], a.ldb, col0, a.N, k0, BTR ? a.K : K4, tid);
+        if constexpr (PAIR) tb2.load(a.B[1], a.ldb, col0, a.N, k0, K4, tid);
     };
     auto store = [&](int stage) {
         float* p = lds + stage * STAGE;
         ta.store(p, tid);
-        tb.store(p + BM * LD, tid);
-        if constexpr (PAIR) tb2.store(p + (BM + BNO) * LD, tid);
+        tb.store(p + TileA::FLOATS, tid);
+        if constexpr (PAIR) tb2.store(p + TileA::FLOATS + TileB::FLOATS, tid);
     };
     f32x16 acc[MB][NB];
 #pragma unroll
@@ -398,24 +437,37 @@ __global__ void __launch_bounds__(WM* WN * 64) gemm_f32_kernel(GemmArgs a, int t
         const bool more = k + 1 < k_end;
         if (more) load(k + 1);
         const float* A = lds + stage * STAGE;
-        const float* B = A + BM * LD;
+        const float* B = A + TileA::FLOATS;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < KS; ++ks) {
+            const int kk = (wk * KS + ks) * 16;
             Elem<float>::frag af[MB], bf[NB];
 #pragma unroll
-            for (int i = 0; i < MB; ++i) af[i] = Elem<float>::load(A + (wm * TM + i * 32 + l32) * LD + ks * 16 + g * 8);
+            for (int i = 0; i < MB; ++i) af[i] = TileA::frag(A, wm * TM + i * 32 + l32, kk, g);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const int r = PAIR ? (j & 1) * BNO + wn * (TN / 2) + (j >> 1) * 32 : wn * TN + j * 32;
-                bf[j] = Elem<float>::load(B + (r + l32) * LD + ks * 16 + g * 8);
-            }
+            for (int j = 0; j < NB; ++j)
+                bf[j] = PAIR ? TileB::frag(B + (j & 1) * TileB::FLOATS, wn * (TN / 2) + (j >> 1) * 32 + l32, kk, g)
+                             : TileB::frag(B, wn * TN + j * 32 + l32, kk, g);
+            // (blocks in turn within a product index, so that no instruction waits for the one before it)
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
+            for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = EPI == EPI_PART ? Elem<float>::mma(af[i], bf[j], acc[i][j]) : Elem<float>::mma(bf[j], af[i], acc[i][j]);
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        acc[i][j] = EPI == EPI_PART ? __builtin_amdgcn_mfma_f32_32x32x2f32(af[i].v[e], bf[j].v[e], acc[i][j], 0, 0, 0)
+                                                    : __builtin_amdgcn_mfma_f32_32x32x2f32(bf[j].v[e], af[i].v[e], acc[i][j], 0, 0, 0);
         }
         if (more) store(stage ^ 1);
         __syncthreads();
+    }
+    if constexpr (WK > 1) {
+        f32x4* area = reinterpret_cast<f32x4*>(lds);
+        join_put<MB, NB>(area, acc, wk > 0 ? (wk - 1) * NW + wave % NW : -1, lane);
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int p = 0; p < WK - 1; ++p) join_add<MB, NB>(area, acc, p * NW + wave, lane);
     }
     wave_epilogue<float, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }

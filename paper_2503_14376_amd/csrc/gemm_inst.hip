@@ -16,7 +16,10 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     const int tms = (a.M + p.bm - 1) / p.bm, tns = (a.N + bno - 1) / bno;
     const unsigned n = (unsigned)((long)tms * tns * a.split * a.batch);
 #if TFLA_GEMM >= 4
-    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(128), 0, s, a, tms, tns);
+    // (the pair's tiles cover as many columns of each matrix)
+    if (p.bm == 128) hipLaunchKernelGGL((gemm_f32_kernel<128, 128, 2, 2, 1, 32, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    else if (p.bm == 64) hipLaunchKernelGGL((gemm_f32_kernel<64, PAIR ? 128 : 64, 2, 2, 1, 32, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    else hipLaunchKernelGGL((gemm_f32_kernel<32, PAIR ? 64 : 32, 1, 1, 4, 64, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
 #else
     // (one workgroup of the wide kernels fits a CU; the 256 of them take the tiles in turn)
     if (p.bn == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<256, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
