@@ -28,8 +28,8 @@ UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "s
                                             "-mllvm", "-amdgpu-mfma-vgpr-form"]) for m in range(4)] + [
     ("tile_grads.hip", "tile_grads%d.o" % w, ["-DTFLA_GRADS_DQK=%d" % w, "-mllvm", "-pragma-unroll-threshold=200000",
                                               "-mllvm", "-amdgpu-mfma-vgpr-form"]) for w in (64, 128, 256)] + [
-    # matrix products: operand layouts 0 - 2, + 4 for fp32
-    ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l]) for l in (0, 1, 2, 4, 5, 6)]
+    # matrix products: operand layouts 0 - 2, two products in one launch 3, + 4 for fp32
+    ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l]) for l in range(8)]
 
 
 def _compile(unit):

@@ -114,15 +114,18 @@ int product_fwd(const void* x, const void* const (&w)[2], const float* const (&b
     const long Kp = padded(K);
     GemmArgs g{};
     g.A[0] = x; g.B[0] = w[0]; g.B[1] = w[1]; g.lda = K; g.ldb = K;
+    RepackArgs rp{};
+    rp.cols = K; rp.ldd = Kp; rp.dtype = dtype;
     if (l.move_x) {
-        TFLA_LAUNCH(K_ACT_BWD, launch_repack(x, ws + l.x, M, K, Kp, dtype, s));
+        rp.add(x, ws + l.x, M);
         g.A[0] = ws + l.x; g.lda = Kp;
     }
     if (l.move_w) {
-        TFLA_LAUNCH(K_ACT_BWD, launch_repack(w[0], ws + l.w0, N, K, Kp, dtype, s));
-        if (pair) TFLA_LAUNCH(K_ACT_BWD, launch_repack(w[1], ws + l.w1, N, K, Kp, dtype, s));
+        rp.add(w[0], ws + l.w0, N);
+        if (pair) rp.add(w[1], ws + l.w1, N);
         g.B[0] = ws + l.w0; g.B[1] = pair ? ws + l.w1 : nullptr; g.ldb = Kp;
     }
+    if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_repack(rp, s));
     g.M = M; g.N = N; g.K = K; g.segs = 1; g.batch = 1; g.pair = pair;
     g.bias[0] = bias[0]; g.bias[1] = bias[1]; g.residual = residual; g.out[0] = out; g.z[0] = z[0]; g.z[1] = z[1];
     g.act = act; g.dtype = dtype;
@@ -151,36 +154,44 @@ int product_bwd(const void* x, const void* const (&w)[2], const void* dy, const 
         ActBwdArgs a{};
         a.dy = dy; a.z = act == TFLA_ACT_NONE && !pair ? nullptr : z; a.u = u;
         a.dz0 = l.move_dz ? ws + l.dz0 : nullptr; a.dz1 = pair ? ws + l.dz1 : nullptr;
-        a.part = want_db ? reinterpret_cast<float*>(ws + l.dbpart) : nullptr;
+        const bool direct = act_bwd_row_blocks(M, N) == 1;       // the sums need not be joined
+        a.part = want_db && !direct ? reinterpret_cast<float*>(ws + l.dbpart) : nullptr;
+        a.db0 = direct ? db[0] : nullptr; a.db1 = direct ? db[1] : nullptr;
         a.M = M; a.N = N; a.ldd = Np; a.ldp = Np; a.act = act; a.dtype = dtype; a.pair = pair;
         TFLA_LAUNCH(K_ACT_BWD, launch_act_bwd(a, s));
     }
-    if (want_db)
+    if (want_db && (M == 0 || act_bwd_row_blocks(M, N) > 1))
         TFLA_LAUNCH(K_ACT_BWD, launch_sum_rows(reinterpret_cast<float*>(ws + l.dbpart), M > 0 ? act_bwd_row_blocks(M, N) : 0,
                                                (pair ? 2 : 1) * Np, Np, N, db[0], db[1], s));
+    GemmArgs gx{}, gw{};
+    RepackArgs rp{};
+    rp.cols = K; rp.ldd = Kp; rp.dtype = dtype;
     if (dx && M > 0) {
-        GemmArgs g{};
-        g.A[0] = dz[0]; g.A[1] = dz[1]; g.lda = ldz;
-        g.B[0] = w[0]; g.B[1] = w[1]; g.ldb = K;
+        gx.A[0] = dz[0]; gx.A[1] = dz[1]; gx.lda = ldz;
+        gx.B[0] = w[0]; gx.B[1] = w[1]; gx.ldb = K;
         if (l.move_w) {
-            TFLA_LAUNCH(K_ACT_BWD, launch_repack(w[0], ws + l.w0, N, K, Kp, dtype, s));
-            if (pair) TFLA_LAUNCH(K_ACT_BWD, launch_repack(w[1], ws + l.w1, N, K, Kp, dtype, s));
-            g.B[0] = ws + l.w0; g.B[1] = pair ? ws + l.w1 : nullptr; g.ldb = Kp;
+            rp.add(w[0], ws + l.w0, N);
+            if (pair) rp.add(w[1], ws + l.w1, N);
+            gx.B[0] = ws + l.w0; gx.B[1] = pair ? ws + l.w1 : nullptr; gx.ldb = Kp;
         }
-        g.M = M; g.N = K; g.K = N; g.segs = pair ? 2 : 1; g.batch = 1; g.out[0] = dx; g.dtype = dtype;
-        g.split = l.plan_dx.split; g.part = reinterpret_cast<float*>(ws + l.part); g.ld_part = (K + 7) & ~7;
-        TFLA_LAUNCH(K_GEMM, launch_gemm(g, l.plan_dx, false, true, EPI_STORE, s));
+        gx.M = M; gx.N = K; gx.K = N; gx.segs = pair ? 2 : 1; gx.batch = 1; gx.out[0] = dx; gx.dtype = dtype;
+        gx.split = l.plan_dx.split; gx.part = reinterpret_cast<float*>(ws + l.part); gx.ld_part = (K + 7) & ~7;
     }
     if (want_dw) {
-        GemmArgs g{};
-        g.A[0] = dz[0]; g.A[1] = dz[1]; g.lda = ldz; g.B[0] = x; g.ldb = K;
+        gw.A[0] = dz[0]; gw.A[1] = dz[1]; gw.lda = ldz; gw.B[0] = x; gw.ldb = K;
         if (l.move_x && M > 0) {
-            TFLA_LAUNCH(K_ACT_BWD, launch_repack(x, ws + l.x, M, K, Kp, dtype, s));
-            g.B[0] = ws + l.x; g.ldb = Kp;
+            rp.add(x, ws + l.x, M);
+            gw.B[0] = ws + l.x; gw.ldb = Kp;
         }
-        g.M = N; g.N = K; g.K = M; g.segs = 1; g.batch = pair ? 2 : 1; g.out[0] = dw[0]; g.out[1] = dw[1]; g.dtype = dtype;
-        g.split = l.plan_dw.split; g.part = reinterpret_cast<float*>(ws + l.part); g.ld_part = (K + 7) & ~7;
-        TFLA_LAUNCH(K_GEMM, launch_gemm(g, l.plan_dw, true, true, EPI_STORE, s));
+        gw.M = N; gw.N = K; gw.K = M; gw.segs = 1; gw.batch = pair ? 2 : 1; gw.out[0] = dw[0]; gw.out[1] = dw[1]; gw.dtype = dtype;
+        gw.split = l.plan_dw.split; gw.part = reinterpret_cast<float*>(ws + l.part); gw.ld_part = (K + 7) & ~7;
+    }
+    if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_repack(rp, s));
+    if (gx.M > 0 && gw.M > 0 && gemm_both_applies(l.plan_dx, l.plan_dw)) {
+        TFLA_LAUNCH(K_GEMM, launch_gemm_both(gx, gw, l.plan_dx, s));
+    } else {
+        if (gx.M > 0) TFLA_LAUNCH(K_GEMM, launch_gemm(gx, l.plan_dx, false, true, EPI_STORE, s));
+        if (gw.M > 0) TFLA_LAUNCH(K_GEMM, launch_gemm(gw, l.plan_dw, true, true, EPI_STORE, s));
     }
     return TFLA_OK;
 }
@@ -191,7 +202,7 @@ extern "C" {
 
 size_t tfla_norm_workspace_bytes(int direction, int M, int D, int dtype, int norm_kind) {
     if ((direction != TFLA_FWD && direction != TFLA_BWD) || check_norm(M, D, dtype, norm_kind) != TFLA_OK) return 0;
-    if (direction == TFLA_FWD || M == 0) return 0;
+    if (direction == TFLA_FWD || M == 0 || rownorm_bwd_blocks(M, D) == 1) return 0;
     return align_up((size_t)rownorm_bwd_blocks(M, D) * 2 * D * sizeof(float));
 }
 
@@ -226,9 +237,11 @@ int tfla_norm_bwd(const void* x, const void* dy, const float* rstd, const float*
     }
     const int blocks = rownorm_bwd_blocks(M, D);
     float* part = reinterpret_cast<float*>(workspace);
-    RowNormBwdArgs a{x, dy, rstd, mean, gamma, d_residual, dx, params ? part : nullptr, M, D, norm_kind, dtype, blocks};
+    const bool join = params && blocks > 1;
+    RowNormBwdArgs a{x, dy, rstd, mean, gamma, d_residual, dx, join ? part : nullptr, blocks > 1 ? nullptr : dgamma, blocks > 1 ? nullptr : dbeta,
+                     M, D, norm_kind, dtype, blocks};
     TFLA_LAUNCH(K_ROWNORM_BWD, launch_rownorm_bwd(a, s));
-    if (params) TFLA_LAUNCH(K_ROWNORM_BWD, launch_sum_rows(part, blocks, 2L * D, D, D, dgamma, dbeta, s));
+    if (join) TFLA_LAUNCH(K_ROWNORM_BWD, launch_sum_rows(part, blocks, 2L * D, D, D, dgamma, dbeta, s));
     return TFLA_OK;
 }
 

@@ -7,20 +7,22 @@ namespace tfla {
 
 // one instantiation of the products' launcher per operand layout and type (gemm_inst.hip)
 template <int L> hipError_t launch_gemm_layout(const GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);
+template <int DTYPE> hipError_t launch_gemm_both_as(const GemmArgs& x, const GemmArgs& w, int bm, hipStream_t s);
 
 namespace {
 
-// rows of `cols` elements at any address -> rows of ldd elements (a multiple of eight), zeros behind the columns
-template <typename DT> __global__ void __launch_bounds__(256) repack_kernel(const void* src, void* dst, long rows, int cols, long ldd) {
-    const int c = (blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
-    if (c >= ldd) return;
-    for (long r = (long)blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.y * 4)
-        load8<DT>(src, r * cols + c, cols - c).store(dst, r * ldd + c);
+template <typename DT> __global__ void __launch_bounds__(256) repack_kernel(RepackArgs a) {
+    const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8, q = blockIdx.z;
+    if (c >= a.ldd) return;
+    const long step = (long)gridDim.x * 4;
+#pragma unroll 4
+    for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows[q]; r += step)
+        load8<DT>(a.src[q], r * a.cols + c, a.cols - c).store(a.dst[q], r * a.ldd + c);
 }
 
-// Workgroups of 4 wavefronts: 512 columns, the rows of a row block in turn over the wavefronts.
-template <typename DT, bool PAIR> __global__ void __launch_bounds__(256) act_bwd_kernel(ActBwdArgs a, int rpb) {
-    __shared__ float red[4][PAIR ? 2 : 1][512];
+// Workgroups of NW wavefronts: 512 columns, the rows of a row block in turn over the wavefronts.
+template <typename DT, bool PAIR, int NW> __global__ void __launch_bounds__(NW * 64) act_bwd_kernel(ActBwdArgs a, int rpb) {
+    __shared__ float red[NW][PAIR ? 2 : 1][512];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = (blockIdx.y * 64 + lane) * 8, left = a.N - c;
     const long r0 = (long)blockIdx.x * rpb, r1 = min(a.M, r0 + rpb);
@@ -29,7 +31,7 @@ template <typename DT, bool PAIR> __global__ void __launch_bounds__(256) act_bwd
     for (int e = 0; e < 8; ++e) { s0[e] = 0.0f; s1[e] = 0.0f; }
     if (c < a.ldd) {
 #pragma unroll 2
-        for (long r = r0 + wave; r < r1; r += 4) {
+        for (long r = r0 + wave; r < r1; r += NW) {
             float g[8], z[8], u[8];
             load8<DT>(a.dy, r * a.N + c, left).get(g);
             if (a.z) load8<DT>(a.z, r * a.N + c, left).get(z);
@@ -53,16 +55,18 @@ template <typename DT, bool PAIR> __global__ void __launch_bounds__(256) act_bwd
             if constexpr (PAIR) store8<DT>(a.dz1, r * a.ldd + c, 8, u);
         }
     }
-    if (!a.part) return;
+    if (!a.part && !a.db0 && !a.db1) return;
     store8<float>(red[wave][0], lane * 8, 8, s0);
     if constexpr (PAIR) store8<float>(red[wave][1], lane * 8, 8, s1);
     __syncthreads();
-    for (int i = threadIdx.x; i < 512; i += 256) {
-        const int n = blockIdx.y * 512 + i;
+    for (int i = threadIdx.x; i < (PAIR ? 1024 : 512); i += NW * 64) {
+        const int p = i >> 9, n = blockIdx.y * 512 + (i & 511);
         if (n >= a.N) continue;
+        float s = red[0][p][i & 511];
 #pragma unroll
-        for (int p = 0; p < (PAIR ? 2 : 1); ++p)
-            a.part[((long)blockIdx.x * (PAIR ? 2 : 1) + p) * a.ldp + n] = ((red[0][p][i] + red[1][p][i]) + red[2][p][i]) + red[3][p][i];
+        for (int w = 1; w < NW; ++w) s += red[w][p][i & 511];
+        if (a.part) a.part[((long)blockIdx.x * (PAIR ? 2 : 1) + p) * a.ldp + n] = s;
+        else if (float* db = p ? a.db1 : a.db0) db[n] = s;
     }
 }
 
@@ -90,9 +94,15 @@ template <typename DT, int EPI> __global__ void __launch_bounds__(256) gemm_redu
     epilogue8<DT, EPI>(a, b, m, n, v, w);
 }
 
-// rows of a block of the activation's backward: the partial sums stay a small part of the traffic, and a launch has enough
-// workgroups to stream
-int rows_per_block(long M) { return M <= 1024 ? 16 : 64; }
+// Rows of a block of the activation's backward: the partial sums stay a small part of the traffic, and a launch has enough
+// workgroups to stream.  Up to 128 rows are one block of sixteen wavefronts, whose sums need no second launch.
+constexpr int ONE_BLOCK = 128;
+int rows_per_block(long M, int N) { return M <= ONE_BLOCK ? ONE_BLOCK : ((M + 63) / 64 * ((N + 511) / 512) < 1024 ? 16 : 64); }
+template <typename DT, bool PAIR> void act_bwd(const ActBwdArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)act_bwd_row_blocks(a.M, a.N), (unsigned)((a.ldd + 511) / 512));
+    if (a.M <= ONE_BLOCK) hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 16>), grid, dim3(1024), 0, s, a, ONE_BLOCK);
+    else hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 4>), grid, dim3(256), 0, s, a, rows_per_block(a.M, a.N));
+}
 
 template <typename DT> hipError_t reduce(const GemmArgs& a, int epi, hipStream_t s) {
     const dim3 grid((unsigned)((a.M + 3) / 4), (a.N + 511) / 512, a.batch), block(256);
@@ -104,25 +114,26 @@ template <typename DT> hipError_t reduce(const GemmArgs& a, int epi, hipStream_t
 
 }  // namespace
 
-hipError_t launch_repack(const void* src, void* dst, long rows, int cols, long ldd, int dtype, hipStream_t s) {
-    const long ny = (rows + 3) / 4;
-    const dim3 grid((unsigned)((ldd + 511) / 512), (unsigned)(ny < 2048 ? ny : 2048));
-    if (dtype == 1) hipLaunchKernelGGL((repack_kernel<bf16_t>), grid, dim3(256), 0, s, src, dst, rows, cols, ldd);
-    else hipLaunchKernelGGL((repack_kernel<float>), grid, dim3(256), 0, s, src, dst, rows, cols, ldd);
+hipError_t launch_repack(const RepackArgs& a, hipStream_t s) {
+    if (a.count == 0) return hipSuccess;
+    long most = 1;
+    for (int q = 0; q < a.count; ++q) most = a.rows[q] > most ? a.rows[q] : most;
+    const long n = (most + 3) / 4;
+    const dim3 grid((unsigned)(n < 1024 ? n : 1024), (unsigned)((a.ldd + 511) / 512), a.count);
+    if (a.dtype == 1) hipLaunchKernelGGL((repack_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((repack_kernel<float>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
-int act_bwd_row_blocks(long M, int N) { const int r = rows_per_block(M); return (int)((M + r - 1) / r); }
+int act_bwd_row_blocks(long M, int N) { const int r = rows_per_block(M, N); return (int)((M + r - 1) / r); }
 
 hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
-    const int rpb = rows_per_block(a.M);
-    const dim3 grid((unsigned)act_bwd_row_blocks(a.M, a.N), (unsigned)((a.ldd + 511) / 512)), block(256);
     if (a.dtype == 1) {
-        if (a.pair) hipLaunchKernelGGL((act_bwd_kernel<bf16_t, true>), grid, block, 0, s, a, rpb);
-        else hipLaunchKernelGGL((act_bwd_kernel<bf16_t, false>), grid, block, 0, s, a, rpb);
+        if (a.pair) act_bwd<bf16_t, true>(a, s);
+        else act_bwd<bf16_t, false>(a, s);
     } else {
-        if (a.pair) hipLaunchKernelGGL((act_bwd_kernel<float, true>), grid, block, 0, s, a, rpb);
-        else hipLaunchKernelGGL((act_bwd_kernel<float, false>), grid, block, 0, s, a, rpb);
+        if (a.pair) act_bwd<float, true>(a, s);
+        else act_bwd<float, false>(a, s);
     }
     return hipGetLastError();
 }
@@ -133,7 +144,7 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
 //   bf16   256 x 256   8 + n (t (1.0 + 0.45 min(1, w / 256)) + 4)        (the power that all CUs draw lowers the clock)
 //          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
 //          128 x 128   6 + t max(0.63, 0.51 n) + 1.5 max(0, n - 2)
-//          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.27 t n)
+//          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.34 t n)
 //   fp32   128 x 128   7 + max(2.3, 2.1 n) t     (steps of 32)
 //          64 x 64     5.5 + max(0.68, 0.57 n) t (pairs: 64 x 128, twice that)
 //          32 x 32     4.8 + max(0.4, 0.34 n) t  (steps of 64; pairs: 32 x 64, 1.9 times that)
@@ -160,7 +171,7 @@ GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtyp
             else if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
             else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
             else if (bm == 128) us = 6 + t * (0.51 * n > 0.63 ? 0.51 * n : 0.63) + 1.5 * more;
-            else us = 4.8 + (pair ? 0.27 : 0.177) * t * n + 0.9 * more;
+            else us = 4.8 + (pair ? 0.34 : 0.177) * t * n + 0.9 * more;
             if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
             if (best.bm == 0 || us < least) { least = us; best = {bm, bn, split}; }
         }
@@ -175,6 +186,14 @@ hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_t
     else rc = !b_tr ? launch_gemm_layout<4>(a, p, e, s) : (!a_tr ? launch_gemm_layout<5>(a, p, e, s) : launch_gemm_layout<6>(a, p, e, s));
     if (rc != hipSuccess || e != EPI_PART) return rc;
     return a.dtype == 1 ? reduce<bf16_t>(a, epi, s) : reduce<float>(a, epi, s);
+}
+
+// Small products: what a launch costs beside its work (3.4 us of the host's time, 2 of the GPU's) is saved once.
+bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w) {
+    return x.split == 1 && w.split == 1 && x.bm == w.bm && x.bm <= 64;
+}
+hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s) {
+    return x.dtype == 1 ? launch_gemm_both_as<1>(x, w, p.bm, s) : launch_gemm_both_as<0>(x, w, p.bm, s);
 }
 
 }  // namespace tfla

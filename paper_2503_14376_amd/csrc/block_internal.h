@@ -15,7 +15,8 @@ struct RowNormArgs {
 struct RowNormBwdArgs {
     const void* x; const void* dy; const float* rstd; const float* mean; const float* gamma; const void* d_residual;
     void* dx;
-    float* part;                               // (blocks, 2, D) partial sums of dgamma and dbeta, or NULL
+    // (blocks, 2, D) partial sums of dgamma and dbeta, or NULL: the sums of one block are the results (each may be NULL)
+    float* part; float* dgamma; float* dbeta;
     long M; int D, kind, dtype, blocks;
 };
 int rownorm_bwd_blocks(long M, int D);         // workgroups of the backward launch = partial sums per column
@@ -52,15 +53,24 @@ constexpr int GEMM_ROWS_MAX = 32;
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s);
 
+// dx = dz W and dw = dz^T x in one launch, where gemm_both_applies: both whole, in the same small tiles.
+bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w);
+hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s);
+
 // ---- elementwise passes around the products ---------------------------------------------------
-// (rows, cols) dense at any address -> rows of ldd elements (zeros behind the columns)
-hipError_t launch_repack(const void* src, void* dst, long rows, int cols, long ldd, int dtype, hipStream_t s);
+// Up to three matrices of (rows, cols) dense at any address -> rows of ldd elements (zeros behind the columns), in one launch.
+struct RepackArgs {
+    const void* src[3]; void* dst[3]; long rows[3];
+    int count, cols; long ldd; int dtype;
+    void add(const void* s, void* d, long r) { src[count] = s; dst[count] = d; rows[count++] = r; }
+};
+hipError_t launch_repack(const RepackArgs& a, hipStream_t s);
 // Backward of the activation: dz = dy act'(z) (act none: dz = dy), or for the pair da = dh u act'(a), du = dh act(a).
 // dz0 / dz1 in rows of ldd elements, zeros behind the columns; dz0 == NULL: sums only.  part: (row blocks, 1 or 2, ldp)
-// partial column sums in fp32 of the unrounded values, or NULL.
+// partial column sums in fp32 of the unrounded values, or NULL; with one row block the sums go to db0, db1 (each may be NULL).
 struct ActBwdArgs {
     const void* dy; const void* z; const void* u;
-    void* dz0; void* dz1; float* part;
+    void* dz0; void* dz1; float* part; float* db0; float* db1;
     long M; int N; long ldd, ldp; int act, dtype, pair;
 };
 int act_bwd_row_blocks(long M, int N);

@@ -251,18 +251,19 @@ template <int MB, int NB> __device__ __forceinline__ void join_add(const f32x4* 
 // wavefronts take the steps in turn, each through stages of its own, and meet in LDS at the end: where a launch has no more
 // than one workgroup per CU, a wavefront per SIMD spends a step on issuing its instructions (64 x 64 tiles: 0.29 us, with two
 // wavefronts per SIMD 0.2).  PAIR: the columns of a tile are BN / 2 of B[0] and the same BN / 2 of B[1], wavefront by wavefront.
+// id, total: which of the product's workgroups this is.
+template <int BM, int BN, int WM, int WN, int S, int KG> constexpr int gemm_bf16_lds = KG * S * (BM + BN) * 128;
 template <int BM, int BN, int WM, int WN, int S, int KG, bool ATR, bool BTR, bool PAIR, int EPI>
-__global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int tms, int tns) {
+__device__ __forceinline__ void gemm_bf16(const GemmArgs& a, int tms, int tns, unsigned id, unsigned total, char* lds) {
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128, STAGE = ABYTES + BBYTES;
     constexpr int JOIN = (KG - 1) * WM * WN * MB * NB * 4096;
     static_assert(JOIN <= KG * S * STAGE, "the groups' results fit the stages");
-    __shared__ __align__(1024) char lds[KG * S * STAGE];
     const int tid = threadIdx.x % NT, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const int wm = wave / WN, wn = wave % WN;
-    const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
+    const GemmWork w = gemm_work(xcd_range(id, total), tms, tns, a.split);
     const long row0 = (long)w.tm * BM;
     const int col0 = w.tn * BNO;
 
@@ -338,6 +339,19 @@ __global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_kernel(GemmArgs a, 
     wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
 
+template <int BM, int BN, int WM, int WN, int S, int KG, bool ATR, bool BTR, bool PAIR, int EPI>
+__global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_kernel(GemmArgs a, int tms, int tns) {
+    __shared__ __align__(1024) char lds[gemm_bf16_lds<BM, BN, WM, WN, S, KG>];
+    gemm_bf16<BM, BN, WM, WN, S, KG, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
+}
+// Both products of a small backward pass, dx = dz W and dw = dz^T x, in one launch: the first n of the workgroups take dx.
+template <int BM, int BN, int WM, int WN, int S, int KG>
+__global__ void __launch_bounds__(KG* WM* WN * 64) gemm_bf16_both_kernel(GemmArgs x, GemmArgs w, int xms, int xns, int wms, int wns, unsigned n) {
+    __shared__ __align__(1024) char lds[gemm_bf16_lds<BM, BN, WM, WN, S, KG>];
+    if (blockIdx.x < n) gemm_bf16<BM, BN, WM, WN, S, KG, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
+    else gemm_bf16<BM, BN, WM, WN, S, KG, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
+}
+
 // fp32 products: tiles through registers into two LDS stages, contraction steps of STEP.  The matrix unit takes 64 clocks for
 // 2 x 32 x 32 products of fp32, a sixteenth of its bf16 rate, so LDS never bounds it: what does is how many other instructions
 // its wavefronts have to issue.  So tiles keep the order that they have in memory (plain: rows of STEP, fragments by 16-byte reads;
@@ -385,18 +399,19 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
     }
 };
 
+template <int BM, int BN, int STEP, bool ATR, bool BTR> constexpr int gemm_f32_lds = 2 * ((ATR ? STEP * (BM + 4) : BM * (STEP + 4)) + (BTR ? STEP * (BN + 4) : BN * (STEP + 4)));
 template <int BM, int BN, int WM, int WN, int WK, int STEP, bool ATR, bool BTR, bool PAIR, int EPI>
-__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
+__device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, unsigned id, unsigned total, float* lds) {
     constexpr int NW = WM * WN, NT = NW * WK * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     typedef OperandTileF32<BM, ATR, STEP, NT> TileA;
     typedef OperandTileF32<BNO, BTR, STEP, NT> TileB;
     constexpr int STAGE = TileA::FLOATS + (PAIR ? 2 : 1) * TileB::FLOATS, KS = STEP / 16 / WK;      // 16 contraction steps per fragment
     static_assert((WK - 1) * NW * MB * NB * 1024 <= 2 * STAGE, "the wavefronts' results fit the stages");
-    __shared__ __align__(16) float lds[2 * STAGE];
+    static_assert(2 * STAGE == gemm_f32_lds<BM, BN, STEP, ATR, BTR>, "two stages");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wk = wave / NW, wm = wave % NW / WN, wn = wave % WN, l32 = lane & 31, g = lane >> 5;
-    const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.split);
+    const GemmWork w = gemm_work(xcd_range(id, total), tms, tns, a.split);
     const long row0 = (long)w.tm * BM;
     const int col0 = w.tn * BNO;
     const int ksteps = (a.K + STEP - 1) / STEP, all = ksteps * a.segs;
@@ -470,6 +485,19 @@ __global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a
         for (int p = 0; p < WK - 1; ++p) join_add<MB, NB>(area, acc, p * NW + wave, lane);
     }
     wave_epilogue<float, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
+}
+
+template <int BM, int BN, int WM, int WN, int WK, int STEP, bool ATR, bool BTR, bool PAIR, int EPI>
+__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
+    __shared__ __align__(16) float lds[gemm_f32_lds<BM, BN, STEP, ATR, BTR>];
+    gemm_f32<BM, BN, WM, WN, WK, STEP, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
+}
+template <int BM, int BN, int WM, int WN, int WK, int STEP>
+__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_both_kernel(GemmArgs x, GemmArgs w, int xms, int xns, int wms, int wns, unsigned n) {
+    constexpr int LX = gemm_f32_lds<BM, BN, STEP, false, true>, LW = gemm_f32_lds<BM, BN, STEP, true, true>;
+    __shared__ __align__(16) float lds[LX > LW ? LX : LW];
+    if (blockIdx.x < n) gemm_f32<BM, BN, WM, WN, WK, STEP, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
+    else gemm_f32<BM, BN, WM, WN, WK, STEP, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
 }
 
 }  // namespace tfla

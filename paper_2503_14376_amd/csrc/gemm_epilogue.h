@@ -70,9 +70,10 @@ template <typename DT> __device__ __forceinline__ float act_both(float z, int ac
 // all groups, so that the loads of a part are under way together.  v: the product (of the first matrix), w: of the second (EPI_GATED).  b: which
 // result of a batch.  FULL: all of the row and the columns exist.
 template <typename DT, int EPI, int NG, bool FULL, typename DOWN, typename STEP>
-__device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m, int n, DOWN down, STEP step, float (&v)[NG][8], float (&w)[NG][8]) {
+__device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m, int n, DOWN down, STEP step, float (&v)[NG][8], float (&w)[NG][8],
+                                                int width = 8) {
     auto at = [&](int i) { return (m + down(i)) * a.N + n + step(i); };
-    auto left = [&](int i) { return FULL ? 8 : (m + down(i) < a.M ? a.N - n - step(i) : 0); };
+    auto left = [&](int i) { return FULL ? 8 : (m + down(i) < a.M ? min(width, a.N - n - step(i)) : 0); };
     auto add = [&](const float* bias, float (&x)[NG][8]) {
         Vec8<float> t[NG];
 #pragma unroll
@@ -128,11 +129,11 @@ __device__ __forceinline__ void epilogue_groups(const GemmArgs& a, int b, long m
     put(a.out[EPI == EPI_STORE ? b : 0], v);
 }
 // one group
-template <typename DT, int EPI> __device__ __forceinline__ void epilogue8(const GemmArgs& a, int b, long m, int n, float (&v)[8], float (&w)[8]) {
+template <typename DT, int EPI> __device__ __forceinline__ void epilogue8(const GemmArgs& a, int b, long m, int n, float (&v)[8], float (&w)[8], int width = 8) {
     float v1[1][8], w1[1][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { v1[0][e] = v[e]; w1[0][e] = w[e]; }
-    if (n < a.N) epilogue_groups<DT, EPI, 1, false>(a, b, m, n, [](int) { return 0; }, [](int) { return 0; }, v1, w1);
+    if (n < a.N) epilogue_groups<DT, EPI, 1, false>(a, b, m, n, [](int) { return 0; }, [](int) { return 0; }, v1, w1, width);
 }
 // where the partial results of one part of the contraction lie: plane (part, result) of M rows of ld_part values
 __device__ __forceinline__ float* partial_plane(const GemmArgs& a, int planes, int part, int plane) {

@@ -1,11 +1,13 @@
-// Compiled once per TFLA_GEMM (0: both operands plain, 1: B transposed, 2: both transposed; + 4 for fp32): the product
-// kernels of that layout and their launcher.
+// Compiled once per TFLA_GEMM (0: both operands plain, 1: B transposed, 2: both transposed, 3: one launch for both products of a
+// small backward pass; + 4 for fp32): the product kernels of that layout and their launcher.
 #ifndef TFLA_GEMM
-#error "compile with -DTFLA_GEMM=<0..2, 4..6>"
+#error "compile with -DTFLA_GEMM=<0..7>"
 #endif
 #include "gemm_wide.h"
 
 namespace tfla {
+
+#if (TFLA_GEMM & 3) != 3
 
 namespace {
 
@@ -52,5 +54,24 @@ template <> hipError_t launch_gemm_layout<TFLA_GEMM>(const GemmArgs& a, const Ge
 #endif
     return hipGetLastError();
 }
+
+#else
+
+template <int DTYPE> hipError_t launch_gemm_both_as(const GemmArgs& x, const GemmArgs& w, int bm, hipStream_t s);
+template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, const GemmArgs& w, int bm, hipStream_t s) {
+    auto up = [&](int v) { return (v + bm - 1) / bm; };
+    const int xms = up(x.M), xns = up(x.N), wms = up(w.M), wns = up(w.N);
+    const unsigned n = (unsigned)(xms * xns), all = n + (unsigned)(wms * wns * w.batch);
+#if TFLA_GEMM == 3
+    if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, xms, xns, wms, wns, n);
+#else
+    if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    else hipLaunchKernelGGL((gemm_f32_both_kernel<32, 32, 1, 1, 4, 64>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+#endif
+    return hipGetLastError();
+}
+
+#endif
 
 }  // namespace tfla

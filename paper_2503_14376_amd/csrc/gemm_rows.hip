@@ -1,6 +1,6 @@
 // Products of few rows with a whole matrix of weights (tokens being generated): out(m, n) = sum_k x(m, k) w(n, k), m < 32.
 // What bounds them is one read of the weights, so nothing but the loads matters: every wavefront reads 16 rows of w
-// straight into the operand registers of v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), 128 bytes of each row at a time, all of
+// straight into the operand registers of v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), 64 consecutive bytes of each row per access, all of
 // its share requested before the first product; the rows of x are the other operand, out of the caches.  The wavefronts of
 // a workgroup divide the contraction and meet in LDS.  Rows may start at any address.
 #include "gemm_epilogue.h"
@@ -20,99 +20,145 @@ template <> __device__ __forceinline__ f32x4 mma16<float>(const Vec8<float>& w, 
 }
 
 // MB blocks of 16 rows of x, NW wavefronts, U pieces of 64 contraction steps in flight per wavefront.
-template <typename DT, int MB, bool PAIR, int EPI, int NW, int U>
-__global__ void __launch_bounds__(NW * 64) gemm_rows_kernel(GemmArgs a) {
-    constexpr int P = PAIR ? 2 : 1, LD = 20;
-    __shared__ __align__(16) float red[NW][P][MB * 16][LD];
+// SL slices: with no more than 16 / SL rows of x (MB = 1) the matrix unit's 16 rows and columns are 16 / SL rows of w and x in SL
+// slices of the contraction each; of its results those of equal slices count.  A block of work is then 16 / SL rows of w, so
+// that there are SL times as many: the CUs are loaded evenly, and matrices of few rows reach more of them.  (One token
+// through 512 x 8192: 12.2 us without slices, 6.0 with.)
+// HOLD: a wavefront's share of x is no more than U pieces: it stays in registers while the workgroup takes block after block,
+// the next block's weights requested before the last one's sums are joined.  (What reaches the CUs in all, 6.2 TB/s, bounds
+// the kernel: four tokens through 2 x 10944 x 4096 take 43 us where every four rows of w fetch x anew, 33 where x is one row.)
+template <typename DT, int MB, int SL, bool PAIR, int EPI, int NW, int U, bool HOLD>
+__global__ void __launch_bounds__(NW * 64) gemm_rows_kernel(GemmArgs a, int blocks) {
+    constexpr int P = PAIR ? 2 : 1, RB = 16 / SL, LD = RB + 4;
+    static_assert(SL == 1 || MB == 1, "slices take one block of rows");
+    __shared__ __align__(16) float red[NW * SL][P][MB * RB][LD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16;
-    // rows behind the last one read it again: their results are not stored
-    const long wrow = (long)min(n0 + r, a.N - 1) * a.ldb + g * 16;
+    const int r = lane & 15, g = lane >> 4, slice = r / RB;
+    const int full = a.K >> 6, pieces = (a.K + 63) >> 6, ps = (pieces + SL - 1) / SL;      // ps: pieces of a slice
     long xrow[MB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) xrow[i] = (long)min(i * 16 + r, a.M - 1) * a.lda + g * 16;
-    f32x4 acc[P][MB];
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int i = 0; i < MB; ++i) acc[p][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int full = a.K >> 6, pieces = (a.K + 63) >> 6;
-    for (int c0 = wave; c0 < pieces; c0 += NW * U) {
-        Vec8<DT> w[U][P][2], x[U][MB][2];
+    for (int i = 0; i < MB; ++i) xrow[i] = (long)min(i * 16 + r % RB, a.M - 1) * a.lda + g * 8;
+    Vec8<DT> w[U][P][2], x[U][MB][2];
+    // piece c0 + u NW of this lane's slice
+    auto fetch = [&](int c0, int n0, bool with_w, bool with_x) {
+        // rows behind the last one read it again: their results are not stored
+        const long wrow = (long)min(n0 + r % RB, a.N - 1) * a.ldb + g * 8;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + u * NW, k = c * 64;
+            const int c = c0 + u * NW, k = (slice * ps + c) * 64;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (c < full) {
+                if ((SL - 1) * ps + c < full && c < ps) {
 #pragma unroll
-                    for (int p = 0; p < P; ++p) w[u][p][h].load(a.B[p], wrow + k + h * 8);
+                    for (int p = 0; p < P; ++p)
+                        if (with_w) w[u][p][h].load(a.B[p], wrow + k + h * 32);
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) x[u][i][h].load(a.A[0], xrow[i] + k + h * 8);
-                } else if (c < pieces) {
-                    const int left = a.K - k - g * 16 - h * 8;
-#pragma unroll
-                    for (int p = 0; p < P; ++p) w[u][p][h] = load8<DT>(a.B[p], wrow + k + h * 8, left);
-#pragma unroll
-                    for (int i = 0; i < MB; ++i) x[u][i][h] = load8<DT>(a.A[0], xrow[i] + k + h * 8, left);
+                    for (int i = 0; i < MB; ++i)
+                        if (with_x) x[u][i][h].load(a.A[0], xrow[i] + k + h * 32);
                 } else {
+                    const int left = c < ps ? a.K - k - g * 8 - h * 32 : 0;
 #pragma unroll
-                    for (int p = 0; p < P; ++p) w[u][p][h].zero();
+                    for (int p = 0; p < P; ++p)
+                        if (with_w) w[u][p][h] = load8<DT>(a.B[p], wrow + k + h * 32, left);
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) x[u][i][h].zero();
+                    for (int i = 0; i < MB; ++i)
+                        if (with_x) x[u][i][h] = load8<DT>(a.A[0], xrow[i] + k + h * 32, left);
                 }
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int i = 0; i < MB; ++i) acc[p][i] = mma16<DT>(w[u][p][h], x[u][i][h], acc[p][i]);
+    };
+    int block = blockIdx.x;
+    if (HOLD) {
+        fetch(wave, block * RB, true, false);
+        fetch(wave, block * RB, false, true);
     }
-    // lane (r, g) holds row r of x, columns 4 g ... 4 g + 3
+    for (; block < blocks; block += gridDim.x) {
+        const int n0 = block * RB;
+        f32x4 acc[P][MB];
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int i = 0; i < MB; ++i) *reinterpret_cast<f32x4*>(&red[wave][p][i * 16 + r][4 * g]) = acc[p][i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < P * MB * 256; i += NW * 64) {
-        const int n = i & 15, m = (i >> 4) % (MB * 16), p = i / (MB * 256);
-        float s = red[0][p][m][n];
+            for (int i = 0; i < MB; ++i) acc[p][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c0 = wave; c0 < ps || HOLD; c0 += NW * U) {
+            if (!HOLD) fetch(c0, n0, true, true);
 #pragma unroll
-        for (int q = 1; q < NW; ++q) s += red[q][p][m][n];
-        red[0][p][m][n] = s;
-    }
-    __syncthreads();
-    const int m = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8;
-    if (m < MB * 16) {
-        float v[8], u[8];
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { v[e] = red[0][0][m][c + e]; u[e] = PAIR ? red[0][P - 1][m][c + e] : 0.0f; }
-        epilogue8<DT, EPI>(a, 0, m, n0 + c, v, u);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) acc[p][i] = mma16<DT>(w[u][p][h], x[u][i][h], acc[p][i]);
+            if (HOLD) break;
+        }
+        if (HOLD && block + (int)gridDim.x < blocks) fetch(wave, n0 + gridDim.x * RB, true, false);
+        // lane (r, g) holds column r (a slice and a row of x) of the rows 4 g ... 4 g + 3 (a slice, four rows of w)
+        if (4 * g / RB == slice) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < MB; ++i) *reinterpret_cast<f32x4*>(&red[wave * SL + slice][p][i * RB + r % RB][4 * g % RB]) = acc[p][i];
+        }
+        // (barriers without the fence of __syncthreads, which would wait for the next block's weights)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        for (int i = threadIdx.x; i < P * MB * RB * RB; i += NW * 64) {
+            const int n = i % RB, m = i / RB % (MB * RB), p = i / (MB * RB * RB);
+            float s = red[0][p][m][n];
+#pragma unroll
+            for (int q = 1; q < NW * SL; ++q) s += red[q][p][m][n];
+            red[0][p][m][n] = s;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        constexpr int W = RB < 8 ? RB : 8, GR = RB / W;
+        const int m = threadIdx.x / GR, c = threadIdx.x % GR * W;
+        if (m < MB * RB) {
+            float v[8], u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = e < W ? red[0][0][m][c + e] : 0.0f;
+                u[e] = PAIR && e < W ? red[0][P - 1][m][c + e] : 0.0f;
+            }
+            epilogue8<DT, EPI>(a, 0, m, n0 + c, v, u, W);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 }
 
-template <typename DT, int MB, bool PAIR, int EPI> void go(const GemmArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, PAIR, EPI, 8, 4>), dim3((a.N + 15) / 16), dim3(512), 0, s, a);
+// Wavefronts: as many as leave each of them four pieces, up to eight; sixteen for few blocks with more to read.  As many
+// pieces in flight as their registers hold.  Workgroups: one per block, where x is held as many as the chip runs at a time.
+template <typename DT, int MB, int SL, bool PAIR, int EPI, int NW, int U> void launch(const GemmArgs& a, int n, int ps, hipStream_t s) {
+    const int most = 256 * (NW <= 4 ? 4 : 2);
+    if (NW <= 8 && ps <= NW * U && n > most) hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, (NW <= 8)>), dim3(most), dim3(NW * 64), 0, s, a, n);
+    else hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, false>), dim3(n), dim3(NW * 64), 0, s, a, n);
 }
-template <typename DT> void by_rows(const GemmArgs& a, hipStream_t s) {
-    if (a.M <= 16) {
-        if (a.pair) go<DT, 1, true, EPI_GATED>(a, s);
-        else go<DT, 1, false, EPI_LINEAR>(a, s);
-    } else {
-        if (a.pair) go<DT, 2, true, EPI_GATED>(a, s);
-        else go<DT, 2, false, EPI_LINEAR>(a, s);
-    }
+template <typename DT, int MB, int SL, bool PAIR, int EPI> void go(const GemmArgs& a, hipStream_t s) {
+    constexpr int V = sizeof(DT) / 2 * (MB * (PAIR ? 2 : 1) < 4 ? 1 : 2), U8 = V == 4 ? 2 : 4, U16 = 4 / V;
+    const int n = (a.N + 16 / SL - 1) / (16 / SL), ps = ((a.K + 63) / 64 + SL - 1) / SL;
+    if (ps <= 16) launch<DT, MB, SL, PAIR, EPI, 4, U8>(a, n, ps, s);
+    else if (n >= 128 || ps <= 32) launch<DT, MB, SL, PAIR, EPI, 8, U8>(a, n, ps, s);
+    else launch<DT, MB, SL, PAIR, EPI, 16, U16>(a, n, ps, s);
+}
+// Slices where blocks of 16 rows leave CUs without work: fewer than 256, or a last round that is not full (one token through
+// 4096 x 4096, 256 blocks: 8.3 us whole, 9.0 in four slices; 684 blocks of a pair: 41.5 and 37.5).
+template <typename DT, bool PAIR, int EPI> void by_rows(const GemmArgs& a, hipStream_t s) {
+    const int n = (a.N + 15) / 16, rounds = (n + 255) / 256;
+    const bool uneven = n < 256 || (rounds < 8 && 256 * rounds * 10 > 11 * n);
+    if (a.M <= 4 && uneven) go<DT, 1, 4, PAIR, EPI>(a, s);
+    else if (a.M <= 8 && uneven) go<DT, 1, 2, PAIR, EPI>(a, s);
+    else if (a.M <= 16) go<DT, 1, 1, PAIR, EPI>(a, s);
+    else go<DT, 2, 1, PAIR, EPI>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s) {
-    if (a.dtype == 1) by_rows<bf16_t>(a, s);
-    else by_rows<float>(a, s);
+    if (a.dtype == 1) {
+        if (a.pair) by_rows<bf16_t, true, EPI_GATED>(a, s);
+        else by_rows<bf16_t, false, EPI_LINEAR>(a, s);
+    } else {
+        if (a.pair) by_rows<float, true, EPI_GATED>(a, s);
+        else by_rows<float, false, EPI_LINEAR>(a, s);
+    }
     return hipGetLastError();
 }
 
