@@ -95,13 +95,18 @@ template <typename DT, int EPI> __global__ void __launch_bounds__(256) gemm_redu
 }
 
 // Rows of a block of the activation's backward: the partial sums stay a small part of the traffic, and a launch has enough
-// workgroups to stream.  Up to 128 rows are one block of sixteen wavefronts, whose sums need no second launch.
-constexpr int ONE_BLOCK = 128;
-int rows_per_block(long M, int N) { return M <= ONE_BLOCK ? ONE_BLOCK : ((M + 63) / 64 * ((N + 511) / 512) < 1024 ? 16 : 64); }
+// workgroups to stream.  Up to 32 rows are one block of sixteen wavefronts, whose sums need no second launch.
+constexpr int ONE_BLOCK = 32;
+int rows_per_block(long M, int N, bool sums) {
+    if (sums && M <= ONE_BLOCK) return ONE_BLOCK;
+    const long cells = M * ((N + 511) / 512);
+    return cells >= 64 * 1024 ? 64 : (cells >= 16 * 512 ? 16 : 4);
+}
 template <typename DT, bool PAIR> void act_bwd(const ActBwdArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)act_bwd_row_blocks(a.M, a.N), (unsigned)((a.ldd + 511) / 512));
-    if (a.M <= ONE_BLOCK) hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 16>), grid, dim3(1024), 0, s, a, ONE_BLOCK);
-    else hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 4>), grid, dim3(256), 0, s, a, rows_per_block(a.M, a.N));
+    const int rpb = rows_per_block(a.M, a.N, a.part || a.db0 || a.db1);
+    const dim3 grid((unsigned)((a.M + rpb - 1) / rpb), (unsigned)((a.ldd + 511) / 512));
+    if (rpb == ONE_BLOCK) hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 16>), grid, dim3(1024), 0, s, a, rpb);
+    else hipLaunchKernelGGL((act_bwd_kernel<DT, PAIR, 4>), grid, dim3(256), 0, s, a, rpb);
 }
 
 template <typename DT> hipError_t reduce(const GemmArgs& a, int epi, hipStream_t s) {
@@ -125,7 +130,7 @@ hipError_t launch_repack(const RepackArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-int act_bwd_row_blocks(long M, int N) { const int r = rows_per_block(M, N); return (int)((M + r - 1) / r); }
+int act_bwd_row_blocks(long M, int N) { const int r = rows_per_block(M, N, true); return (int)((M + r - 1) / r); }
 
 hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
     if (a.dtype == 1) {
@@ -155,8 +160,7 @@ GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtyp
     const bool b16 = dtype == 1;
     const Tile* tiles = b16 ? bf16_tiles : f32_tiles;
     const int kinds = b16 ? 4 : 3;
-    GemmPlan best{0, 0, 1};
-    double least = 0;
+    GemmPlan best{};
     for (int i = 0; i < kinds; ++i) {
         int bm = tiles[i].bm, bn = tiles[i].bn;
         if (pair && bm <= 64 && bn == bm) bn = 2 * bm;
@@ -173,7 +177,7 @@ GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtyp
             else if (bm == 128) us = 6 + t * (0.51 * n > 0.63 ? 0.51 * n : 0.63) + 1.5 * more;
             else us = 4.8 + (pair ? 0.34 : 0.177) * t * n + 0.9 * more;
             if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
-            if (best.bm == 0 || us < least) { least = us; best = {bm, bn, split}; }
+            if (best.bm == 0 || us < best.us) best = {bm, bn, split, us};
         }
     }
     return best;
@@ -189,9 +193,7 @@ hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_t
 }
 
 // Small products: what a launch costs beside its work (3.4 us of the host's time, 2 of the GPU's) is saved once.
-bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w) {
-    return x.split == 1 && w.split == 1 && x.bm == w.bm && x.bm <= 64;
-}
+bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w) { return x.split == 1 && w.split == 1 && x.bm == w.bm && x.bm <= 64; }
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s) {
     return x.dtype == 1 ? launch_gemm_both_as<1>(x, w, p.bm, s) : launch_gemm_both_as<0>(x, w, p.bm, s);
 }

@@ -46,7 +46,7 @@ struct GemmArgs {
     float* part; long ld_part; int split;
 };
 // how a product is cut (a rule on its sizes): used for the workspace and by the launcher
-struct GemmPlan { int bm, bn, split; };
+struct GemmPlan { int bm, bn, split; double us; };      // us: time by the model
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype);
 // Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens)
 constexpr int GEMM_ROWS_MAX = 32;

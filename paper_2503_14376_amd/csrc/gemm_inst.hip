@@ -32,7 +32,7 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
         if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 1, ATR, BTR, true, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
         else hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 2, ATR, BTR, true, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
     } else {
-        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 4, 1, ATR, BTR, false, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 3, 1, ATR, BTR, false, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
         else hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 4, 2, ATR, BTR, false, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
     }
 #endif
@@ -63,7 +63,7 @@ template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, co
     const int xms = up(x.M), xns = up(x.N), wms = up(w.M), wns = up(w.N);
     const unsigned n = (unsigned)(xms * xns), all = n + (unsigned)(wms * wns * w.batch);
 #if TFLA_GEMM == 3
-    if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
     else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, xms, xns, wms, wns, n);
 #else
     if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
