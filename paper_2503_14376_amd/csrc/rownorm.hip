@@ -294,34 +294,35 @@ template <typename DT, int T, int J> void bwd(const RowNormBwdArgs& a, hipStream
 
 }  // namespace
 
-#define TFLA_BY_WIDTH(F, DT)                       \
+// (4097 to 8192 columns: forward two workgroups of 512 threads share a CU; backward 1024 threads, of which one fits either way)
+#define TFLA_BY_WIDTH(F, DT, T8K, J8K)             \
     do {                                           \
         if (a.D <= 512) F<DT, 64, 1>(a, s);        \
         else if (a.D <= 1024) F<DT, 64, 2>(a, s);  \
         else if (a.D <= 2048) F<DT, 256, 1>(a, s); \
         else if (a.D <= 4096) F<DT, 256, 2>(a, s); \
-        else if (a.D <= 8192) F<DT, 1024, 1>(a, s); \
+        else if (a.D <= 8192) F<DT, T8K, J8K>(a, s); \
         else F<DT, 1024, 2>(a, s);                 \
     } while (0)
 
 int rownorm_bwd_blocks(long M, int D) {
     // workgroups = partial sums per column: enough of them to fill the chip, few enough that the partial sums stay a small
-    // part of the traffic.  Where one takes no more than 8 rows a group, its sums are the results: 3.4 us of the host's time
-    // and a launch saved for some 0.5 us a row.
+    // part of the traffic.  Where one takes no more than 8 rows a group (wide rows: 4), its sums are the results: 3.4 us of the
+    // host's time and a launch saved for some 0.5 us a row (wide: 1.2).
     const int groups = D <= 1024 ? 4 : 1;
-    if (M <= 8 * groups) return 1;
+    if (M <= (D <= 4096 ? 8 * groups : 4)) return 1;
     const long most = D <= 4096 ? 512 : 256, need = (M + groups - 1) / groups;
     return (int)(need < most ? need : most);
 }
 
 hipError_t launch_rownorm_fwd(const RowNormArgs& a, hipStream_t s) {
-    if (a.dtype == 1) TFLA_BY_WIDTH(fwd, bf16_t);
-    else TFLA_BY_WIDTH(fwd, float);
+    if (a.dtype == 1) TFLA_BY_WIDTH(fwd, bf16_t, 512, 2);
+    else TFLA_BY_WIDTH(fwd, float, 512, 2);
     return hipGetLastError();
 }
 hipError_t launch_rownorm_bwd(const RowNormBwdArgs& a, hipStream_t s) {
-    if (a.dtype == 1) TFLA_BY_WIDTH(bwd, bf16_t);
-    else TFLA_BY_WIDTH(bwd, float);
+    if (a.dtype == 1) TFLA_BY_WIDTH(bwd, bf16_t, 1024, 1);
+    else TFLA_BY_WIDTH(bwd, float, 1024, 1);
     return hipGetLastError();
 }
 hipError_t launch_sum_rows(const float* part, int rows, long rstride, long ostride, int n, float* out0, float* out1, hipStream_t s) {
