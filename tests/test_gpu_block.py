@@ -187,6 +187,82 @@ def test_gated(tfla, i, dtype, shift):
         bu.within(name, g[name], *r)
 
 
+# ---- every tile that the sizes choose between, whole and with the contraction in parts: one product of M x N results over K
+# at a time, forward, input gradient and weight gradient -------------------------------------------------------------
+PRODUCTS = [(BF16, 520, 6001, 41), (BF16, 72, 8200, 3505), (BF16, 3500, 8200, 41), (BF16, 200, 6001, 8200), (BF16, 5000, 8200, 333),
+            (BF16, 776, 5001, 4101), (F32, 1365, 8200, 73), (F32, 200, 3501, 2500), (F32, 1000, 1544, 72), (F32, 40, 1365, 3000)]
+PAIRS = [(BF16, 3500, 4100, 41), (BF16, 3500, 4101, 200), (BF16, 6000, 73, 8200), (BF16, 2500, 8201, 333), (BF16, 8200, 72, 8200),
+         (BF16, 72, 3001, 5000), (BF16, 136, 6000, 5000), (BF16, 3001, 1365, 520), (F32, 2056, 2501, 72), (F32, 2056, 40, 5000),
+         (F32, 40, 1365, 3000), (F32, 200, 3500, 1544), (F32, 201, 2500, 4100)]
+
+
+@pytest.mark.parametrize("dtype,M,N,K", PRODUCTS)
+def test_linear_tiles(tfla, dtype, M, N, K):
+    print("linear tiles", M, N, K, dtype, flush=True)
+    gen = generator(N)
+    x, w, b = fenced(normal(gen, M, K, dtype=dtype)), fenced(normal(gen, N, K, std=K ** -0.5, dtype=dtype)), normal(gen, N)
+    (z, ez), (y, ey) = bu.linear(x, w, b, None, "silu")
+    f = tfla.linear_fwd(x, w, b, act=tfla.ACT_SILU, keep_pre=True)
+    bu.within("z", f["z"], z, ez)
+    bu.within("y", f["y"], y, ey)
+    del f, z, ez, y, ey
+    # dx: M tokens, N input columns, K output columns
+    w, dy = fenced(normal(gen, K, N, std=K ** -0.5, dtype=dtype)), fenced(normal(gen, M, K, dtype=dtype))
+    dx, edx = bu.product(dy, w.t())
+    bu.within("dx", tfla.linear_bwd(fenced(normal(gen, M, N, dtype=dtype)), w, dy, want_dw=False)["dx"], dx, edx)
+    del dx, edx
+    # dw: K tokens, N input columns, M output columns
+    x, dy = fenced(normal(gen, K, N, dtype=dtype)), fenced(normal(gen, K, M, dtype=dtype))
+    dw, edw = bu.product(dy.t(), x.t())
+    bu.within("dw", tfla.linear_bwd(x, fenced(normal(gen, M, N, dtype=dtype)), dy, want_dx=False)["dw"], dw, edw)
+
+
+@pytest.mark.parametrize("dtype,M,N,K", PAIRS)
+def test_gated_tiles(tfla, dtype, M, N, K):
+    print("gated tiles", M, N, K, dtype, flush=True)
+    gen = generator(N + 1)
+    x, wg, wu = (fenced(normal(gen, r, K, std=s, dtype=dtype)) for r, s in ((M, 1.0), (N, K ** -0.5), (N, K ** -0.5)))
+    (a, ea), (u, eu), (h, eh) = bu.gated(x, wg, wu, None, None, "gelu")
+    f = tfla.gated_fwd(x, wg, wu, act=tfla.ACT_GELU, keep_pre=True)
+    for name, r, e in (("a", a, ea), ("u", u, eu), ("h", h, eh)):
+        bu.within(name, f[name], r, e)
+    del f, a, ea, u, eu, h, eh
+    for want, T, C, O in (("dx", M, N, K), ("dw", K, N, M)):       # tokens, input columns, output columns
+        x, wg, wu = (fenced(normal(gen, r, C, std=0.05, dtype=dtype)) for r in (T, O, O))
+        a, u, dh = (fenced(normal(gen, T, O, dtype=dtype)) for _ in range(3))
+        g = tfla.gated_bwd(x, wg, wu, a, u, dh, act=tfla.ACT_RELU, want_dx=want == "dx", want_dw=want == "dw")
+        av, uv, d = a.to(bu.F64), u.to(bu.F64), dh.to(bu.F64)
+        da, du = d * uv * bu.act_grad(av, "relu"), d * bu.act(av, "relu")
+        dx, dw, _ = bu.back([da, du], [bu.U * da.abs(), bu.U * du.abs()], x, [wg, wu], dtype)
+        if want == "dx":
+            bu.within("dx", g["dx"], *dx)
+        else:
+            bu.within("dw_gate", g["dw_gate"], *dw[0])
+            bu.within("dw_up", g["dw_up"], *dw[1])
+
+
+# ---- activations over their whole range ----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_activations_over_all_values(tfla, act, dtype):
+    """every bf16 value through a projection by one and back: z is the value itself; infinities and NaN as the formula has them"""
+    x = torch.arange(65536, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).to(dtype)[:, None].contiguous()
+    x = torch.where(x.abs() < 1e-37, torch.zeros_like(x), x)       # (values that the matrix unit may take as zero)
+    one = torch.ones((1, 1), dtype=dtype, device="cuda")
+    f = tfla.linear_fwd(x, one, act=code(tfla, act), keep_pre=True)
+    ok = torch.isfinite(x[:, 0])
+    z = x[ok].to(bu.F64)
+    assert torch.equal(f["z"][ok], x[ok])
+    big = z.abs() < 1e30                                            # (z^2 of larger ones leaves fp32; the results are z or 0)
+    ref = bu.act(z, act)
+    bu.within("act", f["y"][ok][big].clone(), ref[big], (bu.FN * z.abs())[big])
+    bu.within("act of large values", f["y"][ok][~big].clone(), ref[~big], torch.zeros_like(ref[~big]))
+    assert bool(torch.isnan(f["y"][torch.isnan(x[:, 0])]).all())
+    g = tfla.linear_bwd(x, one, torch.ones_like(x), f["z"], act=code(tfla, act), want_dw=False)
+    slope = bu.act_grad(z, act)
+    bu.within("slope", g["dx"][ok][big].clone(), slope[big], (bu.FN * (1 + z.abs()) + bu.HALF[dtype] * slope.abs())[big])
+
+
 # ---- what a caller may leave out, and calls of nothing -------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_parts_that_are_not_wanted(tfla, dtype):
@@ -235,6 +311,43 @@ def test_bad_tokens_stay_in_their_rows(tfla, M, dtype):
     assert torch.equal(y[keep], y2[keep]) and torch.equal(h[keep], h2[keep])
     assert bool(torch.isnan(y2[1]).all()) and bool(torch.isnan(h2[1]).all())
     assert torch.equal(y2[2].float(), torch.where(w[:, 3] > 0, float("inf"), -float("inf")))
+
+
+# ---- tensors of more than 2^31 elements -----------------------------------------------------------------------------
+def test_norm_beyond_32_bits(tfla):
+    M, D = 1_050_000, 2056
+    gen = generator(1)
+    x = torch.randn((M, D), generator=gen, device="cuda", dtype=BF16)
+    f = tfla.norm_fwd(x)
+    b = tfla.norm_bwd(x, x, f["rstd"], d_residual=x)
+    for lo in (0, M - 64):
+        part = x[lo:lo + 64].contiguous()
+        mean, rstd, y = bu.norm(part, None, None, False, 1e-6)
+        bu.within("rstd", f["rstd"][lo:lo + 64], *rstd)
+        bu.within("y", f["y"][lo:lo + 64], *y)
+        bu.within("dx", b["dx"][lo:lo + 64], *bu.norm_back(part, part, f["rstd"][lo:lo + 64].contiguous(), None, None, part, False)[0])
+
+
+def test_products_beyond_32_bits(tfla):
+    M, K, N = 540_000, 64, 4008
+    gen = generator(2)
+    x, w = torch.randn((M, K), generator=gen, device="cuda", dtype=BF16), normal(gen, N, K, std=0.1, dtype=BF16)
+    y = tfla.linear_fwd(x, w, act=tfla.ACT_RELU)["y"]
+    dy = torch.randn((M, N), generator=gen, device="cuda", dtype=BF16)
+    g = tfla.linear_bwd(x, w, dy, want_db=True)
+    dw = edw = db = 0
+    for lo in range(0, M, 60_000):
+        part = slice(lo, lo + 60_000)
+        d = dy[part].to(bu.F64)
+        dw = dw + d.t() @ x[part].to(bu.F64)
+        edw = edw + M * bu.U * (d.abs().t() @ x[part].to(bu.F64).abs())
+        db = db + d.sum(0)
+    bu.within("dw", g["dw"], dw, edw)
+    bu.within("db", g["db"], db, M * bu.U * dy[:1000].to(bu.F64).abs().mean(0) * M)
+    for lo in (0, M - 100):
+        part = slice(lo, lo + 100)
+        bu.within("y", y[part], *bu.linear(x[part], w, None, None, "relu")[1])
+        bu.within("dx", g["dx"][part], *bu.product(dy[part], w.t()))
 
 
 # ---- differences ---------------------------------------------------------------------------------------------------
