@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_bf16_both_kernel(Gemm
 template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
     static constexpr int R = TR ? STEP : ROWS, C = TR ? ROWS : STEP, CPR = C / 4, N = R * CPR / NT, LD = C + 4, FLOATS = R * LD;
     static_assert(R * CPR % NT == 0, "whole loads per thread");
-    u32x4 r[N];
+    struct Regs { u32x4 r[N]; };
     uint32_t goff[N];
     __device__ __forceinline__ void init(long ld, int tid) {
 #pragma unroll
@@ -387,7 +387,7 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
     }
     // p: the matrix; first: its first row (column) in the tile, of `extent`; K: contraction length (plain: whole groups of four).
     // Columns behind the end of a transposed operand's rows are other rows' values: they meet results that are not stored.
-    __device__ __forceinline__ void load(const void* p, long ld, long first, long extent, int k0, int K, int tid) {
+    __device__ __forceinline__ void load(Regs& to, const void* p, long ld, long first, long extent, int k0, int K, int tid) const {
         const long left = extent - first, rows = TR ? (K - k0 < STEP ? K - k0 : STEP) : (left < ROWS ? left : ROWS);
         const int cols = TR ? (int)(left < ROWS ? (left + 3) & ~3l : ROWS) : (K - k0 < STEP ? K - k0 : STEP);
         const float* base = reinterpret_cast<const float*>(p) + (TR ? k0 * ld + first : first * ld + k0);
@@ -397,12 +397,12 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t at = ends && (tid + i * NT) % CPR * 4 >= cols ? 0x7ffffff0u : goff[i];
-            r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+            to.r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
         }
     }
-    __device__ __forceinline__ void store(float* lds, int tid) const {
+    static __device__ __forceinline__ void store(const Regs& from, float* lds, int tid) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + (tid + i * NT) / CPR * LD + (tid + i * NT) % CPR * 4) = r[i];
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + (tid + i * NT) / CPR * LD + (tid + i * NT) % CPR * 4) = from.r[i];
     }
     // the eight values k = k0 + 8 g ... of row `row`
     static __device__ __forceinline__ Elem<float>::frag frag(const float* lds, int row, int k0, int g) {
@@ -418,9 +418,13 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
 };
 
 template <int BM, int BN, int STEP, bool ATR, bool BTR> constexpr int gemm_f32_lds = 2 * ((ATR ? STEP * (BM + 4) : BM * (STEP + 4)) + (BTR ? STEP * (BN + 4) : BN * (STEP + 4)));
-template <int BM, int BN, int WM, int WN, int WK, int STEP, bool ATR, bool BTR, bool PAIR, int EPI>
+// AHEAD: steps that are loaded ahead in registers.  64 x 64 tiles take two: a pair's 1500 x 1024 x 2048 107 us against 128,
+// 2048 x 1024 x 1024 37.2 against 38.5.  32 x 32 tiles, whose work-groups are short, lose by it (333 x 1000 x 777 17.8 us
+// against 16.7), and 128 x 128 tiles have no registers left for it.
+template <int BM, int BN, int WM, int WN, int WK, int STEP, int AHEAD, bool ATR, bool BTR, bool PAIR, int EPI>
 __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, unsigned id, unsigned total, float* lds) {
     constexpr int NW = WM * WN, NT = NW * WK * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
+    static_assert(AHEAD == 1 || AHEAD == 2, "the loop's steps");
     static_assert(!PAIR || !BTR, "pairs are plain operands");
     typedef OperandTileF32<BM, ATR, STEP, NT> TileA;
     typedef OperandTileF32<BNO, BTR, STEP, NT> TileB;
@@ -438,21 +442,22 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
     const int K4 = (a.K + 3) & ~3;
 
     TileA ta;
-    TileB tb, tb2;
+    TileB tb;
     ta.init(a.lda, tid);
     tb.init(a.ldb, tid);
-    if constexpr (PAIR) tb2.init(a.ldb, tid);
-    auto load = [&](int kt) {
-        const int seg = kt >= ksteps ? 1 : 0, k0 = (kt - seg * ksteps) * STEP;
-        ta.load(seg ? a.A[1] : a.A[w.b], a.lda, row0, a.M, k0, ATR ? a.K : K4, tid);
-        tb.load(a.B[seg], a.ldb, col0, a.N, k0, BTR ? a.K : K4, tid);
-        if constexpr (PAIR) tb2.load(a.B[1], a.ldb, col0, a.N, k0, K4, tid);
+    struct { typename TileA::Regs a; typename TileB::Regs b, b2; } regs[AHEAD];
+    auto load = [&](int kt, auto& to) {
+        // (behind the last step zeros, which cost no traffic: with loads in every step it is known how many are in flight)
+        const int seg = kt < k_end && kt >= ksteps ? 1 : 0, k0 = (kt < k_end ? kt - seg * ksteps : ksteps) * STEP;
+        ta.load(to.a, seg ? a.A[1] : a.A[w.b], a.lda, row0, a.M, k0, ATR ? a.K : K4, tid);
+        tb.load(to.b, a.B[seg], a.ldb, col0, a.N, k0, BTR ? a.K : K4, tid);
+        if constexpr (PAIR) tb.load(to.b2, a.B[1], a.ldb, col0, a.N, k0, K4, tid);
     };
-    auto store = [&](int stage) {
+    auto store = [&](int stage, const auto& from) {
         float* p = lds + stage * STAGE;
-        ta.store(p, tid);
-        tb.store(p + TileA::FLOATS, tid);
-        if constexpr (PAIR) tb2.store(p + TileA::FLOATS + TileB::FLOATS, tid);
+        TileA::store(from.a, p, tid);
+        TileB::store(from.b, p + TileA::FLOATS, tid);
+        if constexpr (PAIR) TileB::store(from.b2, p + TileA::FLOATS + TileB::FLOATS, tid);
     };
     f32x16 acc[MB][NB];
 #pragma unroll
@@ -461,14 +466,14 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
         for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-    if (k_begin < k_end) {
-        load(k_begin);
-        store(0);
-    }
-    __syncthreads();
-    for (int k = k_begin, stage = 0; k < k_end; ++k, stage ^= 1) {
-        const bool more = k + 1 < k_end;
-        if (more) load(k + 1);
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) load(k_begin + p, regs[p]);
+    store(0, regs[0]);
+    load(k_begin + AHEAD, regs[0]);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    int stage = 0;
+    // step k, whose successor lies in regs[next]
+    auto step = [&](int k, auto& next) {
         const float* A = lds + stage * STAGE;
         const float* B = A + TileA::FLOATS;
 #pragma unroll
@@ -491,8 +496,20 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
                         acc[i][j] = EPI == EPI_PART ? __builtin_amdgcn_mfma_f32_32x32x2f32(af[i].v[e], bf[j].v[e], acc[i][j], 0, 0, 0)
                                                     : __builtin_amdgcn_mfma_f32_32x32x2f32(bf[j].v[e], af[i].v[e], acc[i][j], 0, 0, 0);
         }
-        if (more) store(stage ^ 1);
-        __syncthreads();
+        stage ^= 1;
+        store(stage, next);
+        load(k + 1 + AHEAD, next);
+        // (without the fence of __syncthreads, which would wait for the loads)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    // (one way back to the loop's start, or the compiler would count the loads in flight there as none)
+    for (int k = k_begin;;) {
+        if (k++ >= k_end) break;
+        step(k - 1, regs[AHEAD - 1]);
+        if constexpr (AHEAD > 1) {
+            if (k++ >= k_end) break;
+            step(k - 1, regs[0]);
+        }
     }
     if constexpr (WK > 1) {
         f32x4* area = reinterpret_cast<f32x4*>(lds);
@@ -505,17 +522,17 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
     wave_epilogue<float, EPI, PAIR, MB, NB>(a, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int WK, int STEP, bool ATR, bool BTR, bool PAIR, int EPI>
+template <int BM, int BN, int WM, int WN, int WK, int STEP, int AHEAD, bool ATR, bool BTR, bool PAIR, int EPI>
 __global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a, int tms, int tns) {
     __shared__ __align__(16) float lds[gemm_f32_lds<BM, BN, STEP, ATR, BTR>];
-    gemm_f32<BM, BN, WM, WN, WK, STEP, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
+    gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
 }
-template <int BM, int BN, int WM, int WN, int WK, int STEP>
+template <int BM, int BN, int WM, int WN, int WK, int STEP, int AHEAD>
 __global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_both_kernel(GemmArgs x, GemmArgs w, int xms, int xns, int wms, int wns, unsigned n) {
     constexpr int LX = gemm_f32_lds<BM, BN, STEP, false, true>, LW = gemm_f32_lds<BM, BN, STEP, true, true>;
     __shared__ __align__(16) float lds[LX > LW ? LX : LW];
-    if (blockIdx.x < n) gemm_f32<BM, BN, WM, WN, WK, STEP, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
-    else gemm_f32<BM, BN, WM, WN, WK, STEP, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
+    if (blockIdx.x < n) gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
+    else gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
 }
 
 }  // namespace tfla

@@ -19,9 +19,9 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     const unsigned n = (unsigned)((long)tms * tns * a.split * a.batch);
 #if TFLA_GEMM >= 4
     // (the pair's tiles cover as many columns of each matrix)
-    if (p.bm == 128) hipLaunchKernelGGL((gemm_f32_kernel<128, 128, 2, 2, 1, 32, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
-    else if (p.bm == 64) hipLaunchKernelGGL((gemm_f32_kernel<64, PAIR ? 128 : 64, 2, 2, 1, 32, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
-    else hipLaunchKernelGGL((gemm_f32_kernel<32, PAIR ? 64 : 32, 1, 1, 4, 64, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    if (p.bm == 128) hipLaunchKernelGGL((gemm_f32_kernel<128, 128, 2, 2, 1, 32, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    else if (p.bm == 64) hipLaunchKernelGGL((gemm_f32_kernel<64, PAIR ? 128 : 64, 2, 2, 1, 32, 2, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    else hipLaunchKernelGGL((gemm_f32_kernel<32, PAIR ? 64 : 32, 1, 1, 4, 64, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
 #else
     // (one workgroup of the wide kernels fits a CU; the 256 of them take the tiles in turn)
     if (p.bn == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<256, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
@@ -66,8 +66,8 @@ template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, co
     if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
     else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, xms, xns, wms, wns, n);
 #else
-    if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
-    else hipLaunchKernelGGL((gemm_f32_both_kernel<32, 32, 1, 1, 4, 64>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32, 2>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    else hipLaunchKernelGGL((gemm_f32_both_kernel<32, 32, 1, 1, 4, 64, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
 #endif
     return hipGetLastError();
 }
