@@ -362,12 +362,15 @@ __global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_bf16_kernel(GemmArgs 
     __shared__ __align__(1024) char lds[gemm_bf16_lds<BM, BN, WM, WN, S, KG>];
     gemm_bf16<BM, BN, WM, WN, S, KG, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
 }
-// Both products of a small backward pass, dx = dz W and dw = dz^T x, in one launch: the first n of the workgroups take dx.
+// Both products of a small backward pass, dx = dz W and dw = dz^T x, in one launch: nx workgroups from x0 on take dx.  Those
+// with the longer contraction come first, so that the shorter ones fill the end (2392 x 656 x 800 25.5 us against 27.1).
+struct BothGrid { int xms, xns, wms, wns; unsigned nx, x0; };
 template <int BM, int BN, int WM, int WN, int S, int KG>
-__global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_bf16_both_kernel(GemmArgs x, GemmArgs w, int xms, int xns, int wms, int wns, unsigned n) {
+__global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_bf16_both_kernel(GemmArgs x, GemmArgs w, BothGrid n) {
     __shared__ __align__(1024) char lds[gemm_bf16_lds<BM, BN, WM, WN, S, KG>];
-    if (blockIdx.x < n) gemm_bf16<BM, BN, WM, WN, S, KG, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
-    else gemm_bf16<BM, BN, WM, WN, S, KG, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
+    const unsigned i = blockIdx.x;
+    if (i >= n.x0 && i < n.x0 + n.nx) gemm_bf16<BM, BN, WM, WN, S, KG, false, true, false, EPI_STORE>(x, n.xms, n.xns, i - n.x0, n.nx, lds);
+    else gemm_bf16<BM, BN, WM, WN, S, KG, true, true, false, EPI_STORE>(w, n.wms, n.wns, i < n.x0 ? i : i - n.nx, gridDim.x - n.nx, lds);
 }
 
 // fp32 products: tiles through registers into two LDS stages, contraction steps of STEP.  The matrix unit takes 64 clocks for
@@ -528,11 +531,12 @@ __global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_kernel(GemmArgs a
     gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, ATR, BTR, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
 }
 template <int BM, int BN, int WM, int WN, int WK, int STEP, int AHEAD>
-__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_both_kernel(GemmArgs x, GemmArgs w, int xms, int xns, int wms, int wns, unsigned n) {
+__global__ void __launch_bounds__(WM* WN* WK * 64, 2) gemm_f32_both_kernel(GemmArgs x, GemmArgs w, BothGrid n) {
     constexpr int LX = gemm_f32_lds<BM, BN, STEP, false, true>, LW = gemm_f32_lds<BM, BN, STEP, true, true>;
     __shared__ __align__(16) float lds[LX > LW ? LX : LW];
-    if (blockIdx.x < n) gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, false, true, false, EPI_STORE>(x, xms, xns, blockIdx.x, n, lds);
-    else gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, true, true, false, EPI_STORE>(w, wms, wns, blockIdx.x - n, gridDim.x - n, lds);
+    const unsigned i = blockIdx.x;
+    if (i >= n.x0 && i < n.x0 + n.nx) gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, false, true, false, EPI_STORE>(x, n.xms, n.xns, i - n.x0, n.nx, lds);
+    else gemm_f32<BM, BN, WM, WN, WK, STEP, AHEAD, true, true, false, EPI_STORE>(w, n.wms, n.wns, i < n.x0 ? i : i - n.nx, gridDim.x - n.nx, lds);
 }
 
 }  // namespace tfla

@@ -59,15 +59,32 @@ template <> hipError_t launch_gemm_layout<TFLA_GEMM>(const GemmArgs& a, const Ge
 
 template <int DTYPE> hipError_t launch_gemm_both_as(const GemmArgs& x, const GemmArgs& w, int bm, hipStream_t s);
 template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, const GemmArgs& w, int bm, hipStream_t s) {
-    auto up = [&](int v) { return (v + bm - 1) / bm; };
-    const int xms = up(x.M), xns = up(x.N), wms = up(w.M), wns = up(w.N);
-    const unsigned n = (unsigned)(xms * xns), all = n + (unsigned)(wms * wns * w.batch);
+    auto up = [](int v, int by) { return (v + by - 1) / by; };
+    BothGrid g;
+    unsigned all;
+    auto cut = [&](int bn) {
+        g = {up(x.M, bm), up(x.N, bn), up(w.M, bm), up(w.N, bn), 0, 0};
+        g.nx = (unsigned)(g.xms * g.xns);
+        const unsigned nw = (unsigned)(g.wms * g.wns * w.batch);
+        g.x0 = (long)w.K * w.segs > (long)x.K * x.segs ? nw : 0;
+        all = g.nx + nw;
+    };
+    cut(bm);
 #if TFLA_GEMM == 3
-    if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
-    else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, xms, xns, wms, wns, n);
+    const long longest = up((int)(g.x0 ? w.K : x.K), 64) * (g.x0 ? w.segs : x.segs);
+    const long steps = (long)g.nx * up(x.K, 64) * x.segs + (long)(all - g.nx) * up(w.K, 64) * w.segs;
+    // 64 x 128 tiles bring three quarters of the operands' bytes into LDS, which is what bounds these launches, but have half the
+    // workgroups: taken where the longest of them is at most half of an even share of the steps (2952 x 896 x 3088 65.9 us
+    // against 82.9, 944 x 1624 x 1360 25.2 against 30.3; with a longest of a whole share 512 x 1024 x 1365, a pair, 26.3 against
+    // 22.3).  Up to a workgroup per CU two groups of wavefronts share a tile's steps.
+    if (all > 512 && 2 * longest * 256 <= steps) {
+        cut(128);
+        hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 128, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
+    } else if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
+    else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, g);
 #else
-    if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32, 2>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
-    else hipLaunchKernelGGL((gemm_f32_both_kernel<32, 32, 1, 1, 4, 64, 1>), dim3(all), dim3(256), 0, s, x, w, xms, xns, wms, wns, n);
+    if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32, 2>), dim3(all), dim3(256), 0, s, x, w, g);
+    else hipLaunchKernelGGL((gemm_f32_both_kernel<32, 32, 1, 1, 4, 64, 1>), dim3(all), dim3(256), 0, s, x, w, g);
 #endif
     return hipGetLastError();
 }

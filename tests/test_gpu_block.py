@@ -241,6 +241,36 @@ def test_gated_tiles(tfla, dtype, M, N, K):
             bu.within("dw_up", g["dw_up"], *dw[1])
 
 
+# Both products of a backward pass in one launch: the longer contraction (columns of the result, or tokens) first, and every
+# choice of tile and of wavefront groups
+BOTH = [(1, BF16, 600, 130, 100), (1, BF16, 70, 133, 555), (1, BF16, 365, 1243, 2227), (1, BF16, 2390, 651, 801), (1, BF16, 431, 2839, 757),
+        (1, BF16, 2061, 837, 1255), (2, BF16, 531, 1333, 941), (2, BF16, 1221, 2197, 287), (2, BF16, 1013, 1527, 653),
+        (1, F32, 1000, 301, 99), (1, F32, 99, 301, 1003), (2, F32, 777, 515, 259), (2, F32, 257, 515, 770), (1, F32, 1021, 1023, 1025)]
+
+
+@pytest.mark.parametrize("count,dtype,M,K,N", BOTH)
+def test_both_backward_products(tfla, count, dtype, M, K, N):
+    print("both", count, M, K, N, dtype, flush=True)
+    gen = generator(N + 2)
+    x = fenced(normal(gen, M, K, dtype=dtype))
+    ws = [fenced(normal(gen, N, K, std=0.05, dtype=dtype)) for _ in range(count)]
+    if count == 1:
+        dy = fenced(normal(gen, M, N, dtype=dtype))
+        dx, dw, _ = bu.back([dy.to(bu.F64)], [torch.zeros_like(dy, dtype=bu.F64)], x, ws, dtype)
+        g = tfla.linear_bwd(x, ws[0], dy)
+        names = ["dw"]
+    else:
+        a, u, dh = (fenced(normal(gen, M, N, dtype=dtype)) for _ in range(3))
+        g = tfla.gated_bwd(x, ws[0], ws[1], a, u, dh, act=tfla.ACT_RELU)
+        av, uv, d = a.to(bu.F64), u.to(bu.F64), dh.to(bu.F64)
+        da, du = d * uv * bu.act_grad(av, "relu"), d * bu.act(av, "relu")
+        dx, dw, _ = bu.back([da, du], [bu.U * da.abs(), bu.U * du.abs()], x, ws, dtype)
+        names = ["dw_gate", "dw_up"]
+    bu.within("dx", g["dx"], *dx)
+    for name, r in zip(names, dw):
+        bu.within(name, g[name], *r)
+
+
 # ---- activations over their whole range ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
