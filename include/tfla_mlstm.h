@@ -284,8 +284,8 @@ TFLA_API int tfla_transfer_gain(const void* h, const void* v, int B, int NH, int
  *    dz / da / du of the backward passes on its way into the matrix products (db is summed from the unrounded values).
  *  - 0 <= M <= 2^24; 1 <= K, N <= 2^20; 1 <= D <= 16384; M * K, M * N and N * K at most 2^36.  M = 0 is no work: forward
  *    calls write nothing, backward calls write zeros to the gradients of weights, biases, gamma and beta.
- *  - Tensors may lie at any address that their element type allows and K, N, D may be odd.  The products work on rows that
- *    are multiples of 16 bytes at 16-byte addresses; other operands are copied into the workspace first.
+ *  - Tensors may lie at any address that their element type allows and K, N, D may be odd.  The products of bf16 work on
+ *    rows that are multiples of 16 bytes at 16-byte addresses; other operands are copied into the workspace first.
  *  - Results do not depend on the order of execution: the same call gives the same bits.
  *  - Outputs must not overlap inputs, except that y / dx of the norm may be x, dy or d_residual, and y of the linear
  *    projection may be its residual.

@@ -11,13 +11,13 @@ template <int DTYPE> hipError_t launch_gemm_both_as(const GemmArgs& x, const Gem
 
 namespace {
 
-template <typename DT> __global__ void __launch_bounds__(256) repack_kernel(RepackArgs a) {
+__global__ void __launch_bounds__(256) repack_kernel(RepackArgs a) {
     const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8, q = blockIdx.z;
     if (c >= a.ldd) return;
     const long step = (long)gridDim.x * 4;
 #pragma unroll 4
     for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows[q]; r += step)
-        load8<DT>(a.src[q], r * a.cols + c, a.cols - c).store(a.dst[q], r * a.ldd + c);
+        load8<bf16_t>(a.src[q], r * a.cols + c, a.cols - c).store(a.dst[q], r * a.ldd + c);
 }
 
 // Workgroups of NW wavefronts: 512 columns, the rows of a row block in turn over the wavefronts.
@@ -125,8 +125,7 @@ hipError_t launch_repack(const RepackArgs& a, hipStream_t s) {
     for (int q = 0; q < a.count; ++q) most = a.rows[q] > most ? a.rows[q] : most;
     const long n = (most + 3) / 4;
     const dim3 grid((unsigned)(n < 1024 ? n : 1024), (unsigned)((a.ldd + 511) / 512), a.count);
-    if (a.dtype == 1) hipLaunchKernelGGL((repack_kernel<bf16_t>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((repack_kernel<float>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(repack_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

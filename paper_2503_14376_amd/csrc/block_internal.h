@@ -58,10 +58,10 @@ bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w);
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s);
 
 // ---- elementwise passes around the products ---------------------------------------------------
-// Up to three matrices of (rows, cols) dense at any address -> rows of ldd elements (zeros behind the columns), in one launch.
+// Up to three bf16 matrices of (rows, cols) dense at any address -> rows of ldd elements (zeros behind the columns), in one launch.
 struct RepackArgs {
     const void* src[3]; void* dst[3]; long rows[3];
-    int count, cols; long ldd; int dtype;
+    int count, cols; long ldd;
     void add(const void* s, void* d, long r) { src[count] = s; dst[count] = d; rows[count++] = r; }
 };
 hipError_t launch_repack(const RepackArgs& a, hipStream_t s);

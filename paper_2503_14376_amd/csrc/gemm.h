@@ -388,11 +388,12 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
 #pragma unroll
         for (int i = 0; i < N; ++i) goff[i] = (uint32_t)(((tid + i * NT) / CPR * ld + (tid + i * NT) % CPR * 4) * 4);
     }
-    // p: the matrix; first: its first row (column) in the tile, of `extent`; K: contraction length (plain: whole groups of four).
-    // Columns behind the end of a transposed operand's rows are other rows' values: they meet results that are not stored.
+    // p: the matrix; first: its first row (column) in the tile, of `extent`; K: contraction length.  Rows may begin at any
+    // element: these loads want no more than 4 bytes' alignment, and their bounds hold word by word.  Columns behind the end of a
+    // transposed operand's rows are other rows' values: they meet results that are not stored.
     __device__ __forceinline__ void load(Regs& to, const void* p, long ld, long first, long extent, int k0, int K, int tid) const {
         const long left = extent - first, rows = TR ? (K - k0 < STEP ? K - k0 : STEP) : (left < ROWS ? left : ROWS);
-        const int cols = TR ? (int)(left < ROWS ? (left + 3) & ~3l : ROWS) : (K - k0 < STEP ? K - k0 : STEP);
+        const int cols = TR ? (int)(left < ROWS ? left : ROWS) : (K - k0 < STEP ? K - k0 : STEP);
         const float* base = reinterpret_cast<const float*>(p) + (TR ? k0 * ld + first : first * ld + k0);
         const int bytes = rows > 0 && cols > 0 ? (int)((rows - 1) * ld * 4) + 4 * cols : 0;
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, bytes, 0x00020000);
@@ -406,6 +407,12 @@ template <int ROWS, bool TR, int STEP, int NT> struct OperandTileF32 {
     static __device__ __forceinline__ void store(const Regs& from, float* lds, int tid) {
 #pragma unroll
         for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + (tid + i * NT) / CPR * LD + (tid + i * NT) % CPR * 4) = from.r[i];
+    }
+    // A plain operand's last group of four can end in the next row: zeros in the place of columns k ... of that group
+    static __device__ __forceinline__ void clear(float* lds, int k, int tid) {
+        if constexpr (!TR)
+            for (int i = tid; i < ROWS * 4; i += NT)
+                if ((k & ~3) + i % 4 >= k) lds[i / 4 * LD + (k & ~3) + i % 4] = 0.0f;
     }
     // the eight values k = k0 + 8 g ... of row `row`
     static __device__ __forceinline__ Elem<float>::frag frag(const float* lds, int row, int k0, int g) {
@@ -441,8 +448,6 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
     const int col0 = w.tn * BNO;
     const int ksteps = (a.K + STEP - 1) / STEP, all = ksteps * a.segs;
     const int per = (all + a.split - 1) / a.split, k_begin = w.part * per, k_end = min(all, k_begin + per);
-    // (plain operands are read in groups of four: what lies behind K is the row's padding)
-    const int K4 = (a.K + 3) & ~3;
 
     TileA ta;
     TileB tb;
@@ -452,9 +457,9 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
     auto load = [&](int kt, auto& to) {
         // (behind the last step zeros, which cost no traffic: with loads in every step it is known how many are in flight)
         const int seg = kt < k_end && kt >= ksteps ? 1 : 0, k0 = (kt < k_end ? kt - seg * ksteps : ksteps) * STEP;
-        ta.load(to.a, seg ? a.A[1] : a.A[w.b], a.lda, row0, a.M, k0, ATR ? a.K : K4, tid);
-        tb.load(to.b, a.B[seg], a.ldb, col0, a.N, k0, BTR ? a.K : K4, tid);
-        if constexpr (PAIR) tb.load(to.b2, a.B[1], a.ldb, col0, a.N, k0, K4, tid);
+        ta.load(to.a, seg ? a.A[1] : a.A[w.b], a.lda, row0, a.M, k0, a.K, tid);
+        tb.load(to.b, a.B[seg], a.ldb, col0, a.N, k0, a.K, tid);
+        if constexpr (PAIR) tb.load(to.b2, a.B[1], a.ldb, col0, a.N, k0, a.K, tid);
     };
     auto store = [&](int stage, const auto& from) {
         float* p = lds + stage * STAGE;
@@ -475,10 +480,19 @@ __device__ __forceinline__ void gemm_f32(const GemmArgs& a, int tms, int tns, un
     load(k_begin + AHEAD, regs[0]);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     int stage = 0;
+    // the next step whose plain operands end inside a group
+    int ends = (ATR && BTR) || a.K % 4 == 0 ? -1 : (k_begin / ksteps + 1) * ksteps - 1;
     // step k, whose successor lies in regs[next]
     auto step = [&](int k, auto& next) {
-        const float* A = lds + stage * STAGE;
-        const float* B = A + TileA::FLOATS;
+        float* A = lds + stage * STAGE;
+        float* B = A + TileA::FLOATS;
+        if (k == ends) {
+            TileA::clear(A, a.K % STEP, tid);
+            TileB::clear(B, a.K % STEP, tid);
+            if constexpr (PAIR) TileB::clear(B + TileB::FLOATS, a.K % STEP, tid);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            ends += ksteps;
+        }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int kk = (wk * KS + ks) * 16;

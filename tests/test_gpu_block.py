@@ -271,6 +271,31 @@ def test_both_backward_products(tfla, count, dtype, M, K, N):
         bu.within(name, g[name], *r)
 
 
+@pytest.mark.parametrize("M,K,N", [(40, 61, 77), (333, 1001, 70), (150, 66, 1400), (1500, 995, 1030), (2050, 2050, 2050)])
+def test_fp32_rows_that_end_inside_a_group(tfla, M, K, N):
+    """rows are read in groups of four: what the next row begins with, infinities included, and what follows the last row stays out"""
+    print("groups", M, K, N, flush=True)
+    gen = generator(M)
+    x, w, dy = (fenced(normal(gen, r, c, std=c ** -0.5, dtype=F32)) for r, c in ((M, K), (N, K), (M, N)))
+    row = M // 2
+    x[row, 0], dy[row, 0] = float("inf"), float("inf")
+    keep = torch.arange(M, device="cuda") != row
+    y = tfla.linear_fwd(x, w)["y"]
+    assert not torch.isfinite(y[row]).any()
+    (_, _), (ry, ery) = bu.linear(x[keep], w, None, None, "none")
+    bu.within("y", y[keep], ry, ery)
+    # dx: a row of dy is a row of the contraction's operand
+    dx = tfla.linear_bwd(x, w, dy, want_dw=False)["dx"]
+    assert not torch.isfinite(dx[row]).any()
+    bu.within("dx", dx[keep], *bu.product(dy[keep], w.t()))
+    # dw with the infinities taken out: both operands transposed
+    x[row, 0], dy[row, 0] = 0.0, 0.0
+    x[:, K - 1], dy[:, N - 1] = float("inf"), 1.0
+    dw = tfla.linear_bwd(x, w, dy, want_dx=False)["dw"]
+    assert not torch.isfinite(dw[:, K - 1]).any()
+    bu.within("dw", dw[:, :K - 1], *bu.product(dy.t(), x[:, :K - 1].t()))
+
+
 # ---- activations over their whole range ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
