@@ -66,7 +66,8 @@ struct RepackArgs {
 };
 hipError_t launch_repack(const RepackArgs& a, hipStream_t s);
 // Backward of the activation: dz = dy act'(z) (act none: dz = dy), or for the pair da = dh u act'(a), du = dh act(a).
-// dz0 / dz1 in rows of ldd elements, zeros behind the columns; dz0 == NULL: sums only.  part: (row blocks, 1 or 2, ldp)
+// dz is rounded to the tensors' type, as the matrix unit takes it (bf16: half a step, 2^-8, independent from element to element
+// of the sums that follow); the column sums take it before that.  dz0 / dz1 in rows of ldd elements, zeros behind the columns; dz0 == NULL: sums only.  part: (row blocks, 1 or 2, ldp)
 // partial column sums in fp32 of the unrounded values, or NULL; with one row block the sums go to db0, db1 (each may be NULL).
 struct ActBwdArgs {
     const void* dy; const void* z; const void* u;

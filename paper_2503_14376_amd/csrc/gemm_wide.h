@@ -1,6 +1,8 @@
 // bf16 products in tiles of 256 x 256 or 256 x 128 (BN): four wavefronts, one per SIMD, each with 128 x BN / 2 results in its
 // accumulation registers.
 // (Eight wavefronts of 128 x 64 read half as much again from LDS; under load the clock goes by the power that is drawn.)
+// The matrix unit bounds it, busy in 76 - 83 % of the CUs' clocks, at a clock that falls with the operands' toggling (zeros take
+// 1 / 1.35 of the time of random values): 8192^3 1439 TFLOP/s, pair 8192 x 4096 x 10944 1.10 - 1.19 ms (1234 - 1330).
 //
 // A step of the contraction is 64 wide.  Each operand's tile is kept as two halves (half h: of every wavefront's 128 rows or
 // columns the first or second half; of a pair's columns: matrix h), in two slots each: 128 KB for BN = 256.  A step has two phases

