@@ -260,26 +260,38 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_bwd_kernel(RowNormB
     }
 }
 
-// Column sums of partial rows: 64 columns per workgroup, 16 slices of the rows side by side, joined in LDS in order.
+// Column sums of partial rows: 32 columns per workgroup, 32 slices of the rows side by side, joined in LDS in order.  A slice
+// has eight loads under way, also at its end (in place of those behind it, its last row), where a plain loop would wait for one
+// after another: 1132 rows of 125 columns 3.8 us, against 6.7 by 16 slices of 64 columns in a plain loop.
 __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* part, int rows, long rstride, long ostride, int n, float* out0,
                                                         float* out1) {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
+    __shared__ float red[32][32];
+    const int lane = threadIdx.x & 31, sl = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
     float* out = blockIdx.y ? out1 : out0;
-    const float* p = part + (blockIdx.y ? ostride : 0) + c;
-    const int per = (rows + 15) / 16, r1 = min(rows, (sl + 1) * per);
+    const int per = (rows + 31) / 32, r0 = sl * per, left = min(rows - r0, per);
+    const float* p = part + (blockIdx.y ? ostride : 0) + c + r0 * rstride;
     float s = 0.0f;
     if (c < n) {
-#pragma unroll 8
-        for (int r = sl * per; r < r1; ++r) s += p[(long)r * rstride];
+        int r = 0;
+        for (; r + 8 <= left; r += 8, p += 8 * rstride) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += p[k * rstride];
+        }
+        if (r < left) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p[min(k, left - 1 - r) * rstride];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += r + k < left ? v[k] : 0.0f;
+        }
     }
     red[sl][lane] = s;
     __syncthreads();
     if (sl == 0 && c < n) {
         s = red[0][lane];
 #pragma unroll
-        for (int k = 1; k < 16; ++k) s += red[k][lane];
+        for (int k = 1; k < 32; ++k) s += red[k][lane];
         out[c] = s;
     }
 }
@@ -332,7 +344,7 @@ hipError_t launch_sum_rows(const float* part, int rows, long rstride, long ostri
     const bool both = out0 && out1;
     if (!out0 && !out1) return hipSuccess;
     const float* p = out0 ? part : part + ostride;
-    hipLaunchKernelGGL(sum_rows_kernel, dim3((n + 63) / 64, both ? 2 : 1), dim3(1024), 0, s, p, rows, rstride, ostride, n,
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((n + 31) / 32, both ? 2 : 1), dim3(1024), 0, s, p, rows, rstride, ostride, n,
                        out0 ? out0 : out1, out1);
     return hipGetLastError();
 }
