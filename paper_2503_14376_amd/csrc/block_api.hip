@@ -48,15 +48,16 @@ int check_product(int M, int K, int N, int act, int dtype) {
 // caller says) and the call (as the pointers are).
 struct FwdLayout {
     size_t x, w0, w1, part, bytes;
-    GemmPlan plan; bool move_x, move_w;
+    GemmPlan plan; bool rows, move_x, move_w;
 };
 FwdLayout fwd_layout(int M, int K, int N, int dtype, bool pair, bool x_off, bool w_off) {
     FwdLayout l{};
-    if (M <= GEMM_ROWS_MAX) return l;      // that kernel reads the tensors where they are
-    const size_t e = esize(dtype), Kp = padded(K);
-    l.plan = gemm_plan(M, N, K, 1, 1, pair, dtype);
     l.move_x = moved(K, x_off, dtype);
     l.move_w = moved(K, w_off, dtype);
+    l.rows = gemm_rows_applies(M, N, K, pair, dtype, l.move_x || l.move_w);
+    if (l.rows) return l;      // that kernel reads the tensors where they are
+    const size_t e = esize(dtype), Kp = padded(K);
+    l.plan = gemm_plan(M, N, K, 1, 1, pair, dtype);
     Carver c(nullptr);
     if (l.move_x) { l.x = c.off; c.take(M * Kp * e); }
     if (l.move_w) {
@@ -67,6 +68,13 @@ FwdLayout fwd_layout(int M, int K, int N, int dtype, bool pair, bool x_off, bool
     if (l.plan.split > 1) c.take((size_t)l.plan.split * (pair ? 2 : 1) * M * (((size_t)N + 7) & ~(size_t)7) * sizeof(float));
     l.bytes = c.off;
     return l;
+}
+// what a query answers: with tensors off 16 bytes, which of them is not known (few rows of x or w then need no workspace, of the
+// others may)
+size_t fwd_bytes(int M, int K, int N, int dtype, bool pair, bool off) {
+    if (M == 0) return 0;
+    const size_t in = fwd_layout(M, K, N, dtype, pair, false, false).bytes, out = off ? fwd_layout(M, K, N, dtype, pair, true, true).bytes : 0;
+    return in > out ? in : out;
 }
 struct BwdLayout {
     size_t dz0, dz1, x, w0, w1, dbpart, part, bytes;
@@ -115,6 +123,13 @@ int product_fwd(const void* x, const void* const (&w)[2], const float* const (&b
     const long Kp = padded(K);
     GemmArgs g{};
     g.A[0] = x; g.B[0] = w[0]; g.B[1] = w[1]; g.lda = K; g.ldb = K;
+    g.M = M; g.N = N; g.K = K; g.segs = 1; g.batch = 1; g.pair = pair;
+    g.bias[0] = bias[0]; g.bias[1] = bias[1]; g.residual = residual; g.out[0] = out; g.z[0] = z[0]; g.z[1] = z[1];
+    g.act = act; g.dtype = dtype;
+    if (l.rows) {
+        TFLA_LAUNCH(K_GEMM, launch_gemm_rows(g, s));
+        return TFLA_OK;
+    }
     RepackArgs rp{};
     rp.cols = K; rp.ldd = Kp;
     if (l.move_x) {
@@ -127,13 +142,6 @@ int product_fwd(const void* x, const void* const (&w)[2], const float* const (&b
         g.B[0] = ws + l.w0; g.B[1] = pair ? ws + l.w1 : nullptr; g.ldb = Kp;
     }
     if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_repack(rp, s));
-    g.M = M; g.N = N; g.K = K; g.segs = 1; g.batch = 1; g.pair = pair;
-    g.bias[0] = bias[0]; g.bias[1] = bias[1]; g.residual = residual; g.out[0] = out; g.z[0] = z[0]; g.z[1] = z[1];
-    g.act = act; g.dtype = dtype;
-    if (M <= GEMM_ROWS_MAX) {
-        TFLA_LAUNCH(K_GEMM, launch_gemm_rows(g, s));
-        return TFLA_OK;
-    }
     g.split = l.plan.split; g.part = reinterpret_cast<float*>(ws + l.part); g.ld_part = (N + 7) & ~7;
     TFLA_LAUNCH(K_GEMM, launch_gemm(g, l.plan, false, false, pair ? EPI_GATED : EPI_LINEAR, s));
     return TFLA_OK;
@@ -249,7 +257,7 @@ int tfla_norm_bwd(const void* x, const void* dy, const float* rstd, const float*
 size_t tfla_linear_workspace_bytes(int direction, int M, int K, int N, int act, int dtype, int unaligned) {
     if (check_product(M, K, N, act, dtype) != TFLA_OK) return 0;
     const bool off = unaligned != 0;
-    if (direction == TFLA_FWD) return M == 0 ? 0 : fwd_layout(M, K, N, dtype, false, off, off).bytes;
+    if (direction == TFLA_FWD) return fwd_bytes(M, K, N, dtype, false, off);
     if (direction == TFLA_BWD) return bwd_layout(M, K, N, act, dtype, false, off, off, off).bytes;
     return 0;
 }
@@ -276,7 +284,7 @@ int tfla_linear_bwd(const void* x, const void* w, const void* dy, const void* z,
 size_t tfla_gated_workspace_bytes(int direction, int M, int K, int N, int act, int dtype, int unaligned) {
     if (check_product(M, K, N, act, dtype) != TFLA_OK) return 0;
     const bool off = unaligned != 0;
-    if (direction == TFLA_FWD) return M == 0 ? 0 : fwd_layout(M, K, N, dtype, true, off, off).bytes;
+    if (direction == TFLA_FWD) return fwd_bytes(M, K, N, dtype, true, off);
     if (direction == TFLA_BWD) return bwd_layout(M, K, N, act, dtype, true, off, off, off).bytes;
     return 0;
 }

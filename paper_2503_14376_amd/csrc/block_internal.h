@@ -48,8 +48,10 @@ struct GemmArgs {
 // how a product is cut (a rule on its sizes): used for the workspace and by the launcher
 struct GemmPlan { int bm, bn, split; double us; };      // us: time by the model
 GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype);
-// Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens)
+// Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens, where gemm_rows_applies;
+// copies: the tiles would need the weights copied)
 constexpr int GEMM_ROWS_MAX = 32;
+bool gemm_rows_applies(long M, int N, int K, int pair, int dtype, bool copies);
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s);
 

@@ -1,6 +1,8 @@
 """Host-side checks of the residual block's entry points: invalid arguments come back as the documented codes before anything is
 launched, the workspace queries agree with the calls, and the binding refuses tensors that are not what a call needs.  No compute
 call is made here: every call below fails its checks."""
+import itertools
+
 import pytest
 import torch
 
@@ -89,6 +91,23 @@ def test_a_workspace_is_asked_for_and_checked(lib, f, query):
     # tensors at odd addresses: more where the rows themselves are fine
     assert q(0, 300, 512, 256, 1, 1, 1) >= q(0, 300, 512, 256, 1, 1, 0) + 2 * 512 * (300 + 256)
     assert f(lib, M=300, K=512, N=256, x=P + 2, ws=P, wsb=q(0, 300, 512, 256, 1, 1, 0)) == WORKSPACE
+
+
+def test_few_tokens_through_many_weights(lib):
+    """up to 32 tokens are taken by either kernel: a query with an unaligned tensor covers the call whichever tensor that is"""
+    asked = 0
+    for q, f, names in ((lib.tfla_linear_workspace_bytes, lin_fwd, ("x", "w")), (lib.tfla_gated_workspace_bytes, gat_fwd, ("x", "wg"))):
+        for M, K, N in itertools.product((1, 4, 5, 8, 16, 17, 24, 32, 33), (512, 4096, 10944), (512, 1024, 4096)):
+            need, off = q(0, M, K, N, 1, 1, 0), q(0, M, K, N, 1, 1, 1)
+            assert off >= need and (need == 0 or M > 4)
+            if need > 0:
+                asked += M <= 32
+                assert f(lib, M=M, K=K, N=N, act=1) == WORKSPACE
+                assert f(lib, M=M, K=K, N=N, act=1, ws=P, wsb=need - 1) == WORKSPACE
+            if M > 32:                                     # (below, an unaligned operand needs none and the call would run)
+                for name in names:
+                    assert f(lib, M=M, K=K, N=N, act=1, ws=P, wsb=0, **{name: P + 2}) == WORKSPACE
+    assert asked > 0
 
 
 def test_backward_workspaces(lib):

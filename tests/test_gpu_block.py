@@ -296,6 +296,28 @@ def test_fp32_rows_that_end_inside_a_group(tfla, M, K, N):
     bu.within("dw", dw[:, :K - 1], *bu.product(dy.t(), x[:, :K - 1].t()))
 
 
+# Up to 32 tokens: the kernel for few rows or tiles, by the sizes; with x or the weights off 16 bytes, always the former
+FEW = [(M, 4096, 1030) for M in (5, 12, 16, 17, 24, 32, 33)] + [(8, 5000, 2056), (32, 5000, 2056), (32, 512, 1365), (24, 4096, 4096)]
+
+
+@pytest.mark.parametrize("M,K,N", FEW)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shift", [(0, 0, 0), (1, 0, 0), (0, 1, 0), (0, 0, 1)])
+def test_few_tokens(tfla, M, K, N, dtype, shift):
+    print("few", M, K, N, dtype, shift, flush=True)
+    gen = generator(M + N)
+    x, r = (fenced(normal(gen, M, c, dtype=dtype), s) for c, s in ((K, shift[0]), (N, shift[2])))
+    w, w2 = (fenced(normal(gen, N, K, std=K ** -0.5, dtype=dtype), shift[1]) for _ in range(2))
+    b = normal(gen, N, std=0.3)
+    z, y = bu.linear(x, w, b, r, "gelu")
+    f = tfla.linear_fwd(x, w, b, r, act=tfla.ACT_GELU, keep_pre=True)
+    bu.within("z", f["z"], *z)
+    bu.within("y", f["y"], *y)
+    f = tfla.gated_fwd(x, w, w2, b, act=tfla.ACT_SILU, keep_pre=True)
+    for name, v in zip("auh", bu.gated(x, w, w2, b, None, "silu")):
+        bu.within(name, f[name], *v)
+
+
 # ---- activations over their whole range ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
