@@ -196,7 +196,8 @@ int product_bwd(const void* x, const void* const (&w)[2], const void* dy, const 
         gw.split = l.plan_dw.split; gw.part = reinterpret_cast<float*>(ws + l.part); gw.ld_part = (K + 7) & ~7;
     }
     if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_repack(rp, s));
-    if (gx.M > 0 && gw.M > 0 && gemm_both_applies(l.plan_dx, l.plan_dw)) {
+    if (gx.M > 0 && gw.M > 0 && gemm_both_applies(l.plan_dx, l.plan_dw, M, K, N, pair, dtype)) {
+        gx.split = gw.split = 1;
         TFLA_LAUNCH(K_GEMM, launch_gemm_both(gx, gw, l.plan_dx, s));
     } else {
         if (gx.M > 0) TFLA_LAUNCH(K_GEMM, launch_gemm(gx, l.plan_dx, false, true, EPI_STORE, s));

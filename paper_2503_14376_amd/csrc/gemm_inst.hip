@@ -26,7 +26,12 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     // (one workgroup of the wide kernels fits a CU; the 256 of them take the tiles in turn)
     if (p.bn == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<256, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
     else if (p.bm == 256) hipLaunchKernelGGL((gemm_bf16_wide_kernel<128, ATR, BTR, PAIR, EPI>), dim3(n < 256 ? n : 256), dim3(256), 0, s, a, tms, tns);
-    else if (p.bm == 128) hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+    // 128 x 128: two workgroups on a CU, or one with eight wavefronts and three steps under way instead of one (1024 x 4096 x 4096
+    // 64 us with four wavefronts and one step, 46 with three, 44.5 with eight as well)
+    else if (p.bm == 128) {
+        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        else hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 4, 2, 4, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
+    }
     // 64 rows: two groups of wavefronts where no CU gets a second workgroup
     else if constexpr (PAIR) {
         if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 1, ATR, BTR, true, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
@@ -71,13 +76,8 @@ template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, co
     };
     cut(bm);
 #if TFLA_GEMM == 3
-    const long longest = up((int)(g.x0 ? w.K : x.K), 64) * (g.x0 ? w.segs : x.segs);
-    const long steps = (long)g.nx * up(x.K, 64) * x.segs + (long)(all - g.nx) * up(w.K, 64) * w.segs;
-    // 64 x 128 tiles bring three quarters of the operands' bytes into LDS, which is what bounds these launches, but have half the
-    // workgroups: taken where the longest of them is at most half of an even share of the steps (2952 x 896 x 3088 65.9 us
-    // against 82.9, 944 x 1624 x 1360 25.2 against 30.3; with a longest of a whole share 512 x 1024 x 1365, a pair, 26.3 against
-    // 22.3).  Up to a workgroup per CU two groups of wavefronts share a tile's steps.
-    if (all > 512 && 2 * longest * 256 <= steps) {
+    // (up to a workgroup per CU two groups of wavefronts share a tile's steps)
+    if (both_steps(x.M, x.N, x.K, x.segs == 2).wide()) {
         cut(128);
         hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 128, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
     } else if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);

@@ -190,10 +190,12 @@ def test_gated(tfla, i, dtype, shift):
 # ---- every tile that the sizes choose between, whole and with the contraction in parts: one product of M x N results over K
 # at a time, forward, input gradient and weight gradient -------------------------------------------------------------
 PRODUCTS = [(BF16, 520, 6001, 41), (BF16, 72, 8200, 3505), (BF16, 3500, 8200, 41), (BF16, 200, 6001, 8200), (BF16, 5000, 8200, 333),
-            (BF16, 776, 5001, 4101), (F32, 1365, 8200, 73), (F32, 200, 3501, 2500), (F32, 1000, 1544, 72), (F32, 40, 1365, 3000)]
+            (BF16, 776, 5001, 4101), (F32, 1365, 8200, 73), (F32, 200, 3501, 2500), (F32, 1000, 1544, 72), (F32, 40, 1365, 3000),
+            (BF16, 1000, 2050, 1100), (BF16, 700, 1500, 9000), (BF16, 300, 1000, 9000), (BF16, 700, 2100, 3000)]
 PAIRS = [(BF16, 3500, 4100, 41), (BF16, 3500, 4101, 200), (BF16, 6000, 73, 8200), (BF16, 2500, 8201, 333), (BF16, 8200, 72, 8200),
          (BF16, 72, 3001, 5000), (BF16, 136, 6000, 5000), (BF16, 3001, 1365, 520), (F32, 2056, 2501, 72), (F32, 2056, 40, 5000),
-         (F32, 40, 1365, 3000), (F32, 200, 3500, 1544), (F32, 201, 2500, 4100)]
+         (F32, 40, 1365, 3000), (F32, 200, 3500, 1544), (F32, 201, 2500, 4100),
+         (BF16, 250, 1500, 9000), (BF16, 500, 1365, 2000)]
 
 
 @pytest.mark.parametrize("dtype,M,N,K", PRODUCTS)
