@@ -143,8 +143,8 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
 }
 
 // How a product is cut: the tile and the number of parts with the shortest time by a model of the kernels, measured on products
-// of 40 to 8192 rows and columns (forward, both backward layouts; of 80 random ones 2.5 % above the best of all choices on average,
-// 20 % at most).  In us, with w
+// of 40 to 8192 rows and columns (forward, both backward layouts; of 160 random ones 2 % above the best of all choices on average,
+// 23 % at most).  In us, with w
 // workgroups in all, n = ceil(w / 256) of them per CU one after another or side by side, and t steps each:
 //   bf16   256 x 256   8 + n (t (1.0 + 0.45 min(1, w / 256)) + 4)        (the power that all CUs draw lowers the clock)
 //          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
