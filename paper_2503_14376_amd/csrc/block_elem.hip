@@ -148,7 +148,7 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
 // workgroups in all, n = ceil(w / 256) of them per CU one after another or side by side, and t steps each:
 //   bf16   256 x 256   8 + n (t (1.0 + 0.45 min(1, w / 256)) + 4)        (the power that all CUs draw lowers the clock)
 //          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
-//          128 x 128   5 + t (0.42 + 0.15 w / 256) up to 256 workgroups, 6 + 0.48 t n + 1.5 max(0, n - 2) above
+//          128 x 128   5 + t (0.42 + 0.15 w / 256) up to 256 workgroups, 6 + 0.49 t n + 1.5 max(0, n - 2) above
 //          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.34 t n)
 //   fp32   128 x 128   7 + max(2.3, 2.1 n) t     (steps of 32)
 //          64 x 64     5.5 + max(0.68, 0.57 n) t (pairs: 64 x 128, twice that)
@@ -174,7 +174,7 @@ GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtyp
             if (!b16) us = bm == 128 ? 7 + (n < 2 ? 2.3 : 2.1 * n) * t : (bm == 64 ? 5.5 + (n < 2 ? 0.68 : 0.57 * n) * t * (pair ? 2 : 1) : 4.8 + (n < 2 ? 0.4 : 0.34 * n) * t * (pair ? 1.9 : 1));
             else if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
             else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
-            else if (bm == 128) us = n < 2 ? 5 + t * (0.42 + 0.15 * part) : 6 + 0.48 * t * n + 1.5 * more;
+            else if (bm == 128) us = n < 2 ? 5 + t * (0.42 + 0.15 * part) : 6 + 0.49 * t * n + 1.5 * more;
             else us = 4.8 + (pair ? 0.34 : 0.177) * t * n + 0.9 * more;
             if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
             if (best.bm == 0 || us < best.us) best = {bm, bn, split, us};
