@@ -309,8 +309,8 @@ TFLA_API int tfla_norm_bwd(const void* x, const void* dy, const float* rstd, con
 
 /*
  * Linear projection.  z = x W^T + bias;  y = act(z) + residual.  bias (N), residual (M, N) and z (M, N, stored for the
- * backward call of an activation) may be NULL.  act: silu z sigma(z); gelu z Phi(z) (the error function, no approximation);
- * relu max(z, 0).
+ * backward call of an activation) may be NULL.  act: silu z sigma(z); gelu z Phi(z), Phi by the error function (not the tanh
+ * form; for bf16 tensors to 2^-13 of its value and 1.2e-7 absolute); relu max(z, 0).
  * Backward: dz = dy (.) act'(z) (act'(0) = 0 for relu);  dx = dz W;  dw = dz^T x;  db = sum_m dz.  z: as the forward call
  * stored it, NULL for TFLA_ACT_NONE.  dx, dw, db: each may be NULL = not wanted.
  */

@@ -9,9 +9,12 @@ namespace tfla {
 enum { ACT_NONE = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
 
 // act(z) and act'(z).  silu: z sigma(z), sigma (1 + z (1 - sigma)); gelu: z Phi(z), Phi + z phi; relu: (z > 0).
-// For bf16 tensors sigma and Phi come from the hardware's exponential and reciprocal (errors of some 2^-22, where the result is
-// rounded to 2^-8), for fp32 from the library's functions (erfc, which keeps Phi's digits where it is small).  Phi(-|z|) = 1/2 erfc(|z| / sqrt 2) by the approximation 7.1.26 of
-// Abramowitz and Stegun, Handbook of Mathematical Functions (1.5e-7 absolute), a polynomial in 1 / (1 + p x) times exp(-x^2).
+// For bf16 tensors sigma comes from the hardware's exponential and reciprocal (2^-16 of its value at most, most of it the rounding of
+// the exponent's argument; the result is rounded to 2^-8).  Phi(-|z|) = exp(-z^2 / 2) h(|z|), h falling from 1/2 as 1 / (|z| sqrt(2 pi)), so
+// that a fit of h keeps Phi's digits also where it is small: h = t P(t), t = 1 / (1 + c |z|), c and the six coefficients fitted over |z| <= 14.5 (beyond,
+// exp(-z^2 / 2) leaves fp32) to the smallest error against min(2^-12 of h, 2.5e-7 / Phi(-|z|)): 2^-13 of Phi(-|z|) and 1.2e-7 absolute.  (Formula 7.1.26 of
+// Abramowitz and Stegun, one term shorter, is bounded absolutely only: 1 % of Phi at z = -8, 3.7 % at -13.)
+// For fp32 both come from the library's functions (erfc, which keeps Phi's digits where it is small).
 template <typename DT> __device__ __forceinline__ float sigmoid(float z);
 template <> __device__ __forceinline__ float sigmoid<float>(float z) {
     const float e = expf(-fabsf(z));
@@ -28,12 +31,13 @@ template <> __device__ __forceinline__ float normal_cdf<float>(float z, float& e
 }
 template <> __device__ __forceinline__ float normal_cdf<bf16_t>(float z, float& e) {
     e = fast_exp2(-0.72134752f * z * z);
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-    float p = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-    p = __builtin_fmaf(t, p, 1.421413741f);
-    p = __builtin_fmaf(t, p, -0.284496736f);
-    p = __builtin_fmaf(t, p, 0.254829592f);
-    const float h = 0.5f * t * p * e;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.41907025f, fabsf(z), 1.0f));
+    float p = __builtin_fmaf(t, 0.05759048f, -0.2349666f);
+    p = __builtin_fmaf(t, p, 0.26108308f);
+    p = __builtin_fmaf(t, p, 0.07074811f);
+    p = __builtin_fmaf(t, p, 0.17915755f);
+    p = __builtin_fmaf(t, p, 0.16638749f);
+    const float h = t * p * e;
     return z < 0.0f ? h : 1.0f - h;
 }
 template <typename DT> __device__ __forceinline__ float act_value(float z, int act) {
