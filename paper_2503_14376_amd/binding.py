@@ -505,16 +505,39 @@ def _rows(x, name, b16, f32):
     return BF16 if t == b16 else F32, shape[0], shape[1]
 
 
+# Memory and streams.  A call on a stream that is not the current one takes new memory from that stream's own pool, where a block that was
+# freed before has had its last use in the stream's order; the current stream, on which the caller made the call and will drop its tensors, is
+# recorded on it.  (From the current stream's pool the block of a tensor that was dropped a moment ago could come back while work queued there
+# still reads it.)  The call's other tensors belong to other streams: they are recorded on this one, so that none is handed out again before
+# the call has run.
+def _new(shape, dtype, like, stream):
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+    t.record_stream(torch.cuda.current_stream(like.device))
+    return t
+
+
+def _on(stream, *inputs):
+    """the handle of an explicit stream, with the call's inputs recorded on it"""
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
 def _out(o, name, shape, dtype, like, stream):
     """address of o[name], checked, or of a new tensor there"""
     t = o.get(name)
     if t is None:
-        import torch
-        t = o[name] = torch.empty(shape, dtype=dtype, device=like.device)
-        if stream is not None:
-            t.record_stream(stream)
-    elif t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        t = o[name] = _new(shape, dtype, like, stream)
+        return t.data_ptr()
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
         _want(t, dtype, shape, name)
+    if stream is not None:
+        t.record_stream(stream)
     return t.data_ptr()
 
 
@@ -524,9 +547,7 @@ def _scratch(o, workspace, need, like, stream):
         workspace = o.get("workspace")
         if need and (workspace is None or workspace.numel() < need):
             import torch
-            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _new((need,), torch.uint8, like, stream)
     o["workspace"] = workspace
     return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
@@ -541,7 +562,7 @@ def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream
     y, rstd = _out(o, "y", (M, D), x.dtype, x, stream), _out(o, "rstd", (M,), f32, x, stream)
     mean = _out(o, "mean", (M,), f32, x, stream) if norm_kind == NORM_LAYER else None
     rc = (_lib or load_library()).tfla_norm_fwd(x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean,
-                                      raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                      raw_stream(x.get_device()) if stream is None else _on(stream, x, gamma, beta))
     if rc != 0:
         raise TflaError(rc, "tfla_norm_fwd")
     return o
@@ -562,7 +583,7 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
     need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
     ws, wsb = _scratch(o, workspace, need, x, stream)
     rc = (_lib or load_library()).tfla_norm_bwd(x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype,
-                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, dy, rstd, mean, gamma, d_residual))
     if rc != 0:
         raise TflaError(rc, "tfla_norm_bwd")
     return o
@@ -582,7 +603,7 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
     need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, x, stream)
     rc = (_lib or load_library()).tfla_linear_fwd(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb,
-                                        raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                        raw_stream(x.get_device()) if stream is None else _on(stream, x, w, bias, residual))
     if rc != 0:
         raise TflaError(rc, "tfla_linear_fwd")
     return o
@@ -603,7 +624,7 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
     need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr() | dy.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, x, stream)
     rc = (_lib or load_library()).tfla_linear_bwd(x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb,
-                                        raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                        raw_stream(x.get_device()) if stream is None else _on(stream, x, w, dy, z))
     if rc != 0:
         raise TflaError(rc, "tfla_linear_bwd")
     return o
@@ -625,7 +646,7 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
     need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, x, stream)
     rc = (_lib or load_library()).tfla_gated_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype,
-                                       h, a, u, ws, wsb, raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                       h, a, u, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, b_gate, b_up))
     if rc != 0:
         raise TflaError(rc, "tfla_gated_fwd")
     return o
@@ -649,7 +670,7 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
     need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | dh.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, x, stream)
     rc = (_lib or load_library()).tfla_gated_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N,
-                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, raw_stream(x.get_device()) if stream is None else stream.cuda_stream)
+                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, a, u, dh))
     if rc != 0:
         raise TflaError(rc, "tfla_gated_bwd")
     return o

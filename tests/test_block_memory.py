@@ -1,0 +1,169 @@
+"""Which memory the binding of the residual block's operators hands to a call: pools, streams and devices, by stand-ins for device tensors,
+streams and the library's launching calls (its workspace queries are the real ones).  Nothing here needs a device."""
+import contextlib
+import os
+
+import pytest
+import torch
+
+import paper_2503_14376_amd as tfla
+from paper_2503_14376_amd import binding
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+class Stream:
+    def __init__(self, handle, device=0):
+        self.cuda_stream, self.device = handle, torch.device("cuda", device)
+
+
+class Tensor:
+    """what the binding asks of a device tensor; `pool`: the stream whose memory it is, `seen`: the streams recorded on it"""
+    count = 0
+
+    def __init__(self, shape, dtype=BF16, device=0, pool=None):
+        self.shape, self.dtype, self.device, self.pool, self.seen = tuple(shape), dtype, torch.device("cuda", device), pool, set()
+        Tensor.count += 1
+        self.address = Tensor.count << 40
+        self.is_cuda = True
+
+    def get_device(self):
+        return self.device.index
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.address
+
+    def numel(self):
+        n = 1
+        for d in self.shape:
+            n *= d
+        return n
+
+    def element_size(self):
+        return torch.empty(0, dtype=self.dtype).element_size() if self.dtype != torch.uint8 else 1
+
+    def record_stream(self, stream):
+        self.seen.add(stream)
+
+
+class Machine:
+    """the current stream and device, and what was launched: (name, arguments, device that was current)"""
+
+    def __init__(self, monkeypatch):
+        self.device, self.streams, self.calls = 0, [Stream(0, 0), Stream(0, 1)], []
+        empty = torch.empty
+        real = binding.load_library()
+
+        def new(shape, dtype=None, device=None):
+            if device is None or torch.device(device).type != "cuda":
+                return empty(shape, dtype=dtype)
+            d = torch.device(device).index
+            return Tensor((shape,) if isinstance(shape, int) else shape, dtype, d, self.streams[d])
+
+        @contextlib.contextmanager
+        def on_stream(s):
+            d, before, at = s.device.index, self.streams[s.device.index], self.device
+            self.streams[d], self.device = s, d
+            yield
+            self.streams[d], self.device = before, at
+
+        @contextlib.contextmanager
+        def on_device(d):
+            before, self.device = self.device, d if isinstance(d, int) else d.index
+            yield
+            self.device = before
+
+        class Library:
+            def __getattr__(lib, name):
+                if name.endswith("_bytes"):
+                    return getattr(real, name)
+
+                def launch(*args):
+                    self.calls.append((name, args, self.device))
+                    return 0
+                return launch
+
+        def index(device):
+            return self.device if device is None else device if isinstance(device, int) else torch.device(device).index
+
+        monkeypatch.setattr(torch, "empty", new)
+        monkeypatch.setattr(torch.cuda, "stream", on_stream)
+        monkeypatch.setattr(torch.cuda, "device", on_device)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.streams[index(device)])
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: self.device)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: self.streams[d].cuda_stream, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: self.device, raising=False)
+        monkeypatch.setattr(binding, "_torch_names", None)
+        monkeypatch.setattr(binding, "_lib", Library())
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    if not os.path.exists(binding.lib_path()):
+        from paper_2503_14376_amd import build
+        build.build(verbose=False)
+    yield Machine(monkeypatch)
+
+
+def calls(M=300, K=333, N=200, dtype=BF16, device=0):
+    """every operator and direction with tensors of its own: name -> (call, its input tensors)"""
+    def t(*shape, d=dtype):
+        return Tensor(shape, d, device)
+    x, w, w2, y, dy, z = t(M, K), t(N, K), t(N, K), t(M, N), t(M, N), t(M, N)
+    g, b, n, stat, mean = t(K, d=F32), t(K, d=F32), t(N, d=F32), t(M, d=F32), t(M, d=F32)
+    dx, res = t(M, K), t(M, K)
+    return {
+        "norm_fwd": (lambda **k: tfla.norm_fwd(x, g, b, norm_kind=tfla.NORM_LAYER, **k), [x, g, b]),
+        "norm_bwd": (lambda **k: tfla.norm_bwd(x, dx, stat, mean, g, res, norm_kind=tfla.NORM_LAYER, want_dbeta=True, **k),
+                     [x, dx, stat, mean, g, res]),
+        "linear_fwd": (lambda **k: tfla.linear_fwd(x, w, n, y, act=tfla.ACT_SILU, keep_pre=True, **k), [x, w, n, y]),
+        "linear_bwd": (lambda **k: tfla.linear_bwd(x, w, dy, z, act=tfla.ACT_SILU, want_db=True, **k), [x, w, dy, z]),
+        "gated_fwd": (lambda **k: tfla.gated_fwd(x, w, w2, n, n, keep_pre=True, **k), [x, w, w2, n]),
+        "gated_bwd": (lambda **k: tfla.gated_bwd(x, w, w2, y, z, dy, want_db=True, **k), [x, w, w2, y, z, dy])}
+
+
+NAMES = ("norm_fwd", "norm_bwd", "linear_fwd", "linear_bwd", "gated_fwd", "gated_bwd")
+
+
+def tensors(o):
+    return {k: v for k, v in o.items() if v is not None}
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_call_on_another_stream_takes_memory_of_that_stream(machine, name):
+    """new outputs and workspaces come from the pool of the stream that writes them, and the current stream may drop them at any time"""
+    side = Stream(77)
+    call, inputs = calls()[name]
+    o = call(stream=side)
+    assert machine.calls[-1][1][-1] == 77
+    assert len(tensors(o)) >= 2
+    for k, t in tensors(o).items():
+        assert t.pool is side, k
+        assert machine.streams[0] in t.seen, k
+    for t in inputs:
+        assert side in t.seen
+    assert machine.streams[0].cuda_stream == 0
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_call_on_the_current_stream_takes_its_memory(machine, name):
+    call, inputs = calls()[name]
+    o = call()
+    assert machine.calls[-1][1][-1] == 0
+    for t in list(tensors(o).values()):
+        assert t.pool is machine.streams[0] and not t.seen
+    assert not any(t.seen for t in inputs)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_outputs_used_on_another_stream_are_recorded_there(machine, name):
+    side = Stream(78)
+    call, _ = calls()[name]
+    o = call()
+    call(stream=side, out=o)
+    for k, t in tensors(o).items():
+        if k != "workspace":
+            assert side in t.seen, k
