@@ -465,6 +465,8 @@ def transfer_gain(h, v, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None):
 
 
 # ---- the rest of a residual block: norm over the model's columns, linear projection, gated projection pair --------------
+# `out` belongs to one sequence of calls: it holds the outputs and the workspace of the last, which the next writes again.  Calls that share
+# it have to be ordered when they run on different streams, and a graph that was captured with it needs it kept.
 # These calls are the shortest of all while generating, so they do little per argument: outputs and the workspace that `out`
 # holds from the call before are taken after a check of type and shape, torch's names are looked up once, and the current
 # stream is asked for with the tensor's own device (one token, norm_fwd in a loop: 7.0 us per call without these, 6.2 with).
@@ -541,15 +543,33 @@ def _out(o, name, shape, dtype, like, stream):
     return t.data_ptr()
 
 
-def _scratch(o, workspace, need, like, stream):
-    """address and size of the workspace: the caller's, the one that the last call with this `out` left, or a new one"""
-    if workspace is None:
-        workspace = o.get("workspace")
-        if need and (workspace is None or workspace.numel() < need):
-            import torch
-            workspace = _new((need,), torch.uint8, like, stream)
-    o["workspace"] = workspace
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+def _bytes(workspace):
+    return workspace.numel() * workspace.element_size()
+
+
+def _scratch(o, workspace, need, like, stream, handle):
+    """address and size of the workspace: the caller's, which `out` does not keep, or the one in `out` that earlier calls left, or a new one
+    there.  The kept one remembers the stream it was last used on and is recorded on another that uses it.  One that has become too small
+    stays alive beside its successor: a captured graph may hold its address (a change of sizes with the same `out` is rare)."""
+    if workspace is not None:
+        if stream is not None:
+            workspace.record_stream(stream)
+        o.setdefault("workspace", None)
+        return workspace.data_ptr(), _bytes(workspace)
+    kept = o.get("workspace")
+    if need and (kept is None or _bytes(kept) < need):
+        import torch
+        new = o["workspace"] = _new((need,), torch.uint8, like, stream)
+        new.tfla_before, new.tfla_stream = kept, handle
+        return new.data_ptr(), need
+    if kept is None:
+        o["workspace"] = None
+        return None, 0
+    if getattr(kept, "tfla_stream", None) != handle:
+        import torch
+        kept.record_stream(torch.cuda.current_stream(like.device) if stream is None else stream)
+        kept.tfla_stream = handle
+    return kept.data_ptr(), _bytes(kept)
 
 
 def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None, out: Optional[Dict] = None) -> Dict:
@@ -581,9 +601,10 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
     dgamma = _out(o, "dgamma", (D,), f32, x, stream) if want_dgamma else None
     dbeta = _out(o, "dbeta", (D,), f32, x, stream) if want_dbeta else None
     need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
-    ws, wsb = _scratch(o, workspace, need, x, stream)
+    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, dy, rstd, mean, gamma, d_residual)
+    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
     rc = (_lib or load_library()).tfla_norm_bwd(x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype,
-                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, dy, rstd, mean, gamma, d_residual))
+                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_norm_bwd")
     return o
@@ -601,9 +622,10 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
     y = _out(o, "y", (M, N), x.dtype, x, stream)
     z = _out(o, "z", (M, N), x.dtype, x, stream) if keep_pre else None
     need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, x, stream)
+    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w, bias, residual)
+    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
     rc = (_lib or load_library()).tfla_linear_fwd(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb,
-                                        raw_stream(x.get_device()) if stream is None else _on(stream, x, w, bias, residual))
+                                        handle)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_fwd")
     return o
@@ -622,9 +644,10 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
     dw = _out(o, "dw", (N, K), x.dtype, x, stream) if want_dw else None
     db = _out(o, "db", (N,), f32, x, stream) if want_db else None
     need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr() | dy.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, x, stream)
+    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w, dy, z)
+    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
     rc = (_lib or load_library()).tfla_linear_bwd(x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb,
-                                        raw_stream(x.get_device()) if stream is None else _on(stream, x, w, dy, z))
+                                        handle)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_bwd")
     return o
@@ -644,9 +667,10 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
     a = _out(o, "a", (M, N), x.dtype, x, stream) if keep_pre else None
     u = _out(o, "u", (M, N), x.dtype, x, stream) if keep_pre else None
     need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, x, stream)
+    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, b_gate, b_up)
+    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
     rc = (_lib or load_library()).tfla_gated_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype,
-                                       h, a, u, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, b_gate, b_up))
+                                       h, a, u, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_fwd")
     return o
@@ -668,9 +692,10 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
     dbg = _out(o, "db_gate", (N,), f32, x, stream) if want_db else None
     dbu = _out(o, "db_up", (N,), f32, x, stream) if want_db else None
     need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | dh.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, x, stream)
+    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, a, u, dh)
+    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
     rc = (_lib or load_library()).tfla_gated_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N,
-                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, a, u, dh))
+                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_bwd")
     return o

@@ -167,3 +167,70 @@ def test_outputs_used_on_another_stream_are_recorded_there(machine, name):
     for k, t in tensors(o).items():
         if k != "workspace":
             assert side in t.seen, k
+
+
+# ---- the workspace that `out` keeps ---------------------------------------------------------------------------------
+WITH_WORKSPACE = ("norm_bwd", "linear_fwd", "linear_bwd", "gated_fwd", "gated_bwd")
+
+
+def workspace_of(machine, name):
+    """address and size that the last call was given"""
+    where = {"norm_bwd": 13, "linear_fwd": 11, "linear_bwd": 12, "gated_fwd": 13, "gated_bwd": 16}[name]
+    n, args, _ = machine.calls[-1]
+    assert n == "tfla_" + name
+    return args[where], args[where + 1]
+
+
+@pytest.mark.parametrize("name", WITH_WORKSPACE)
+def test_the_kept_workspace_is_recorded_on_every_stream_that_uses_it(machine, name):
+    side = Stream(81)
+    call, _ = calls()[name]
+    o = call()
+    ws = o["workspace"]
+    assert workspace_of(machine, name) == (ws.address, ws.numel())
+    call(stream=side, out=o)
+    assert o["workspace"] is ws and side in ws.seen
+    # and back: a later use on the current stream, which is another one now
+    machine.streams[0] = other = Stream(82)
+    call(out=o)
+    assert other in ws.seen
+    # no second look at a stream it knows
+    ws.seen.clear()
+    call(out=o)
+    assert not ws.seen
+
+
+@pytest.mark.parametrize("name", WITH_WORKSPACE)
+def test_a_workspace_that_became_too_small_stays_alive(machine, name):
+    """a graph that was captured with it holds its address for as long as the caller keeps `out`"""
+    import gc
+    import weakref
+    call, _ = calls()[name]
+    o = call()
+    ws = weakref.ref(o["workspace"])
+    keep = {"workspace": o.pop("workspace")}
+    del o
+    big = calls(M=4000, K=2001, N=1203)[name][0](out=keep)
+    assert big["workspace"].numel() > ws().numel()
+    assert workspace_of(machine, name)[0] == big["workspace"].address
+    del big
+    gc.collect()
+    assert ws() is not None
+    keep.clear()
+    gc.collect()
+    assert ws() is None
+
+
+@pytest.mark.parametrize("name", WITH_WORKSPACE)
+def test_a_callers_workspace_is_not_kept(machine, name):
+    side = Stream(83)
+    call, _ = calls()[name]
+    mine = Tensor((1 << 24,), torch.uint8, pool=machine.streams[0])
+    o = call(workspace=mine, stream=side)
+    assert workspace_of(machine, name) == (mine.address, 1 << 24) and side in mine.seen
+    assert o["workspace"] is None
+    call(out=o)
+    assert o["workspace"] is not mine and workspace_of(machine, name)[0] == o["workspace"].address
+    # its size counts in bytes
+    call(workspace=Tensor((1 << 20,), F32))
+    assert workspace_of(machine, name)[1] == 4 << 20
