@@ -469,7 +469,9 @@ def transfer_gain(h, v, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None):
 # it have to be ordered when they run on different streams, and a graph that was captured with it needs it kept.
 # These calls are the shortest of all while generating, so they do little per argument: outputs and the workspace that `out`
 # holds from the call before are taken after a check of type and shape, torch's names are looked up once, and the current
-# stream is asked for with the tensor's own device (one token, norm_fwd in a loop: 7.0 us per call without these, 6.2 with).
+# stream is asked for without an object around it (one token, norm_fwd in a loop: 7.0 us per call without these, 6.2 with).
+# Every tensor of a call is on the device of its first, whose current stream takes the launch, and that device is made current for it: the
+# handle of a default stream is 0 on every device and means the current one's.
 _torch_names = None
 
 
@@ -480,7 +482,7 @@ def _torch_types():
     if raw is None:
         def raw(device):
             return torch.cuda.current_stream(device).cuda_stream
-    _torch_names = (torch.bfloat16, torch.float32, raw)
+    _torch_names = (torch.bfloat16, torch.float32, raw, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
     return _torch_names
 
 
@@ -497,14 +499,29 @@ def gated_workspace_bytes(direction, M, K, N, act, dtype, unaligned=False) -> in
 
 
 def _rows(x, name, b16, f32):
-    """dtype code and (M, columns) of a dense matrix of rows"""
+    """dtype code, (M, columns) and device of a dense matrix of rows"""
     t = x.dtype
     shape = x.shape
+    dev = x.get_device()
     if t != b16 and t != f32:
         raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, t))
-    if len(shape) != 2 or not x.is_cuda or not x.is_contiguous():
+    if len(shape) != 2 or dev < 0 or not x.is_contiguous():
         raise ValueError("%s must be a contiguous device tensor of two dimensions" % name)
-    return BF16 if t == b16 else F32, shape[0], shape[1]
+    return BF16 if t == b16 else F32, shape[0], shape[1], dev
+
+
+def _like(t, dtype, shape, name, dev):
+    """shape: a tuple; None passes"""
+    if t is not None and (t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous tensor of dtype %s and shape %s on cuda:%d (got %s %s on %s)"
+                         % (name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.device))
+
+
+def _elsewhere(dev, call, args):
+    """the launching call with the tensors' device current, which another one is"""
+    import torch
+    with torch.cuda.device(dev):
+        return call(*args)
 
 
 # Memory and streams.  A call on a stream that is not the current one takes new memory from that stream's own pool, where a block that was
@@ -512,32 +529,34 @@ def _rows(x, name, b16, f32):
 # recorded on it.  (From the current stream's pool the block of a tensor that was dropped a moment ago could come back while work queued there
 # still reads it.)  The call's other tensors belong to other streams: they are recorded on this one, so that none is handed out again before
 # the call has run.
-def _new(shape, dtype, like, stream):
+def _new(shape, dtype, dev, stream):
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
     with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=like.device)
-    t.record_stream(torch.cuda.current_stream(like.device))
+        t = torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
+    t.record_stream(torch.cuda.current_stream(dev))
     return t
 
 
-def _on(stream, *inputs):
+def _on(stream, dev, *inputs):
     """the handle of an explicit stream, with the call's inputs recorded on it"""
+    if stream.device.index != dev:
+        raise ValueError("the stream is one of %s, the tensors are on cuda:%d" % (stream.device, dev))
     for t in inputs:
         if t is not None:
             t.record_stream(stream)
     return stream.cuda_stream
 
 
-def _out(o, name, shape, dtype, like, stream):
+def _out(o, name, shape, dtype, dev, stream):
     """address of o[name], checked, or of a new tensor there"""
     t = o.get(name)
     if t is None:
-        t = o[name] = _new(shape, dtype, like, stream)
+        t = o[name] = _new(shape, dtype, dev, stream)
         return t.data_ptr()
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        _want(t, dtype, shape, name)
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _like(t, dtype, shape, name, dev)
     if stream is not None:
         t.record_stream(stream)
     return t.data_ptr()
@@ -547,7 +566,7 @@ def _bytes(workspace):
     return workspace.numel() * workspace.element_size()
 
 
-def _scratch(o, workspace, need, like, stream, handle):
+def _scratch(o, workspace, need, dev, stream, handle):
     """address and size of the workspace: the caller's, which `out` does not keep, or the one in `out` that earlier calls left, or a new one
     there.  The kept one remembers the stream it was last used on and is recorded on another that uses it.  One that has become too small
     stays alive beside its successor: a captured graph may hold its address (a change of sizes with the same `out` is rare)."""
@@ -559,7 +578,7 @@ def _scratch(o, workspace, need, like, stream, handle):
     kept = o.get("workspace")
     if need and (kept is None or _bytes(kept) < need):
         import torch
-        new = o["workspace"] = _new((need,), torch.uint8, like, stream)
+        new = o["workspace"] = _new((need,), torch.uint8, dev, stream)
         new.tfla_before, new.tfla_stream = kept, handle
         return new.data_ptr(), need
     if kept is None:
@@ -567,7 +586,7 @@ def _scratch(o, workspace, need, like, stream, handle):
         return None, 0
     if getattr(kept, "tfla_stream", None) != handle:
         import torch
-        kept.record_stream(torch.cuda.current_stream(like.device) if stream is None else stream)
+        kept.record_stream(torch.cuda.current_stream(dev) if stream is None else stream)
         kept.tfla_stream = handle
     return kept.data_ptr(), _bytes(kept)
 
@@ -575,14 +594,16 @@ def _scratch(o, workspace, need, like, stream, handle):
 def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None, out: Optional[Dict] = None) -> Dict:
     """tfla_norm_fwd on torch device tensors.  x: (M, D) in bf16 or fp32; gamma, beta: (D,) fp32 or None.  Returns y and the row
     statistics rstd and (LayerNorm) mean, which norm_bwd needs."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, D = _rows(x, "x", b16, f32)
-    _want(gamma, f32, (D,), "gamma"); _want(beta, f32, (D,), "beta")
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, D, dev = _rows(x, "x", b16, f32)
+    _like(gamma, f32, (D,), "gamma", dev); _like(beta, f32, (D,), "beta", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, gamma, beta)
     o = out if out is not None else {}
-    y, rstd = _out(o, "y", (M, D), x.dtype, x, stream), _out(o, "rstd", (M,), f32, x, stream)
-    mean = _out(o, "mean", (M,), f32, x, stream) if norm_kind == NORM_LAYER else None
-    rc = (_lib or load_library()).tfla_norm_fwd(x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean,
-                                      raw_stream(x.get_device()) if stream is None else _on(stream, x, gamma, beta))
+    y, rstd = _out(o, "y", (M, D), x.dtype, dev, stream), _out(o, "rstd", (M,), f32, dev, stream)
+    mean = _out(o, "mean", (M,), f32, dev, stream) if norm_kind == NORM_LAYER else None
+    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean, handle)
+    call = (_lib or load_library()).tfla_norm_fwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_norm_fwd")
     return o
@@ -592,19 +613,21 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
              workspace=None, stream=None, out: Optional[Dict] = None) -> Dict:
     """tfla_norm_bwd on torch device tensors.  rstd, mean: as norm_fwd returned them; d_residual: (M, D), added to dx, or None.
     Returns dx, dgamma, dbeta (the last two where wanted)."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, D = _rows(x, "x", b16, f32)
-    _want(dy, x.dtype, (M, D), "dy"); _want(d_residual, x.dtype, (M, D), "d_residual"); _want(gamma, f32, (D,), "gamma")
-    _want(rstd, f32, (M,), "rstd"); _want(mean, f32, (M,), "mean")
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, D, dev = _rows(x, "x", b16, f32)
+    _like(dy, x.dtype, (M, D), "dy", dev); _like(d_residual, x.dtype, (M, D), "d_residual", dev); _like(gamma, f32, (D,), "gamma", dev)
+    _like(rstd, f32, (M,), "rstd", dev); _like(mean, f32, (M,), "mean", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, dy, rstd, mean, gamma, d_residual)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, D), x.dtype, x, stream)
-    dgamma = _out(o, "dgamma", (D,), f32, x, stream) if want_dgamma else None
-    dbeta = _out(o, "dbeta", (D,), f32, x, stream) if want_dbeta else None
+    dx = _out(o, "dx", (M, D), x.dtype, dev, stream)
+    dgamma = _out(o, "dgamma", (D,), f32, dev, stream) if want_dgamma else None
+    dbeta = _out(o, "dbeta", (D,), f32, dev, stream) if want_dbeta else None
     need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
-    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, dy, rstd, mean, gamma, d_residual)
-    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
-    rc = (_lib or load_library()).tfla_norm_bwd(x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype,
-                                      int(norm_kind), dx, dgamma, dbeta, ws, wsb, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    args = (x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype, int(norm_kind), dx, dgamma,
+            dbeta, ws, wsb, handle)
+    call = (_lib or load_library()).tfla_norm_bwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_norm_bwd")
     return o
@@ -614,18 +637,19 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
                out: Optional[Dict] = None) -> Dict:
     """tfla_linear_fwd on torch device tensors.  x: (M, K), w: (N, K), residual: (M, N) in bf16 or fp32; bias: (N,) fp32.  Returns
     y and, with keep_pre, the pre-activation z, which linear_bwd needs where act is not ACT_NONE."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, K = _rows(x, "x", b16, f32)
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
-    _want(w, x.dtype, (N, K), "w"); _want(bias, f32, (N,), "bias"); _want(residual, x.dtype, (M, N), "residual")
+    _like(w, x.dtype, (N, K), "w", dev); _like(bias, f32, (N,), "bias", dev); _like(residual, x.dtype, (M, N), "residual", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, bias, residual)
     o = out if out is not None else {}
-    y = _out(o, "y", (M, N), x.dtype, x, stream)
-    z = _out(o, "z", (M, N), x.dtype, x, stream) if keep_pre else None
+    y = _out(o, "y", (M, N), x.dtype, dev, stream)
+    z = _out(o, "z", (M, N), x.dtype, dev, stream) if keep_pre else None
     need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr()) & 15)
-    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w, bias, residual)
-    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
-    rc = (_lib or load_library()).tfla_linear_fwd(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb,
-                                        handle)
+    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    args = (x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb, handle)
+    call = (_lib or load_library()).tfla_linear_fwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_fwd")
     return o
@@ -635,19 +659,20 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
                out: Optional[Dict] = None) -> Dict:
     """tfla_linear_bwd on torch device tensors.  dy: (M, N); z: the pre-activation of the forward call where act is not ACT_NONE.
     Returns dx, dw, db (those that are wanted); the gradient of the residual is dy itself."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, K = _rows(x, "x", b16, f32)
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
-    _want(w, x.dtype, (N, K), "w"); _want(dy, x.dtype, (M, N), "dy"); _want(z, x.dtype, (M, N), "z")
+    _like(w, x.dtype, (N, K), "w", dev); _like(dy, x.dtype, (M, N), "dy", dev); _like(z, x.dtype, (M, N), "z", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, dy, z)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, x, stream) if want_dx else None
-    dw = _out(o, "dw", (N, K), x.dtype, x, stream) if want_dw else None
-    db = _out(o, "db", (N,), f32, x, stream) if want_db else None
+    dx = _out(o, "dx", (M, K), x.dtype, dev, stream) if want_dx else None
+    dw = _out(o, "dw", (N, K), x.dtype, dev, stream) if want_dw else None
+    db = _out(o, "db", (N,), f32, dev, stream) if want_db else None
     need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr() | dy.data_ptr()) & 15)
-    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w, dy, z)
-    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
-    rc = (_lib or load_library()).tfla_linear_bwd(x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb,
-                                        handle)
+    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    args = (x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb, handle)
+    call = (_lib or load_library()).tfla_linear_bwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_bwd")
     return o
@@ -657,20 +682,21 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
               out: Optional[Dict] = None) -> Dict:
     """tfla_gated_fwd on torch device tensors: h = act(x w_gate^T + b_gate) * (x w_up^T + b_up).  x: (M, K), w_gate, w_up: (N, K) in
     bf16 or fp32; b_gate, b_up: (N,) fp32.  Returns h and, with keep_pre, a and u, which gated_bwd needs."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, K = _rows(x, "x", b16, f32)
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
-    _want(w_gate, x.dtype, (N, K), "w_gate"); _want(w_up, x.dtype, (N, K), "w_up")
-    _want(b_gate, f32, (N,), "b_gate"); _want(b_up, f32, (N,), "b_up")
+    _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
+    _like(b_gate, f32, (N,), "b_gate", dev); _like(b_up, f32, (N,), "b_up", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, b_gate, b_up)
     o = out if out is not None else {}
-    h = _out(o, "h", (M, N), x.dtype, x, stream)
-    a = _out(o, "a", (M, N), x.dtype, x, stream) if keep_pre else None
-    u = _out(o, "u", (M, N), x.dtype, x, stream) if keep_pre else None
+    h = _out(o, "h", (M, N), x.dtype, dev, stream)
+    a = _out(o, "a", (M, N), x.dtype, dev, stream) if keep_pre else None
+    u = _out(o, "u", (M, N), x.dtype, dev, stream) if keep_pre else None
     need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15)
-    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, b_gate, b_up)
-    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
-    rc = (_lib or load_library()).tfla_gated_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype,
-                                       h, a, u, ws, wsb, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype, h, a, u, ws, wsb, handle)
+    call = (_lib or load_library()).tfla_gated_fwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_fwd")
     return o
@@ -680,22 +706,24 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
               out: Optional[Dict] = None) -> Dict:
     """tfla_gated_bwd on torch device tensors.  a, u: as gated_fwd with keep_pre returned them; dh: (M, N).  Returns dx, dw_gate,
     dw_up, db_gate, db_up (those that are wanted)."""
-    b16, f32, raw_stream = _torch_names or _torch_types()
-    dtype, M, K = _rows(x, "x", b16, f32)
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
-    _want(w_gate, x.dtype, (N, K), "w_gate"); _want(w_up, x.dtype, (N, K), "w_up")
-    _want(a, x.dtype, (M, N), "a"); _want(u, x.dtype, (M, N), "u"); _want(dh, x.dtype, (M, N), "dh")
+    _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
+    _like(a, x.dtype, (M, N), "a", dev); _like(u, x.dtype, (M, N), "u", dev); _like(dh, x.dtype, (M, N), "dh", dev)
+    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, a, u, dh)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, x, stream) if want_dx else None
-    dwg = _out(o, "dw_gate", (N, K), x.dtype, x, stream) if want_dw else None
-    dwu = _out(o, "dw_up", (N, K), x.dtype, x, stream) if want_dw else None
-    dbg = _out(o, "db_gate", (N,), f32, x, stream) if want_db else None
-    dbu = _out(o, "db_up", (N,), f32, x, stream) if want_db else None
+    dx = _out(o, "dx", (M, K), x.dtype, dev, stream) if want_dx else None
+    dwg = _out(o, "dw_gate", (N, K), x.dtype, dev, stream) if want_dw else None
+    dwu = _out(o, "dw_up", (N, K), x.dtype, dev, stream) if want_dw else None
+    dbg = _out(o, "db_gate", (N,), f32, dev, stream) if want_db else None
+    dbu = _out(o, "db_up", (N,), f32, dev, stream) if want_db else None
     need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | dh.data_ptr()) & 15)
-    handle = raw_stream(x.get_device()) if stream is None else _on(stream, x, w_gate, w_up, a, u, dh)
-    ws, wsb = _scratch(o, workspace, need, x, stream, handle)
-    rc = (_lib or load_library()).tfla_gated_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N,
-                                       int(act), dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N, int(act), dtype, dx, dwg, dwu, dbg,
+            dbu, ws, wsb, handle)
+    call = (_lib or load_library()).tfla_gated_bwd
+    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_bwd")
     return o

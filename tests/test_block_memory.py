@@ -234,3 +234,43 @@ def test_a_callers_workspace_is_not_kept(machine, name):
     # its size counts in bytes
     call(workspace=Tensor((1 << 20,), F32))
     assert workspace_of(machine, name)[1] == 4 << 20
+
+
+# ---- devices --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("name", NAMES)
+def test_a_call_runs_on_its_tensors_device(machine, name):
+    """the handle of a default stream is 0 on every device: it means the current one's, which has to be the tensors'"""
+    call, _ = calls(device=1)[name]
+    o = call()
+    _, args, device = machine.calls[-1]
+    assert device == 1 and machine.device == 0
+    for t in tensors(o).values():
+        assert t.get_device() == 1 and t.pool is machine.streams[1]
+    machine.streams[1] = Stream(91, 1)
+    call()
+    assert machine.calls[-1][1][-1] == 91
+    side = Stream(92, 1)
+    o = call(stream=side)
+    assert machine.calls[-1][1][-1] == 92 and machine.calls[-1][2] == 1
+    for t in tensors(o).values():
+        assert t.pool is side and machine.streams[1] in t.seen
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_and_streams_of_other_devices_are_refused(machine, name):
+    call, inputs = calls()[name]
+    with pytest.raises(ValueError):
+        call(stream=Stream(93, 1))
+    for t in inputs:
+        t.device = torch.device("cuda", 1)
+        with pytest.raises(ValueError):
+            call()
+        t.device = torch.device("cuda", 0)
+    o = tensors(call())
+    for k in o:
+        if k != "workspace":
+            o[k].device = torch.device("cuda", 1)
+            with pytest.raises(ValueError):
+                call(out=dict(o))
+            o[k].device = torch.device("cuda", 0)
+    assert len(machine.calls) == 1
