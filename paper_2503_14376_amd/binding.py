@@ -517,6 +517,11 @@ def _like(t, dtype, shape, name, dev):
                          % (name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.device))
 
 
+def _too_large(*sizes):
+    """sizes go to the library as 32-bit integers, which ctypes would cut off without a word"""
+    raise ValueError("sizes of 2^31 and more are not supported (got %s)" % (sizes,))
+
+
 def _elsewhere(dev, call, args):
     """the launching call with the tensors' device current, which another one is"""
     import torch
@@ -596,6 +601,8 @@ def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream
     statistics rstd and (LayerNorm) mean, which norm_bwd needs."""
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
+    if (M | D) >> 31:
+        _too_large(M, D)
     _like(gamma, f32, (D,), "gamma", dev); _like(beta, f32, (D,), "beta", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, gamma, beta)
     o = out if out is not None else {}
@@ -615,6 +622,8 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
     Returns dx, dgamma, dbeta (the last two where wanted)."""
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
+    if (M | D) >> 31:
+        _too_large(M, D)
     _like(dy, x.dtype, (M, D), "dy", dev); _like(d_residual, x.dtype, (M, D), "d_residual", dev); _like(gamma, f32, (D,), "gamma", dev)
     _like(rstd, f32, (M,), "rstd", dev); _like(mean, f32, (M,), "mean", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, dy, rstd, mean, gamma, d_residual)
@@ -640,6 +649,8 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
     _like(w, x.dtype, (N, K), "w", dev); _like(bias, f32, (N,), "bias", dev); _like(residual, x.dtype, (M, N), "residual", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, bias, residual)
     o = out if out is not None else {}
@@ -662,6 +673,8 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
     _like(w, x.dtype, (N, K), "w", dev); _like(dy, x.dtype, (M, N), "dy", dev); _like(z, x.dtype, (M, N), "z", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, dy, z)
     o = out if out is not None else {}
@@ -685,6 +698,8 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
     _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
     _like(b_gate, f32, (N,), "b_gate", dev); _like(b_up, f32, (N,), "b_up", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, b_gate, b_up)
@@ -709,6 +724,8 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
     _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
     _like(a, x.dtype, (M, N), "a", dev); _like(u, x.dtype, (M, N), "u", dev); _like(dh, x.dtype, (M, N), "dh", dev)
     handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, a, u, dh)

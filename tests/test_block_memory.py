@@ -274,3 +274,19 @@ def test_tensors_and_streams_of_other_devices_are_refused(machine, name):
                 call(out=dict(o))
             o[k].device = torch.device("cuda", 0)
     assert len(machine.calls) == 1
+
+
+# ---- sizes of 2^31 and more, which ctypes would cut off --------------------------------------------------------------
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("which", ["M", "K", "N"])
+def test_sizes_beyond_32_bits_are_refused(machine, name, which):
+    import ctypes
+    assert ctypes.c_int((1 << 32) + 4).value == 4
+    if name.startswith("norm") and which == "N":
+        which = "K"
+    sizes = {"M": 2, "K": 3, "N": 2}
+    for n in (1 << 31, (1 << 32) + 4):
+        sizes[which] = n
+        with pytest.raises(ValueError):
+            calls(**sizes)[name][0]()
+    assert not machine.calls
