@@ -571,16 +571,24 @@ def _bytes(workspace):
     return workspace.numel() * workspace.element_size()
 
 
+def _memory(workspace, dev):
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on cuda:%d (got one on %s)" % (dev, workspace.device))
+
+
 def _scratch(o, workspace, need, dev, stream, handle):
     """address and size of the workspace: the caller's, which `out` does not keep, or the one in `out` that earlier calls left, or a new one
     there.  The kept one remembers the stream it was last used on and is recorded on another that uses it.  One that has become too small
     stays alive beside its successor: a captured graph may hold its address (a change of sizes with the same `out` is rare)."""
     if workspace is not None:
+        _memory(workspace, dev)
         if stream is not None:
             workspace.record_stream(stream)
         o.setdefault("workspace", None)
         return workspace.data_ptr(), _bytes(workspace)
     kept = o.get("workspace")
+    if kept is not None:
+        _memory(kept, dev)
     if need and (kept is None or _bytes(kept) < need):
         import torch
         new = o["workspace"] = _new((need,), torch.uint8, dev, stream)

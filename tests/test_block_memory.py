@@ -290,3 +290,19 @@ def test_sizes_beyond_32_bits_are_refused(machine, name, which):
         with pytest.raises(ValueError):
             calls(**sizes)[name][0]()
     assert not machine.calls
+
+
+@pytest.mark.parametrize("name", WITH_WORKSPACE)
+def test_a_workspace_that_the_device_cannot_use_is_refused(machine, name):
+    """host memory, memory of another device, or a tensor with gaps"""
+    call, _ = calls()[name]
+    host, other, gaps = (Tensor((1 << 24,), torch.uint8) for _ in range(3))
+    host.get_device = lambda: -1
+    other.device = torch.device("cuda", 1)
+    gaps.is_contiguous = lambda: False
+    for bad in (host, other, gaps):
+        with pytest.raises(ValueError):
+            call(workspace=bad)
+        with pytest.raises(ValueError):
+            call(out={"workspace": bad})
+    assert not machine.calls
