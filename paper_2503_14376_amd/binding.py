@@ -162,12 +162,38 @@ def _torch_dtype(dtype):
     return torch.bfloat16 if dtype == BF16 else torch.float32
 
 
-def _stream_handle(stream):
+def _stream_handle(stream=None):
     if stream is not None:
         return stream.cuda_stream
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the current stream without a stream object around it
     return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+
+
+# Memory and streams.  A call on an explicit stream is the call on the current stream with that one made current, so that new memory comes
+# from its pool, where a block that was dropped before has had its last use in the stream's order.  (From the pool of the stream that the
+# caller works on, the block of a tensor dropped a moment ago could come back while work queued there still reads it.)  The caller drops
+# results on its own stream, which is recorded on them.  The call's other tensors may belong to any stream: the call's own is recorded on
+# them, so that none is handed out again before the call has run.
+def _within(call, stream, args):
+    """call(**args), args with stream among them, on `stream`"""
+    import torch
+    device = stream.device.index
+    given = [t for t in (*args.values(), *(args.get("out") or {}).values()) if hasattr(t, "record_stream")]
+    for t in given:
+        if t.get_device() not in (device, -1):
+            raise ValueError("the stream is one of cuda:%d, a tensor is on %s" % (device, t.device))
+    args["stream"] = None
+    before = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        result = call(**args)
+    for t in given:
+        if t.is_cuda:
+            t.record_stream(stream)
+    for t in result.values() if isinstance(result, dict) else result:
+        if getattr(t, "is_cuda", False):
+            t.record_stream(before)
+    return result
 
 
 def _want(t, dtype, shape, name):
@@ -183,6 +209,8 @@ def mlstm_fwd(q, k, v, i_pre, f_pre, C0=None, n0=None, m0=None, chunk=256, varia
               return_state=True, workspace=None, stream=None, out: Optional[Dict] = None) -> Dict:
     """tfla_mlstm_fwd on torch device tensors.  q,k: (B,NH,T,dqk); v: (B,NH,T,dhv) in bf16 or
     fp32; gates fp32 (B,NH,T).  Returns a dict with H, Cn, nn, mn, n_out, m_out."""
+    if stream is not None:
+        return _within(mlstm_fwd, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dqk = q.shape
@@ -210,7 +238,7 @@ def mlstm_fwd(q, k, v, i_pre, f_pre, C0=None, n0=None, m0=None, chunk=256, varia
                             B, NH, T, dqk, dhv, int(chunk), int(variant), dtype, float(eps),
                             _ptr(o["H"]), _ptr(o.get("Cn")), _ptr(o.get("nn")), _ptr(o.get("mn")),
                             _ptr(o["n_out"]), _ptr(o["m_out"]),
-                            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream))
+                            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_fwd")
     o["workspace"] = workspace
@@ -226,6 +254,8 @@ def mlstm_fwd_static(q, k, v, i_pre, f_pre, C0=None, n0=None, m0=None, chunk=256
     """tfla_mlstm_fwd_static on torch device tensors: the forward pass on the library's own static scratch memory.
     `out` must hold every output tensor (H, Cn, nn, mn, n_out, m_out; the state and per-step entries may be
     missing = not wanted): this wrapper allocates nothing either."""
+    if stream is not None:
+        return _within(mlstm_fwd_static, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dqk = q.shape
@@ -244,7 +274,7 @@ def mlstm_fwd_static(q, k, v, i_pre, f_pre, C0=None, n0=None, m0=None, chunk=256
     rc = lib.tfla_mlstm_fwd_static(_ptr(q), _ptr(k), _ptr(v), _ptr(i_pre), _ptr(f_pre), _ptr(C0), _ptr(n0), _ptr(m0),
                                    B, NH, T, dqk, dhv, int(chunk), int(variant), dtype, float(eps),
                                    _ptr(o["H"]), _ptr(o.get("Cn")), _ptr(o.get("nn")), _ptr(o.get("mn")),
-                                   _ptr(o.get("n_out")), _ptr(o.get("m_out")), _stream_handle(stream))
+                                   _ptr(o.get("n_out")), _ptr(o.get("m_out")), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_fwd_static")
     return o
@@ -256,6 +286,8 @@ def mlstm_bwd(q, k, v, i_pre, f_pre, dH, n_out=None, m_out=None, C0=None, n0=Non
     """tfla_mlstm_bwd on torch device tensors.  Returns dq, dk, dv, d_i_pre, d_f_pre, dC0.
     fwd_workspace: the (untouched) workspace tensor of the matching mlstm_fwd call, or None to
     recompute gates and chunk states."""
+    if stream is not None:
+        return _within(mlstm_bwd, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dqk = q.shape
@@ -285,7 +317,7 @@ def mlstm_bwd(q, k, v, i_pre, f_pre, dH, n_out=None, m_out=None, C0=None, n0=Non
                             _ptr(o["dq"]), _ptr(o["dk"]), _ptr(o["dv"]), _ptr(o["d_i_pre"]), _ptr(o["d_f_pre"]),
                             _ptr(o.get("dC0")),
                             _ptr(fwd_workspace), 0 if fwd_workspace is None else fwd_workspace.numel(),
-                            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream))
+                            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_bwd")
     o["workspace"] = workspace
@@ -296,6 +328,8 @@ def mlstm_step(q, k, v, i_pre, f_pre, C, n=None, m=None, variant=EXP, eps=1e-6, 
                out: Optional[Dict] = None, inplace_C: bool = False) -> Dict:
     """tfla_mlstm_step on torch device tensors.  q, k: (B,NH,dqk); v: (B,NH,dhv); i_pre, f_pre: (B,NH);
     C: (B,NH,dqk,dhv) fp32, n: (B,NH,dqk), m: (B,NH).  Returns h and the new state C, n, m."""
+    if stream is not None:
+        return _within(mlstm_step, stream, locals())
     import torch
     lib = load_library()
     B, NH, dqk = q.shape
@@ -316,7 +350,7 @@ def mlstm_step(q, k, v, i_pre, f_pre, C, n=None, m=None, variant=EXP, eps=1e-6, 
         o["m"] = torch.empty((B, NH), dtype=f32, device=dev)
     rc = lib.tfla_mlstm_step(_ptr(q), _ptr(k), _ptr(v), _ptr(i_pre), _ptr(f_pre), _ptr(C), _ptr(n), _ptr(m),
                              B, NH, dqk, dhv, int(variant), dtype, float(eps),
-                             _ptr(o["h"]), _ptr(o["C"]), _ptr(o["n"]), _ptr(o["m"]), _stream_handle(stream))
+                             _ptr(o["h"]), _ptr(o["C"]), _ptr(o["n"]), _ptr(o["m"]), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_step")
     return o
@@ -328,6 +362,8 @@ def mlstm_layer_fwd(q, k, v, i_pre, f_pre, o_pre=None, gamma=None, beta=None, C0
     """tfla_mlstm_layer_fwd on torch device tensors: soft-capped gates, cell, multi-head norm, output gate.
     o_pre: (B,NH,T,dhv) like v or None; gamma, beta: (NH,dhv) fp32 or None.  Returns Y, H (cell output), the
     final state, n_out, m_out and the workspace."""
+    if stream is not None:
+        return _within(mlstm_layer_fwd, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dqk = q.shape
@@ -358,7 +394,7 @@ def mlstm_layer_fwd(q, k, v, i_pre, f_pre, o_pre=None, gamma=None, beta=None, C0
                                   float(eps), float(gate_softcap), int(norm_kind), float(norm_eps),
                                   _ptr(o["Y"]), _ptr(o["H"]), _ptr(o.get("Cn")), _ptr(o.get("nn")), _ptr(o.get("mn")),
                                   _ptr(o["n_out"]), _ptr(o["m_out"]),
-                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream))
+                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_layer_fwd")
     o["workspace"] = workspace
@@ -371,6 +407,8 @@ def mlstm_layer_bwd(q, k, v, i_pre, f_pre, H, dY, o_pre=None, gamma=None, beta=N
                     fwd_workspace=None) -> Dict:
     """tfla_mlstm_layer_bwd on torch device tensors.  Returns dq, dk, dv, d_i_pre, d_f_pre, do_pre (if o_pre is
     given), dgamma, dbeta, dC0."""
+    if stream is not None:
+        return _within(mlstm_layer_bwd, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dqk = q.shape
@@ -406,7 +444,7 @@ def mlstm_layer_bwd(q, k, v, i_pre, f_pre, H, dY, o_pre=None, gamma=None, beta=N
                                   _ptr(o["dq"]), _ptr(o["dk"]), _ptr(o["dv"]), _ptr(o["d_i_pre"]), _ptr(o["d_f_pre"]),
                                   _ptr(o.get("do_pre")), _ptr(o.get("dgamma")), _ptr(o.get("dbeta")), _ptr(o.get("dC0")),
                                   _ptr(fwd_workspace), 0 if fwd_workspace is None else fwd_workspace.numel(),
-                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream))
+                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_layer_bwd")
     o["workspace"] = workspace
@@ -418,6 +456,8 @@ def mlstm_layer_step(q, k, v, i_pre, f_pre, C, n=None, m=None, o_pre=None, gamma
                      inplace_C: bool = False) -> Dict:
     """tfla_mlstm_layer_step on torch device tensors: mlstm_step with soft-capped gates, then norm and output gate.
     o_pre: (B,NH,dhv) like v or None.  Returns y, h (cell output) and the new state C, n, m."""
+    if stream is not None:
+        return _within(mlstm_layer_step, stream, locals())
     import torch
     lib = load_library()
     B, NH, dqk = q.shape
@@ -441,7 +481,7 @@ def mlstm_layer_step(q, k, v, i_pre, f_pre, C, n=None, m=None, o_pre=None, gamma
     rc = lib.tfla_mlstm_layer_step(_ptr(q), _ptr(k), _ptr(v), _ptr(i_pre), _ptr(f_pre), _ptr(o_pre), _ptr(gamma), _ptr(beta),
                                    _ptr(C), _ptr(n), _ptr(m), B, NH, dqk, dhv, int(variant), dtype, float(eps),
                                    float(gate_softcap), int(norm_kind), float(norm_eps), _ptr(o["y"]), _ptr(o["h"]),
-                                   _ptr(o["C"]), _ptr(o["n"]), _ptr(o["m"]), _stream_handle(stream))
+                                   _ptr(o["C"]), _ptr(o["n"]), _ptr(o["m"]), _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_mlstm_layer_step")
     return o
@@ -449,6 +489,8 @@ def mlstm_layer_step(q, k, v, i_pre, f_pre, C, n=None, m=None, o_pre=None, gamma
 
 def transfer_gain(h, v, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None):
     """tfla_transfer_gain on torch device tensors h, v (B,NH,T,dhv).  Returns (g_before, g_after), each (B,NH) fp32."""
+    if stream is not None:
+        return _within(transfer_gain, stream, locals())
     import torch
     lib = load_library()
     B, NH, T, dhv = h.shape
@@ -458,7 +500,7 @@ def transfer_gain(h, v, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None):
     gb = torch.empty((B, NH), dtype=torch.float32, device=h.device)
     ga = torch.empty((B, NH), dtype=torch.float32, device=h.device)
     rc = lib.tfla_transfer_gain(_ptr(h), _ptr(v), B, NH, T, dhv, dtype, int(norm_kind), float(norm_eps), _ptr(gb), _ptr(ga),
-                                _stream_handle(stream))
+                                _stream_handle())
     if rc != 0:
         raise TflaError(rc, "tfla_transfer_gain")
     return gb, ga
@@ -529,41 +571,14 @@ def _elsewhere(dev, call, args):
         return call(*args)
 
 
-# Memory and streams.  A call on a stream that is not the current one takes new memory from that stream's own pool, where a block that was
-# freed before has had its last use in the stream's order; the current stream, on which the caller made the call and will drop its tensors, is
-# recorded on it.  (From the current stream's pool the block of a tensor that was dropped a moment ago could come back while work queued there
-# still reads it.)  The call's other tensors belong to other streams: they are recorded on this one, so that none is handed out again before
-# the call has run.
-def _new(shape, dtype, dev, stream):
-    import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
-    t.record_stream(torch.cuda.current_stream(dev))
-    return t
-
-
-def _on(stream, dev, *inputs):
-    """the handle of an explicit stream, with the call's inputs recorded on it"""
-    if stream.device.index != dev:
-        raise ValueError("the stream is one of %s, the tensors are on cuda:%d" % (stream.device, dev))
-    for t in inputs:
-        if t is not None:
-            t.record_stream(stream)
-    return stream.cuda_stream
-
-
-def _out(o, name, shape, dtype, dev, stream):
+def _out(o, name, shape, dtype, dev):
     """address of o[name], checked, or of a new tensor there"""
     t = o.get(name)
     if t is None:
-        t = o[name] = _new(shape, dtype, dev, stream)
-        return t.data_ptr()
-    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        import torch
+        t = o[name] = torch.empty(shape, dtype=dtype, device=dev)
+    elif t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         _like(t, dtype, shape, name, dev)
-    if stream is not None:
-        t.record_stream(stream)
     return t.data_ptr()
 
 
@@ -576,14 +591,12 @@ def _memory(workspace, dev):
         raise ValueError("workspace must be a contiguous tensor on cuda:%d (got one on %s)" % (dev, workspace.device))
 
 
-def _scratch(o, workspace, need, dev, stream, handle):
+def _scratch(o, workspace, need, dev, handle):
     """address and size of the workspace: the caller's, which `out` does not keep, or the one in `out` that earlier calls left, or a new one
     there.  The kept one remembers the stream it was last used on and is recorded on another that uses it.  One that has become too small
     stays alive beside its successor: a captured graph may hold its address (a change of sizes with the same `out` is rare)."""
     if workspace is not None:
         _memory(workspace, dev)
-        if stream is not None:
-            workspace.record_stream(stream)
         o.setdefault("workspace", None)
         return workspace.data_ptr(), _bytes(workspace)
     kept = o.get("workspace")
@@ -591,7 +604,7 @@ def _scratch(o, workspace, need, dev, stream, handle):
         _memory(kept, dev)
     if need and (kept is None or _bytes(kept) < need):
         import torch
-        new = o["workspace"] = _new((need,), torch.uint8, dev, stream)
+        new = o["workspace"] = torch.empty(need, dtype=torch.uint8, device=dev)
         new.tfla_before, new.tfla_stream = kept, handle
         return new.data_ptr(), need
     if kept is None:
@@ -599,7 +612,7 @@ def _scratch(o, workspace, need, dev, stream, handle):
         return None, 0
     if getattr(kept, "tfla_stream", None) != handle:
         import torch
-        kept.record_stream(torch.cuda.current_stream(dev) if stream is None else stream)
+        kept.record_stream(torch.cuda.current_stream(dev))
         kept.tfla_stream = handle
     return kept.data_ptr(), _bytes(kept)
 
@@ -607,16 +620,20 @@ def _scratch(o, workspace, need, dev, stream, handle):
 def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream=None, out: Optional[Dict] = None) -> Dict:
     """tfla_norm_fwd on torch device tensors.  x: (M, D) in bf16 or fp32; gamma, beta: (D,) fp32 or None.  Returns y and the row
     statistics rstd and (LayerNorm) mean, which norm_bwd needs."""
+    if stream is not None:
+        return _within(norm_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
     if (M | D) >> 31:
         _too_large(M, D)
-    _like(gamma, f32, (D,), "gamma", dev); _like(beta, f32, (D,), "beta", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, gamma, beta)
+    if gamma is not None:
+        _like(gamma, f32, (D,), "gamma", dev)
+    if beta is not None:
+        _like(beta, f32, (D,), "beta", dev)
     o = out if out is not None else {}
-    y, rstd = _out(o, "y", (M, D), x.dtype, dev, stream), _out(o, "rstd", (M,), f32, dev, stream)
-    mean = _out(o, "mean", (M,), f32, dev, stream) if norm_kind == NORM_LAYER else None
-    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean, handle)
+    y, rstd = _out(o, "y", (M, D), x.dtype, dev), _out(o, "rstd", (M,), f32, dev)
+    mean = _out(o, "mean", (M,), f32, dev) if norm_kind == NORM_LAYER else None
+    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean, raw_stream(dev))
     call = (_lib or load_library()).tfla_norm_fwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
@@ -628,19 +645,21 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
              workspace=None, stream=None, out: Optional[Dict] = None) -> Dict:
     """tfla_norm_bwd on torch device tensors.  rstd, mean: as norm_fwd returned them; d_residual: (M, D), added to dx, or None.
     Returns dx, dgamma, dbeta (the last two where wanted)."""
+    if stream is not None:
+        return _within(norm_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
     if (M | D) >> 31:
         _too_large(M, D)
     _like(dy, x.dtype, (M, D), "dy", dev); _like(d_residual, x.dtype, (M, D), "d_residual", dev); _like(gamma, f32, (D,), "gamma", dev)
     _like(rstd, f32, (M,), "rstd", dev); _like(mean, f32, (M,), "mean", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, dy, rstd, mean, gamma, d_residual)
+    handle = raw_stream(dev)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, D), x.dtype, dev, stream)
-    dgamma = _out(o, "dgamma", (D,), f32, dev, stream) if want_dgamma else None
-    dbeta = _out(o, "dbeta", (D,), f32, dev, stream) if want_dbeta else None
+    dx = _out(o, "dx", (M, D), x.dtype, dev)
+    dgamma = _out(o, "dgamma", (D,), f32, dev) if want_dgamma else None
+    dbeta = _out(o, "dbeta", (D,), f32, dev) if want_dbeta else None
     need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
-    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
     args = (x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype, int(norm_kind), dx, dgamma,
             dbeta, ws, wsb, handle)
     call = (_lib or load_library()).tfla_norm_bwd
@@ -654,18 +673,24 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
                out: Optional[Dict] = None) -> Dict:
     """tfla_linear_fwd on torch device tensors.  x: (M, K), w: (N, K), residual: (M, N) in bf16 or fp32; bias: (N,) fp32.  Returns
     y and, with keep_pre, the pre-activation z, which linear_bwd needs where act is not ACT_NONE."""
+    if stream is not None:
+        return _within(linear_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
     if (M | K | N) >> 31:
         _too_large(M, K, N)
-    _like(w, x.dtype, (N, K), "w", dev); _like(bias, f32, (N,), "bias", dev); _like(residual, x.dtype, (M, N), "residual", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, bias, residual)
+    _like(w, x.dtype, (N, K), "w", dev)
+    if bias is not None:
+        _like(bias, f32, (N,), "bias", dev)
+    if residual is not None:
+        _like(residual, x.dtype, (M, N), "residual", dev)
+    handle = raw_stream(dev)
     o = out if out is not None else {}
-    y = _out(o, "y", (M, N), x.dtype, dev, stream)
-    z = _out(o, "z", (M, N), x.dtype, dev, stream) if keep_pre else None
+    y = _out(o, "y", (M, N), x.dtype, dev)
+    z = _out(o, "z", (M, N), x.dtype, dev) if keep_pre else None
     need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
     args = (x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb, handle)
     call = (_lib or load_library()).tfla_linear_fwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
@@ -678,19 +703,21 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
                out: Optional[Dict] = None) -> Dict:
     """tfla_linear_bwd on torch device tensors.  dy: (M, N); z: the pre-activation of the forward call where act is not ACT_NONE.
     Returns dx, dw, db (those that are wanted); the gradient of the residual is dy itself."""
+    if stream is not None:
+        return _within(linear_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w.shape[0]
     if (M | K | N) >> 31:
         _too_large(M, K, N)
     _like(w, x.dtype, (N, K), "w", dev); _like(dy, x.dtype, (M, N), "dy", dev); _like(z, x.dtype, (M, N), "z", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w, dy, z)
+    handle = raw_stream(dev)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, dev, stream) if want_dx else None
-    dw = _out(o, "dw", (N, K), x.dtype, dev, stream) if want_dw else None
-    db = _out(o, "db", (N,), f32, dev, stream) if want_db else None
+    dx = _out(o, "dx", (M, K), x.dtype, dev) if want_dx else None
+    dw = _out(o, "dw", (N, K), x.dtype, dev) if want_dw else None
+    db = _out(o, "db", (N,), f32, dev) if want_db else None
     need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr() | dy.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
     args = (x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb, handle)
     call = (_lib or load_library()).tfla_linear_bwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
@@ -703,6 +730,8 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
               out: Optional[Dict] = None) -> Dict:
     """tfla_gated_fwd on torch device tensors: h = act(x w_gate^T + b_gate) * (x w_up^T + b_up).  x: (M, K), w_gate, w_up: (N, K) in
     bf16 or fp32; b_gate, b_up: (N,) fp32.  Returns h and, with keep_pre, a and u, which gated_bwd needs."""
+    if stream is not None:
+        return _within(gated_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
@@ -710,13 +739,13 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
         _too_large(M, K, N)
     _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
     _like(b_gate, f32, (N,), "b_gate", dev); _like(b_up, f32, (N,), "b_up", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, b_gate, b_up)
+    handle = raw_stream(dev)
     o = out if out is not None else {}
-    h = _out(o, "h", (M, N), x.dtype, dev, stream)
-    a = _out(o, "a", (M, N), x.dtype, dev, stream) if keep_pre else None
-    u = _out(o, "u", (M, N), x.dtype, dev, stream) if keep_pre else None
+    h = _out(o, "h", (M, N), x.dtype, dev)
+    a = _out(o, "a", (M, N), x.dtype, dev) if keep_pre else None
+    u = _out(o, "u", (M, N), x.dtype, dev) if keep_pre else None
     need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
     args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype, h, a, u, ws, wsb, handle)
     call = (_lib or load_library()).tfla_gated_fwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
@@ -729,6 +758,8 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
               out: Optional[Dict] = None) -> Dict:
     """tfla_gated_bwd on torch device tensors.  a, u: as gated_fwd with keep_pre returned them; dh: (M, N).  Returns dx, dw_gate,
     dw_up, db_gate, db_up (those that are wanted)."""
+    if stream is not None:
+        return _within(gated_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
     N = w_gate.shape[0]
@@ -736,15 +767,15 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
         _too_large(M, K, N)
     _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
     _like(a, x.dtype, (M, N), "a", dev); _like(u, x.dtype, (M, N), "u", dev); _like(dh, x.dtype, (M, N), "dh", dev)
-    handle = raw_stream(dev) if stream is None else _on(stream, dev, x, w_gate, w_up, a, u, dh)
+    handle = raw_stream(dev)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, dev, stream) if want_dx else None
-    dwg = _out(o, "dw_gate", (N, K), x.dtype, dev, stream) if want_dw else None
-    dwu = _out(o, "dw_up", (N, K), x.dtype, dev, stream) if want_dw else None
-    dbg = _out(o, "db_gate", (N,), f32, dev, stream) if want_db else None
-    dbu = _out(o, "db_up", (N,), f32, dev, stream) if want_db else None
+    dx = _out(o, "dx", (M, K), x.dtype, dev) if want_dx else None
+    dwg = _out(o, "dw_gate", (N, K), x.dtype, dev) if want_dw else None
+    dwu = _out(o, "dw_up", (N, K), x.dtype, dev) if want_dw else None
+    dbg = _out(o, "db_gate", (N,), f32, dev) if want_db else None
+    dbu = _out(o, "db_up", (N,), f32, dev) if want_db else None
     need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | dh.data_ptr()) & 15)
-    ws, wsb = _scratch(o, workspace, need, dev, stream, handle)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
     args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N, int(act), dtype, dx, dwg, dwu, dbg,
             dbu, ws, wsb, handle)
     call = (_lib or load_library()).tfla_gated_bwd

@@ -1,4 +1,4 @@
-"""Which memory the binding of the residual block's operators hands to a call: pools, streams and devices, by stand-ins for device tensors,
+"""Which memory the binding hands to a call: pools, streams and devices, by stand-ins for device tensors,
 streams and the library's launching calls (its workspace queries are the real ones).  Nothing here needs a device."""
 import contextlib
 import os
@@ -58,9 +58,9 @@ class Machine:
         real = binding.load_library()
 
         def new(shape, dtype=None, device=None):
-            if device is None or torch.device(device).type != "cuda":
+            if device is None:
                 return empty(shape, dtype=dtype)
-            d = torch.device(device).index
+            d = index(device)
             return Tensor((shape,) if isinstance(shape, int) else shape, dtype, d, self.streams[d])
 
         @contextlib.contextmanager
@@ -90,6 +90,7 @@ class Machine:
             return self.device if device is None else device if isinstance(device, int) else torch.device(device).index
 
         monkeypatch.setattr(torch, "empty", new)
+        monkeypatch.setattr(torch, "empty_like", lambda t: new(t.shape, t.dtype, t.device))
         monkeypatch.setattr(torch.cuda, "stream", on_stream)
         monkeypatch.setattr(torch.cuda, "device", on_device)
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.streams[index(device)])
@@ -306,3 +307,52 @@ def test_a_workspace_that_the_device_cannot_use_is_refused(machine, name):
         with pytest.raises(ValueError):
             call(out={"workspace": bad})
     assert not machine.calls
+
+
+# ---- the cell's calls: memory and streams ---------------------------------------------------------------------------
+def cell_calls(B=1, H=2, T=128, k=64, v=64):
+    def t(*shape, d=BF16):
+        return Tensor(shape, d)
+    q, kk, u, o, dy, y = t(B, H, T, k), t(B, H, T, k), t(B, H, T, v), t(B, H, T, v), t(B, H, T, v), t(B, H, T, v)
+    i, f, n, m = (t(B, H, T, d=F32) for _ in range(4))
+    g, C, nn, mm = t(H, v, d=F32), t(B, H, k, v, d=F32), t(B, H, k, d=F32), t(B, H, d=F32)
+    q1, k1, u1, o1, i1, f1 = t(B, H, k), t(B, H, k), t(B, H, v), t(B, H, v), t(B, H, d=F32), t(B, H, d=F32)
+    outs = {"H": t(B, H, T, v), "Cn": t(B, H, k, v, d=F32), "nn": t(B, H, k, d=F32), "mn": t(B, H, d=F32), "n_out": t(B, H, T, d=F32),
+            "m_out": t(B, H, T, d=F32)}
+
+    def static(**kw):
+        return tfla.mlstm_fwd_static(q, kk, u, i, f, C, nn, mm, chunk=64, **{"out": outs, **kw})
+    return {
+        "fwd": (lambda **kw: tfla.mlstm_fwd(q, kk, u, i, f, C, nn, mm, chunk=64, **kw), [q, kk, u, i, f, C, nn, mm]),
+        "static": (static, [q, kk, u, i, f, C, nn, mm] + list(outs.values())),
+        "bwd": (lambda **kw: tfla.mlstm_bwd(q, kk, u, i, f, dy, n, m, C, nn, mm, chunk=64, **kw), [q, kk, u, i, f, dy, n, m, C, nn, mm]),
+        "step": (lambda **kw: tfla.mlstm_step(q1, k1, u1, i1, f1, C, nn, mm, **kw), [q1, k1, u1, i1, f1, C, nn, mm]),
+        "layer_fwd": (lambda **kw: tfla.mlstm_layer_fwd(q, kk, u, i, f, o, g, g, C, nn, mm, chunk=64, **kw), [q, kk, u, i, f, o, g, C, nn, mm]),
+        "layer_bwd": (lambda **kw: tfla.mlstm_layer_bwd(q, kk, u, i, f, y, dy, o, g, g, n, m, C, nn, mm, chunk=64, **kw),
+                      [q, kk, u, i, f, y, dy, o, g, n, m, C, nn, mm]),
+        "layer_step": (lambda **kw: tfla.mlstm_layer_step(q1, k1, u1, i1, f1, C, nn, mm, o1, g, g, **kw), [q1, k1, u1, i1, f1, o1, g, C, nn, mm]),
+        "gain": (lambda **kw: dict(enumerate(tfla.transfer_gain(u, y, **kw))), [u, y])}
+
+
+@pytest.mark.parametrize("name", list(cell_calls()))
+def test_the_cells_calls_on_another_stream(machine, name):
+    """as above: new memory from the stream's pool, everything else recorded on it; on the current stream nothing of the kind"""
+    side = Stream(95)
+    call, inputs = cell_calls()[name]
+    o = call(stream=side)
+    assert machine.calls[-1][1][-1] == 95
+    for k, t in tensors(o).items():
+        assert t in inputs or (t.pool is side and machine.streams[0] in t.seen), k
+    for t in inputs:
+        assert side in t.seen
+    if name not in ("gain", "static"):
+        call, _ = cell_calls()[name]
+        o = call()
+        for t in tensors(o).values():
+            assert t.pool is machine.streams[0] and not t.seen
+        kept = {k: t for k, t in tensors(o).items() if k != "workspace"}
+        call(stream=side, out=dict(kept))
+        assert all(side in t.seen for t in kept.values())
+    call, inputs = cell_calls()[name]
+    call()
+    assert machine.calls[-1][1][-1] == 0 and not any(t.seen for t in inputs)
