@@ -159,10 +159,11 @@ int product_bwd(const void* x, const void* const (&w)[2], const void* dy, const 
     const void* dz[2] = {dy, nullptr};
     long ldz = N;
     if (l.move_dz) { dz[0] = ws + l.dz0; dz[1] = pair ? ws + l.dz1 : nullptr; ldz = Np; }
-    if (M > 0 && (l.move_dz || want_db)) {
+    const bool store_dz = l.move_dz && (dx || want_dw);      // (bias gradients alone need the sums only)
+    if (M > 0 && (store_dz || want_db)) {
         ActBwdArgs a{};
         a.dy = dy; a.z = act == TFLA_ACT_NONE && !pair ? nullptr : z; a.u = u;
-        a.dz0 = l.move_dz ? ws + l.dz0 : nullptr; a.dz1 = pair ? ws + l.dz1 : nullptr;
+        a.dz0 = store_dz ? ws + l.dz0 : nullptr; a.dz1 = store_dz && pair ? ws + l.dz1 : nullptr;
         const bool direct = act_bwd_row_blocks(M, N) == 1;       // the sums need not be joined
         a.part = want_db && !direct ? reinterpret_cast<float*>(ws + l.dbpart) : nullptr;
         a.db0 = direct ? db[0] : nullptr; a.db1 = direct ? db[1] : nullptr;

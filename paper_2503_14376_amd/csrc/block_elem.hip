@@ -51,8 +51,10 @@ template <typename DT, bool PAIR, int NW> __global__ void __launch_bounds__(NW *
                 }
                 s0[e] += g[e];
             }
-            if (a.dz0) store8<DT>(a.dz0, r * a.ldd + c, 8, g);
-            if constexpr (PAIR) store8<DT>(a.dz1, r * a.ldd + c, 8, u);
+            if (a.dz0) {
+                store8<DT>(a.dz0, r * a.ldd + c, 8, g);
+                if constexpr (PAIR) store8<DT>(a.dz1, r * a.ldd + c, 8, u);
+            }
         }
     }
     if (!a.part && !a.db0 && !a.db1) return;

@@ -1,0 +1,54 @@
+"""What the residual block's operators write: outputs and workspaces inside larger allocations of a known pattern, which has to stay."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def tfla():
+    import paper_2503_14376_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def normal(gen, *shape, std=1.0, dtype=F32):
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def generator(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,N", [(20, 256), (3000, 256), (3000, 333)])
+@pytest.mark.parametrize("pair", [False, True])
+def test_bias_gradients_alone_store_only_sums(tfla, dtype, M, N, pair):
+    """the workspace holds partial sums of rows (four at least) and nothing of the size of the tensors"""
+    print("bias gradients", M, N, dtype, pair, flush=True)
+    gen, K = generator(M + N), 72
+    x, w, w2, z, u, dy = (normal(gen, *s, dtype=dtype) for s in ((M, K), (N, K), (N, K), (M, N), (M, N), (M, N)))
+    query = tfla.gated_workspace_bytes if pair else tfla.linear_workspace_bytes
+    code = tfla.BF16 if dtype == BF16 else tfla.F32
+    ws = torch.full((query(1, M, K, N, tfla.ACT_SILU, code, True),), 0xA5, dtype=torch.uint8, device="cuda")
+    kw = dict(act=tfla.ACT_SILU, want_db=True)
+    if pair:
+        full = tfla.gated_bwd(x, w, w2, z, u, dy, **kw)
+        one = tfla.gated_bwd(x, w, w2, z, u, dy, want_dx=False, want_dw=False, workspace=ws, **kw)
+        names = ("db_gate", "db_up")
+    else:
+        full = tfla.linear_bwd(x, w, dy, z, **kw)
+        one = tfla.linear_bwd(x, w, dy, z, want_dx=False, want_dw=False, workspace=ws, **kw)
+        names = ("db",)
+    for n in names:
+        assert torch.equal(one[n], full[n])
+    written = int((ws != 0xA5).sum())
+    sums = 0 if M <= 32 else (M + 3) // 4 * ((N + 7) // 8 * 8) * 4 * len(names)
+    assert written <= sums, (written, sums)
+    ws.fill_(0xA5)
+    if pair:
+        tfla.gated_bwd(x, w, w2, z, u, dy, want_dx=False, want_dw=False, workspace=ws, act=tfla.ACT_SILU)
+    else:
+        tfla.linear_bwd(x, w, dy, z, want_dx=False, want_dw=False, workspace=ws, act=tfla.ACT_SILU)
+    assert bool((ws == 0xA5).all())
