@@ -564,6 +564,14 @@ def _too_large(*sizes):
     raise ValueError("sizes of 2^31 and more are not supported (got %s)" % (sizes,))
 
 
+def _columns(x, w, want_dx, want_dw):
+    """input columns of a backward call by the tensors that it reads (for bias gradients alone neither, and any number will do)"""
+    if (want_dw and x is None) or (want_dx and w is None):
+        raise ValueError("%s is needed for the gradients that are wanted" % ("x" if want_dw and x is None else "the weight"))
+    t = w if x is None else x
+    return 1 if t is None else t.shape[-1]
+
+
 def _elsewhere(dev, call, args):
     """the launching call with the tensors' device current, which another one is"""
     import torch
@@ -702,23 +710,24 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
 def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_db=False, workspace=None, stream=None,
                out: Optional[Dict] = None) -> Dict:
     """tfla_linear_bwd on torch device tensors.  dy: (M, N); z: the pre-activation of the forward call where act is not ACT_NONE.
-    Returns dx, dw, db (those that are wanted); the gradient of the residual is dy itself."""
+    Returns dx, dw, db (those that are wanted); the gradient of the residual is dy itself.  x may be None without dw, w without dx."""
     if stream is not None:
         return _within(linear_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
-    dtype, M, K, dev = _rows(x, "x", b16, f32)
-    N = w.shape[0]
+    dtype, M, N, dev = _rows(dy, "dy", b16, f32)
+    K = _columns(x, w, want_dx, want_dw)
     if (M | K | N) >> 31:
         _too_large(M, K, N)
-    _like(w, x.dtype, (N, K), "w", dev); _like(dy, x.dtype, (M, N), "dy", dev); _like(z, x.dtype, (M, N), "z", dev)
+    t = dy.dtype
+    _like(x, t, (M, K), "x", dev); _like(w, t, (N, K), "w", dev); _like(z, t, (M, N), "z", dev)
     handle = raw_stream(dev)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, dev) if want_dx else None
-    dw = _out(o, "dw", (N, K), x.dtype, dev) if want_dw else None
+    dx = _out(o, "dx", (M, K), t, dev) if want_dx else None
+    dw = _out(o, "dw", (N, K), t, dev) if want_dw else None
     db = _out(o, "db", (N,), f32, dev) if want_db else None
-    need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr() | dy.data_ptr()) & 15)
+    need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, ((_ptr(x) or 0) | (_ptr(w) or 0) | dy.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (x.data_ptr(), w.data_ptr(), _ptr(dy), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb, handle)
+    args = (_ptr(x), _ptr(w), dy.data_ptr(), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb, handle)
     call = (_lib or load_library()).tfla_linear_bwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
     if rc != 0:
@@ -757,26 +766,27 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
 def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=True, want_db=False, workspace=None, stream=None,
               out: Optional[Dict] = None) -> Dict:
     """tfla_gated_bwd on torch device tensors.  a, u: as gated_fwd with keep_pre returned them; dh: (M, N).  Returns dx, dw_gate,
-    dw_up, db_gate, db_up (those that are wanted)."""
+    dw_up, db_gate, db_up (those that are wanted).  x may be None without the weights' gradients, the weights without dx."""
     if stream is not None:
         return _within(gated_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
-    dtype, M, K, dev = _rows(x, "x", b16, f32)
-    N = w_gate.shape[0]
+    dtype, M, N, dev = _rows(dh, "dh", b16, f32)
+    K = _columns(x, w_gate, want_dx, want_dw)
     if (M | K | N) >> 31:
         _too_large(M, K, N)
-    _like(w_gate, x.dtype, (N, K), "w_gate", dev); _like(w_up, x.dtype, (N, K), "w_up", dev)
-    _like(a, x.dtype, (M, N), "a", dev); _like(u, x.dtype, (M, N), "u", dev); _like(dh, x.dtype, (M, N), "dh", dev)
+    t = dh.dtype
+    _like(x, t, (M, K), "x", dev); _like(w_gate, t, (N, K), "w_gate", dev); _like(w_up, t, (N, K), "w_up", dev)
+    _like(a, t, (M, N), "a", dev); _like(u, t, (M, N), "u", dev)
     handle = raw_stream(dev)
     o = out if out is not None else {}
-    dx = _out(o, "dx", (M, K), x.dtype, dev) if want_dx else None
-    dwg = _out(o, "dw_gate", (N, K), x.dtype, dev) if want_dw else None
-    dwu = _out(o, "dw_up", (N, K), x.dtype, dev) if want_dw else None
+    dx = _out(o, "dx", (M, K), t, dev) if want_dx else None
+    dwg = _out(o, "dw_gate", (N, K), t, dev) if want_dw else None
+    dwu = _out(o, "dw_up", (N, K), t, dev) if want_dw else None
     dbg = _out(o, "db_gate", (N,), f32, dev) if want_db else None
     dbu = _out(o, "db_up", (N,), f32, dev) if want_db else None
-    need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | dh.data_ptr()) & 15)
+    need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, ((_ptr(x) or 0) | (_ptr(w_gate) or 0) | (_ptr(w_up) or 0) | dh.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(a), _ptr(u), _ptr(dh), M, K, N, int(act), dtype, dx, dwg, dwu, dbg,
+    args = (_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(a), _ptr(u), dh.data_ptr(), M, K, N, int(act), dtype, dx, dwg, dwu, dbg,
             dbu, ws, wsb, handle)
     call = (_lib or load_library()).tfla_gated_bwd
     rc = call(*args) if dev == device() else _elsewhere(dev, call, args)

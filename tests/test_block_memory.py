@@ -356,3 +356,23 @@ def test_the_cells_calls_on_another_stream(machine, name):
     call, inputs = cell_calls()[name]
     call()
     assert machine.calls[-1][1][-1] == 0 and not any(t.seen for t in inputs)
+
+
+# ---- backward calls need the tensors that they read -----------------------------------------------------------------
+def test_backward_calls_take_what_they_read(machine):
+    M, K, N = 40, 24, 16
+    x, w, w2, dy, a, u = (Tensor(s) for s in ((M, K), (N, K), (N, K), (M, N), (M, N), (M, N)))
+    both = ((lambda x, w, **k: tfla.linear_bwd(x, w, dy, **k), ("dx", "dw", "db")),
+            (lambda x, w, **k: tfla.gated_bwd(x, w, None if w is None else w2, a, u, dy, **k), ("dx", "dw_gate", "db_gate")))
+    for call, (dx, dw, db) in both:
+        o = call(None, w, want_dw=False)
+        assert o[dx].shape == (M, K) and machine.calls[-1][1][0] is None
+        o = call(x, None, want_dx=False, want_db=True)
+        assert o[dw].shape == (N, K) and machine.calls[-1][1][1] is None
+        o = call(None, None, want_dx=False, want_dw=False, want_db=True)
+        assert o[db].shape == (N,) and dx not in o and dw not in o
+        n = len(machine.calls)
+        for bad in (dict(x=None, w=w), dict(x=x, w=None), dict(x=None, w=None, want_dw=False), dict(x=None, w=None, want_dx=False)):
+            with pytest.raises(ValueError):
+                call(bad.pop("x"), bad.pop("w"), **bad)
+        assert len(machine.calls) == n

@@ -52,3 +52,20 @@ def test_bias_gradients_alone_store_only_sums(tfla, dtype, M, N, pair):
     else:
         tfla.linear_bwd(x, w, dy, z, want_dx=False, want_dw=False, workspace=ws, act=tfla.ACT_SILU)
     assert bool((ws == 0xA5).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,K,N", [(20, 72, 88), (300, 333, 129)])
+def test_gradients_without_the_tensors_that_they_do_not_read(tfla, dtype, M, K, N):
+    print("without", M, K, N, dtype, flush=True)
+    gen = generator(M + N)
+    x, w, w2, z, u, dy = (normal(gen, *s, dtype=dtype) for s in ((M, K), (N, K), (N, K), (M, N), (M, N), (M, N)))
+    kw = dict(act=tfla.ACT_SILU, want_db=True)
+    full = tfla.linear_bwd(x, w, dy, z, **kw)
+    for o in (tfla.linear_bwd(None, w, dy, z, want_dw=False, **kw), tfla.linear_bwd(x, None, dy, z, want_dx=False, **kw),
+              tfla.linear_bwd(None, None, dy, z, want_dx=False, want_dw=False, **kw)):
+        assert all(torch.equal(o[k], full[k]) for k in o if k != "workspace")
+    full = tfla.gated_bwd(x, w, w2, z, u, dy, **kw)
+    for o in (tfla.gated_bwd(None, w, w2, z, u, dy, want_dw=False, **kw), tfla.gated_bwd(x, None, None, z, u, dy, want_dx=False, **kw),
+              tfla.gated_bwd(None, None, None, z, u, dy, want_dx=False, want_dw=False, **kw)):
+        assert all(torch.equal(o[k], full[k]) for k in o if k != "workspace")
