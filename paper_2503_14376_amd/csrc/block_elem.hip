@@ -144,47 +144,6 @@ hipError_t launch_act_bwd(const ActBwdArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// How a product is cut: the tile and the number of parts with the shortest time by a model of the kernels, measured on products
-// of 40 to 8192 rows and columns (forward, both backward layouts; of 160 random ones 2 % above the best of all choices on average,
-// 23 % at most).  In us, with w
-// workgroups in all, n = ceil(w / 256) of them per CU one after another or side by side, and t steps each:
-//   bf16   256 x 256   8 + n (t (1.0 + 0.45 min(1, w / 256)) + 4)        (the power that all CUs draw lowers the clock)
-//          256 x 128   7 + n (t (0.63 + 0.31 min(1, w / 256)) + 2)
-//          128 x 128   5 + t (0.42 + 0.15 w / 256) up to 256 workgroups, 6 + 0.49 t n + 1.5 max(0, n - 2) above
-//          64 x 64     4.8 + 0.177 t n + 0.9 max(0, n - 2)               (pairs: 64 x 128, 0.34 t n)
-//   fp32   128 x 128   7 + max(2.3, 2.1 n) t     (steps of 32)
-//          64 x 64     5.5 + max(0.68, 0.57 n) t (pairs: 64 x 128, twice that)
-//          32 x 32     4.8 + max(0.4, 0.34 n) t  (steps of 64; pairs: 32 x 64, 1.9 times that)
-//   joining the parts  4.2 + (bytes written and read again) / 7 MB per us
-GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype) {
-    struct Tile { int bm, bn; };
-    static constexpr Tile bf16_tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}}, f32_tiles[] = {{128, 128}, {64, 64}, {32, 32}};
-    const bool b16 = dtype == 1;
-    const Tile* tiles = b16 ? bf16_tiles : f32_tiles;
-    const int kinds = b16 ? 4 : 3;
-    GemmPlan best{};
-    for (int i = 0; i < kinds; ++i) {
-        int bm = tiles[i].bm, bn = tiles[i].bn;
-        if (pair && bm <= 64 && bn == bm) bn = 2 * bm;
-        const int bno = pair ? bn / 2 : bn;
-        const int step = !b16 && bm > 32 ? 32 : 64, all = (K + step - 1) / step * segs;
-        const double cells = (double)((M + bm - 1) / bm) * ((N + bno - 1) / bno) * batch;
-        for (int split = 1; split <= 32 && (split == 1 || (all >= 4 * split && cells * split <= 1024)); split += split < 4 ? 1 : split / 2) {
-            const double w = cells * split, t = (all + split - 1) / split, part = w < 256 ? w / 256 : 1, n = (double)(long)((w + 255) / 256);
-            const double more = n > 2 ? n - 2 : 0;
-            double us;
-            if (!b16) us = bm == 128 ? 7 + (n < 2 ? 2.3 : 2.1 * n) * t : (bm == 64 ? 5.5 + (n < 2 ? 0.68 : 0.57 * n) * t * (pair ? 2 : 1) : 4.8 + (n < 2 ? 0.4 : 0.34 * n) * t * (pair ? 1.9 : 1));
-            else if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
-            else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
-            else if (bm == 128) us = n < 2 ? 5 + t * (0.42 + 0.15 * part) : 6 + 0.49 * t * n + 1.5 * more;
-            else us = 4.8 + (pair ? 0.34 : 0.177) * t * n + 0.9 * more;
-            if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
-            if (best.bm == 0 || us < best.us) best = {bm, bn, split, us};
-        }
-    }
-    return best;
-}
-
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s) {
     const int e = a.split > 1 ? EPI_PART : epi;
     hipError_t rc;
@@ -194,23 +153,6 @@ hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_t
     return a.dtype == 1 ? reduce<bf16_t>(a, epi, s) : reduce<float>(a, epi, s);
 }
 
-BothSteps both_steps(long M, int K, int N, int pair) {
-    auto up = [](long v) { return (v + 63) / 64; };
-    const long segs = pair ? 2 : 1, nx = up(M) * up(K), nw = up(N) * up(K) * segs, tx = up(N) * segs, tw = up(M);
-    return {nx + nw, tx > tw ? tx : tw, nx * tx + nw * tw};
-}
-// What a launch costs beside its work (3.4 us of the host's time, 2 of the GPU's) is saved once, and the items of one product fill
-// what the other leaves of the CUs' time.  Only of products whose contraction is not divided.  fp32: where both take the same
-// small tile.  bf16: by an estimate of the launch of both, fitted as that of single products, against the sum of theirs and 6 us
-// (both, one after the other: 1888 x 776 x 2640 39.3, 51.3 us; 368 x 1248 x 2232 20.9, 26.0; 1024 x 4096 x 4096 some 130, 87).
-bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K, int N, int pair, int dtype) {
-    if (x.split != 1 || w.split != 1) return false;
-    if (dtype != 1) return x.bm == w.bm && x.bm <= 64;
-    const BothSteps b = both_steps(M, K, N, pair);
-    const double share = b.sum / 256.0, chain = (b.items > 256 ? 0.4 : 0.2) * b.longest;
-    const double us = b.wide() ? 9 + 0.225 * share : 7.5 + (0.29 * share > chain ? 0.29 * share : chain);
-    return us <= x.us + w.us + 6;
-}
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s) {
     return x.dtype == 1 ? launch_gemm_both_as<1>(x, w, 64, s) : launch_gemm_both_as<0>(x, w, p.bm, s);
 }

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 
+#include "gemm_plan.h"
+
 namespace tfla {
 
 // ---- norm over D columns ---------------------------------------------------------------------
@@ -45,27 +47,11 @@ struct GemmArgs {
     // (split, batch or pair, M, ld_part); gemm_reduce adds them in order and applies the epilogue.
     float* part; long ld_part; int split;
 };
-// how a product is cut (a rule on its sizes): used for the workspace and by the launcher
-struct GemmPlan { int bm, bn, split; double us; };      // us: time by the model
-GemmPlan gemm_plan(long M, int N, int K, int segs, int batch, int pair, int dtype);
-// Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens, where gemm_rows_applies;
-// copies: the tiles would need the weights copied)
-constexpr int GEMM_ROWS_MAX = 32;
-bool gemm_rows_applies(long M, int N, int K, int pair, int dtype, bool copies);
+// Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens, where gemm_rows_applies)
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s);
 
-// dx = dz W and dw = dz^T x in one launch, where gemm_both_applies: both whole, in the same small tiles.  In tiles of 64 x 64 that
-// is `items` workgroups with the longest contraction of `longest` steps and `sum` steps in all.
-// Tiles of 64 x 128 bring three quarters of the operands' bytes into LDS, which is what bounds these launches, but have half the
-// workgroups: taken where the longest of them is at most half of an even share of the steps (2952 x 896 x 3088 65.9 us against
-// 82.9, 944 x 1624 x 1360 25.2 against 30.3; with a longest of a whole share 512 x 1024 x 1365, a pair, 26.3 against 22.3).
-struct BothSteps {
-    long items, longest, sum;
-    bool wide() const { return items > 512 && 2 * longest * 256 <= sum; }
-};
-BothSteps both_steps(long M, int K, int N, int pair);
-bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K, int N, int pair, int dtype);
+// dx = dz W and dw = dz^T x in one launch, where gemm_both_applies: both whole, in the same small tiles
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s);
 
 // ---- elementwise passes around the products ---------------------------------------------------

@@ -16,7 +16,8 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     constexpr bool ATR = L == 2, BTR = L >= 1;
     const int bno = PAIR ? p.bn / 2 : p.bn;
     const int tms = (a.M + p.bm - 1) / p.bm, tns = (a.N + bno - 1) / bno;
-    const unsigned n = (unsigned)((long)tms * tns * a.split * a.batch);
+    const unsigned n = (unsigned)gemm_workgroups(p, a.M, a.N, a.batch, PAIR);
+    const bool many = gemm_many(n);
 #if TFLA_GEMM >= 4
     // (the pair's tiles cover as many columns of each matrix)
     if (p.bm == 128) hipLaunchKernelGGL((gemm_f32_kernel<128, 128, 2, 2, 1, 32, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
@@ -29,15 +30,15 @@ template <bool PAIR, int EPI> void go(const GemmArgs& a, const GemmPlan& p, hipS
     // 128 x 128: two workgroups on a CU, or one with eight wavefronts and three steps under way instead of one (1024 x 4096 x 4096
     // 64 us with four wavefronts and one step, 46 with three, 44.5 with eight as well)
     else if (p.bm == 128) {
-        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        if (many) hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 2, 2, 2, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
         else hipLaunchKernelGGL((gemm_bf16_kernel<128, 128, 4, 2, 4, 1, ATR, BTR, PAIR, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
     }
     // 64 rows: two groups of wavefronts where no CU gets a second workgroup
     else if constexpr (PAIR) {
-        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 1, ATR, BTR, true, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        if (many) hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 1, ATR, BTR, true, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
         else hipLaunchKernelGGL((gemm_bf16_kernel<64, 128, 2, 2, 3, 2, ATR, BTR, true, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
     } else {
-        if (n > 256) hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 3, 1, ATR, BTR, false, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
+        if (many) hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 3, 1, ATR, BTR, false, EPI>), dim3(n), dim3(256), 0, s, a, tms, tns);
         else hipLaunchKernelGGL((gemm_bf16_kernel<64, 64, 2, 2, 4, 2, ATR, BTR, false, EPI>), dim3(n), dim3(512), 0, s, a, tms, tns);
     }
 #endif
@@ -80,7 +81,7 @@ template <> hipError_t launch_gemm_both_as<TFLA_GEMM == 3>(const GemmArgs& x, co
     if (both_steps(x.M, x.N, x.K, x.segs == 2).wide()) {
         cut(128);
         hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 128, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
-    } else if (all > 256) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
+    } else if (gemm_many(all)) hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 3, 1>), dim3(all), dim3(256), 0, s, x, w, g);
     else hipLaunchKernelGGL((gemm_bf16_both_kernel<64, 64, 2, 2, 4, 2>), dim3(all), dim3(512), 0, s, x, w, g);
 #else
     if (bm == 64) hipLaunchKernelGGL((gemm_f32_both_kernel<64, 64, 2, 2, 1, 32, 2>), dim3(all), dim3(256), 0, s, x, w, g);

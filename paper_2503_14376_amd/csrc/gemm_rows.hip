@@ -125,53 +125,31 @@ __global__ void __launch_bounds__(NW * 64) gemm_rows_kernel(GemmArgs a, int bloc
     }
 }
 
-// Wavefronts: as many as leave each of them four pieces, up to eight; sixteen for few blocks with more to read.  As many
-// pieces in flight as their registers hold.  Workgroups: one per block, where x is held as many as the chip runs at a time.
-template <typename DT, int MB, int SL, bool PAIR, int EPI, int NW, int U> void launch(const GemmArgs& a, int n, int ps, hipStream_t s) {
-    const int most = 256 * (NW <= 4 ? 4 : 2);
-    if (NW <= 8 && ps <= NW * U && n > most) hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, (NW <= 8)>), dim3(most), dim3(NW * 64), 0, s, a, n);
-    else hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, false>), dim3(n), dim3(NW * 64), 0, s, a, n);
+// As many pieces in flight as the wavefronts' registers hold (of eight wavefronts U8, of sixteen U16).
+template <typename DT, int MB, int SL, bool PAIR, int EPI, int NW, int U> void launch(const GemmArgs& a, const RowsPlan& p, hipStream_t s) {
+    if constexpr (NW <= 8) {
+        if (p.hold) {
+            hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, true>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((gemm_rows_kernel<DT, MB, SL, PAIR, EPI, NW, U, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
 }
-template <typename DT, int MB, int SL, bool PAIR, int EPI> void go(const GemmArgs& a, hipStream_t s) {
-    constexpr int V = sizeof(DT) / 2 * (MB * (PAIR ? 2 : 1) < 4 ? 1 : 2), U8 = V == 4 ? 2 : 4, U16 = 4 / V;
-    const int n = (a.N + 16 / SL - 1) / (16 / SL), ps = ((a.K + 63) / 64 + SL - 1) / SL;
-    if (ps <= 16) launch<DT, MB, SL, PAIR, EPI, 4, U8>(a, n, ps, s);
-    else if (n >= 128 || ps <= 32) launch<DT, MB, SL, PAIR, EPI, 8, U8>(a, n, ps, s);
-    else launch<DT, MB, SL, PAIR, EPI, 16, U16>(a, n, ps, s);
-}
-// Slices where blocks of 16 rows leave CUs without work: fewer than 256, or a last round that is not full (one token through
-// 4096 x 4096, 256 blocks: 8.3 us whole, 9.0 in four slices; 684 blocks of a pair: 41.5 and 37.5).
-int slices(long M, int N) {
-    const int n = (N + 15) / 16, rounds = (n + 255) / 256;
-    const bool uneven = n < 256 || (rounds < 8 && 256 * rounds * 10 > 11 * n);
-    return !uneven || M > 8 ? 1 : (M <= 4 ? 4 : 2);
+template <typename DT, int MB, int SL, bool PAIR, int EPI> void go(const GemmArgs& a, const RowsPlan& p, hipStream_t s) {
+    constexpr int V = rows_registers(sizeof(DT), MB, PAIR), U8 = rows_pieces(V, 8), U16 = rows_pieces(V, 16);
+    if (p.waves == 4) launch<DT, MB, SL, PAIR, EPI, 4, U8>(a, p, s);
+    else if (p.waves == 8) launch<DT, MB, SL, PAIR, EPI, 8, U8>(a, p, s);
+    else launch<DT, MB, SL, PAIR, EPI, 16, U16>(a, p, s);
 }
 template <typename DT, bool PAIR, int EPI> void by_rows(const GemmArgs& a, hipStream_t s) {
-    const int sl = slices(a.M, a.N);
-    if (sl == 4) go<DT, 1, 4, PAIR, EPI>(a, s);
-    else if (sl == 2) go<DT, 1, 2, PAIR, EPI>(a, s);
-    else if (a.M <= 16) go<DT, 1, 1, PAIR, EPI>(a, s);
-    else go<DT, 2, 1, PAIR, EPI>(a, s);
+    const RowsPlan p = rows_plan(a.M, a.N, a.K, PAIR, sizeof(DT));
+    if (p.slices == 4) go<DT, 1, 4, PAIR, EPI>(a, p, s);
+    else if (p.slices == 2) go<DT, 1, 2, PAIR, EPI>(a, p, s);
+    else if (p.row_blocks == 1) go<DT, 1, 1, PAIR, EPI>(a, p, s);
+    else go<DT, 2, 1, PAIR, EPI>(a, p, s);
 }
 
 }  // namespace
-
-// Whether this kernel takes a product or the tiles of gemm_plan do.  Every block of rows reads all of x again, which tiles of 64
-// do a quarter as often; tiles need some us more until all CUs have work, and weights that they cannot read in place are
-// copied first.  By estimates of both: here rounds of blocks at 27 GB/s per CU (fewer blocks than CUs: 35; fp32 some 10 % less),
-// there the plan's time, or the weights at the rate of a copy where that is longer.  Measured, here and there:
-// 4096 x 4096, 16 rows 11.8 and 12.2, 32 rows 15.8 and 12.9; pair of 10944 x 4096, 4 rows 38.1 and 39.1, 8 rows 44.9 and 39.5, 32
-// rows 62.9 and 40.6; pair of 2752 x 1024, 32 rows 7.5 and 9.3.
-bool gemm_rows_applies(long M, int N, int K, int pair, int dtype, bool copies) {
-    if (M <= 4 || M > GEMM_ROWS_MAX) return M <= 4;
-    if (copies) return true;
-    const double row = (double)K * (dtype == 1 ? 2 : 4);
-    const int rows = 16 / slices(M, N), n = (N + rows - 1) / rows;
-    const double rate = (dtype == 1 ? 27e3 : 24e3) * (n < 256 ? 1.3 : 1.0);
-    const double here = 1.8 + (n + 255) / 256 * (rows * (pair ? 2 : 1) + M) * row / rate;
-    const double there = gemm_plan(M, N, K, 1, 1, pair, dtype).us, read = 5 + (pair ? 2 : 1) * row * N / 5.2e6;
-    return here <= (there > read ? there : read);
-}
 
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s) {
     if (a.dtype == 1) {
