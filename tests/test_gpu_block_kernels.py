@@ -106,3 +106,57 @@ def test_product(tfla, i):
         for name, ref in (("dx", dx), ("dw", dw[0]), ("db", db[0])):
             bu.within(name, o[name], *ref)
     fences.intact()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,D", [(1, 1), (3, 7), (2, 511), (9, 512), (5, 777), (33, 1024), (40, 1365), (9, 2049), (700, 4096), (6, 4104), (3, 8191),
+                                 (2, 10000), (600, 100)])
+def test_norm_between_fences(tfla, dtype, M, D):
+    print("norm", M, D, dtype, flush=True)
+    gen, fences, shift = generator(M + D), Fences(), (M + D) % 3
+    x, dy, res = (fenced(normal(gen, M, D, dtype=dtype), shift) for _ in range(3))
+    gamma, beta = (fenced(normal(gen, D), shift) for _ in range(2))
+    o = outputs(fences, shift, dtype, y=(M, D), rstd=(M,), mean=(M,))
+    tfla.norm_fwd(x, gamma, beta, norm_kind=tfla.NORM_LAYER, norm_eps=1e-5, out=o)
+    mean, rstd, y = bu.norm(x, gamma, beta, True, 1e-5)
+    bu.within("mean", o["mean"], *mean)
+    if D > 1:                 # (a row of one value has no variance: rstd is eps's alone)
+        bu.within("rstd", o["rstd"], *rstd)
+    bu.within("y", o["y"], *y)
+    g = outputs(fences, shift, dtype, dx=(M, D), dgamma=(D,), dbeta=(D,))
+    need = tfla.norm_workspace_bytes(1, M, D, tfla.BF16 if dtype == BF16 else tfla.F32, tfla.NORM_LAYER)
+    tfla.norm_bwd(x, dy, o["rstd"], o["mean"], gamma, res, norm_kind=tfla.NORM_LAYER, want_dbeta=True, workspace=fences.workspace(need), out=g)
+    for name, ref in zip(("dx", "dgamma", "dbeta"), bu.norm_back(x, dy, o["rstd"], o["mean"], gamma, res, True)):
+        bu.within(name, g[name], *ref)
+    fences.intact()
+
+
+@pytest.mark.parametrize("shifts", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 2, 1)])
+@pytest.mark.parametrize("M,K,N", [(3, 72, 70), (40, 128, 264), (300, 264, 136), (270, 333, 129)])
+@pytest.mark.parametrize("pair", [False, True])
+def test_workspaces_of_copied_operands(tfla, shifts, M, K, N, pair):
+    """bf16 operands off 16 bytes, each alone: copies into a workspace of the size that the query names for them"""
+    print("copied", shifts, M, K, N, pair, flush=True)
+    gen, fences = generator(M), Fences()
+    x, w, w2 = (fenced(normal(gen, r, K, std=K ** -0.5, dtype=BF16), s) for r, s in ((M, shifts[0]), (N, shifts[1]), (N, shifts[1])))
+    a, u, dy = (fenced(normal(gen, M, N, dtype=BF16), s) for s in (0, 0, shifts[2]))
+    query = tfla.gated_workspace_bytes if pair else tfla.linear_workspace_bytes
+    need = [query(b, M, K, N, tfla.ACT_NONE, tfla.BF16, True) for b in (0, 1)]
+    kw = dict(act=tfla.ACT_NONE)
+    if pair:
+        o, g = outputs(fences, 1, BF16, h=(M, N)), outputs(fences, 1, BF16, dx=(M, K), dw_gate=(N, K), dw_up=(N, K))
+        tfla.gated_fwd(x, w, w2, workspace=fences.workspace(need[0]), out=o, **kw)
+        bu.within("h", o["h"], *bu.gated(x, w, w2, None, None, "none")[2])
+        tfla.gated_bwd(x, w, w2, a, u, dy, workspace=fences.workspace(need[1]), out=g, **kw)
+        d = [dy.to(bu.F64) * u.to(bu.F64), dy.to(bu.F64) * a.to(bu.F64)]
+        dx, dw, _ = bu.back(d, [bu.U * t.abs() for t in d], x, [w, w2], BF16)
+    else:
+        o, g = outputs(fences, 1, BF16, y=(M, N)), outputs(fences, 1, BF16, dx=(M, K), dw=(N, K))
+        tfla.linear_fwd(x, w, workspace=fences.workspace(need[0]), out=o, **kw)
+        bu.within("y", o["y"], *bu.linear(x, w, None, None, "none")[1])
+        tfla.linear_bwd(x, w, dy, workspace=fences.workspace(need[1]), out=g, **kw)
+        dx, dw, _ = bu.back([dy.to(bu.F64)], [torch.zeros_like(dy, dtype=bu.F64)], x, [w], BF16)
+    bu.within("dx", g["dx"], *dx)
+    for name, ref in zip(("dw_gate", "dw_up") if pair else ("dw",), dw):
+        bu.within(name, g[name], *ref)
+    fences.intact()
