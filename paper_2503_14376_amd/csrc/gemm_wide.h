@@ -187,8 +187,12 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_wide_kernel(GemmArgs a, int 
         }
         const bool full = wave_epilogue<bf16_t, EPI, PAIR, 4, 2 * NB>(a, done, drow, dcol, acc, lane);
         if (!more) break;
-        // the requests are older than the epilogue's operations, so its last stores need not have arrived
-        if (full) wait_vmcnt<8>();
+        // the requests are older than the epilogue's operations, so its last stores need not have arrived.  Of a whole tile every lane
+        // stores 4 x 2 NB blocks (a pair's two make one) in 16 bytes of two rows, or partial results in 16 words, at the least: a pair of
+        // BN = 128 without a and u has no store to spare.
+        constexpr int STORES = 4 * 2 * NB * (EPI == EPI_PART ? 16 : 2) / (PAIR && EPI != EPI_PART ? 2 : 1), NEWER = 8;
+        static_assert(STORES >= NEWER, "what may be under way is stores alone");
+        if (full) wait_vmcnt<NEWER>();
         else wait_vmcnt<0>();
     }
 #undef TFLA_REQUEST
