@@ -524,7 +524,9 @@ def _torch_types():
     if raw is None:
         def raw(device):
             return torch.cuda.current_stream(device).cuda_stream
-    _torch_names = (torch.bfloat16, torch.float32, raw, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
+    # (of a single device there is no other to be current)
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device) if torch.cuda.device_count() > 1 else None
+    _torch_names = (torch.bfloat16, torch.float32, raw, device)
     return _torch_names
 
 
@@ -554,9 +556,10 @@ def _rows(x, name, b16, f32):
 
 def _like(t, dtype, shape, name, dev):
     """shape: a tuple; None passes"""
-    if t is not None and (t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous()):
-        raise ValueError("%s must be a contiguous tensor of dtype %s and shape %s on cuda:%d (got %s %s on %s)"
-                         % (name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.device))
+    if t is None or (t.dtype == dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()):
+        return
+    raise ValueError("%s must be a contiguous tensor of dtype %s and shape %s on cuda:%d (got %s %s on %s)"
+                     % (name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.device))
 
 
 def _too_large(*sizes):
@@ -572,11 +575,12 @@ def _columns(x, w, want_dx, want_dw):
     return 1 if t is None else t.shape[-1]
 
 
-def _elsewhere(dev, call, args):
-    """the launching call with the tensors' device current, which another one is"""
+def _elsewhere(call, dev, names):
+    """call with its arguments (among the local names of its first lines) and the tensors' device current, which another one is"""
     import torch
+    code = call.__code__
     with torch.cuda.device(dev):
-        return call(*args)
+        return call(**{k: names[k] for k in code.co_varnames[:code.co_argcount]})
 
 
 def _out(o, name, shape, dtype, dev):
@@ -632,18 +636,22 @@ def norm_fwd(x, gamma=None, beta=None, norm_kind=NORM_RMS, norm_eps=1e-6, stream
         return _within(norm_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(norm_fwd, dev, locals())
     if (M | D) >> 31:
         _too_large(M, D)
+    gammap = betap = None
     if gamma is not None:
         _like(gamma, f32, (D,), "gamma", dev)
+        gammap = gamma.data_ptr()
     if beta is not None:
         _like(beta, f32, (D,), "beta", dev)
+        betap = beta.data_ptr()
     o = out if out is not None else {}
     y, rstd = _out(o, "y", (M, D), x.dtype, dev), _out(o, "rstd", (M,), f32, dev)
     mean = _out(o, "mean", (M,), f32, dev) if norm_kind == NORM_LAYER else None
-    args = (x.data_ptr(), _ptr(gamma), _ptr(beta), M, D, dtype, int(norm_kind), float(norm_eps), y, rstd, mean, raw_stream(dev))
-    call = (_lib or load_library()).tfla_norm_fwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_norm_fwd(x.data_ptr(), gammap, betap, M, D, dtype, int(norm_kind), float(norm_eps), y,
+                                                rstd, mean, raw_stream(dev))
     if rc != 0:
         raise TflaError(rc, "tfla_norm_fwd")
     return o
@@ -657,6 +665,8 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
         return _within(norm_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, D, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(norm_bwd, dev, locals())
     if (M | D) >> 31:
         _too_large(M, D)
     _like(dy, x.dtype, (M, D), "dy", dev); _like(d_residual, x.dtype, (M, D), "d_residual", dev); _like(gamma, f32, (D,), "gamma", dev)
@@ -668,10 +678,8 @@ def norm_bwd(x, dy, rstd, mean=None, gamma=None, d_residual=None, norm_kind=NORM
     dbeta = _out(o, "dbeta", (D,), f32, dev) if want_dbeta else None
     need = norm_workspace_bytes(BWD, M, D, dtype, int(norm_kind)) if want_dgamma or want_dbeta else 0
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D, dtype, int(norm_kind), dx, dgamma,
-            dbeta, ws, wsb, handle)
-    call = (_lib or load_library()).tfla_norm_bwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_norm_bwd(x.data_ptr(), _ptr(dy), _ptr(rstd), _ptr(mean), _ptr(gamma), _ptr(d_residual), M, D,
+                                                dtype, int(norm_kind), dx, dgamma, dbeta, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_norm_bwd")
     return o
@@ -685,6 +693,8 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
         return _within(linear_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(linear_fwd, dev, locals())
     N = w.shape[0]
     if (M | K | N) >> 31:
         _too_large(M, K, N)
@@ -699,9 +709,8 @@ def linear_fwd(x, w, bias=None, residual=None, act=ACT_NONE, keep_pre=False, wor
     z = _out(o, "z", (M, N), x.dtype, dev) if keep_pre else None
     need = linear_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z, ws, wsb, handle)
-    call = (_lib or load_library()).tfla_linear_fwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_linear_fwd(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), M, K, N, int(act), dtype, y, z,
+                                                  ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_fwd")
     return o
@@ -715,6 +724,8 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
         return _within(linear_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, N, dev = _rows(dy, "dy", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(linear_bwd, dev, locals())
     K = _columns(x, w, want_dx, want_dw)
     if (M | K | N) >> 31:
         _too_large(M, K, N)
@@ -727,9 +738,8 @@ def linear_bwd(x, w, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_
     db = _out(o, "db", (N,), f32, dev) if want_db else None
     need = linear_workspace_bytes(BWD, M, K, N, int(act), dtype, ((_ptr(x) or 0) | (_ptr(w) or 0) | dy.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (_ptr(x), _ptr(w), dy.data_ptr(), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws, wsb, handle)
-    call = (_lib or load_library()).tfla_linear_bwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_linear_bwd(_ptr(x), _ptr(w), dy.data_ptr(), _ptr(z), M, K, N, int(act), dtype, dx, dw, db, ws,
+                                                  wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_linear_bwd")
     return o
@@ -743,6 +753,8 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
         return _within(gated_fwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, K, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(gated_fwd, dev, locals())
     N = w_gate.shape[0]
     if (M | K | N) >> 31:
         _too_large(M, K, N)
@@ -755,9 +767,8 @@ def gated_fwd(x, w_gate, w_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=Fa
     u = _out(o, "u", (M, N), x.dtype, dev) if keep_pre else None
     need = gated_workspace_bytes(FWD, M, K, N, int(act), dtype, (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act), dtype, h, a, u, ws, wsb, handle)
-    call = (_lib or load_library()).tfla_gated_fwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_gated_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N,
+                                                 int(act), dtype, h, a, u, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_fwd")
     return o
@@ -771,6 +782,8 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
         return _within(gated_bwd, stream, locals())
     b16, f32, raw_stream, device = _torch_names or _torch_types()
     dtype, M, N, dev = _rows(dh, "dh", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(gated_bwd, dev, locals())
     K = _columns(x, w_gate, want_dx, want_dw)
     if (M | K | N) >> 31:
         _too_large(M, K, N)
@@ -786,10 +799,8 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
     dbu = _out(o, "db_up", (N,), f32, dev) if want_db else None
     need = gated_workspace_bytes(BWD, M, K, N, int(act), dtype, ((_ptr(x) or 0) | (_ptr(w_gate) or 0) | (_ptr(w_up) or 0) | dh.data_ptr()) & 15)
     ws, wsb = _scratch(o, workspace, need, dev, handle)
-    args = (_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(a), _ptr(u), dh.data_ptr(), M, K, N, int(act), dtype, dx, dwg, dwu, dbg,
-            dbu, ws, wsb, handle)
-    call = (_lib or load_library()).tfla_gated_bwd
-    rc = call(*args) if dev == device() else _elsewhere(dev, call, args)
+    rc = (_lib or load_library()).tfla_gated_bwd(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(a), _ptr(u), dh.data_ptr(), M, K, N, int(act),
+                                                 dtype, dx, dwg, dwu, dbg, dbu, ws, wsb, handle)
     if rc != 0:
         raise TflaError(rc, "tfla_gated_bwd")
     return o

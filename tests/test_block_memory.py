@@ -95,6 +95,7 @@ class Machine:
         monkeypatch.setattr(torch.cuda, "device", on_device)
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.streams[index(device)])
         monkeypatch.setattr(torch.cuda, "current_device", lambda: self.device)
+        monkeypatch.setattr(torch.cuda, "device_count", lambda: len(self.streams))
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: self.streams[d].cuda_stream, raising=False)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: self.device, raising=False)
         monkeypatch.setattr(binding, "_torch_names", None)
