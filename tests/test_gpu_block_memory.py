@@ -69,3 +69,36 @@ def test_gradients_without_the_tensors_that_they_do_not_read(tfla, dtype, M, K, 
     for o in (tfla.gated_bwd(None, w, w2, z, u, dy, want_dw=False, **kw), tfla.gated_bwd(x, None, None, z, u, dy, want_dx=False, **kw),
               tfla.gated_bwd(None, None, None, z, u, dy, want_dx=False, want_dw=False, **kw)):
         assert all(torch.equal(o[k], full[k]) for k in o if k != "workspace")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_dropped_tensor_is_not_written_from_another_stream(tfla, dtype):
+    """work on the current stream still reads a tensor that was dropped; a call on another stream, whose output has that tensor's size,
+    must not be given its memory"""
+    print("dropped", dtype, flush=True)
+    gen = generator(5)
+    M, K, N = 2048, 256, 2056
+    x, w = normal(gen, M, K, dtype=dtype), normal(gen, N, K, std=0.1, dtype=dtype)
+    want = tfla.linear_fwd(x, w)["y"]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()                             # (no other block that the current stream's pool could give)
+    old, kept, total = (torch.empty((M, N), dtype=d, device="cuda") for d in (dtype, dtype, F32))
+    old.normal_(generator=gen)
+    kept.copy_(old)
+    total.zero_()
+    torch.cuda.synchronize()
+    for _ in range(50):
+        total += old
+    address = old.data_ptr()
+    del old
+    o = tfla.linear_fwd(x, w, stream=side)
+    assert o["y"].data_ptr() != address
+    again = torch.empty((M, N), dtype=dtype, device="cuda")
+    assert again.data_ptr() == address                   # (the current stream may well use it again)
+    torch.cuda.synchronize()
+    assert torch.equal(o["y"], want)
+    ref = torch.zeros((M, N), device="cuda")
+    for _ in range(50):
+        ref += kept
+    assert torch.equal(total, ref)
