@@ -178,6 +178,8 @@ def _stream_handle(stream=None):
 def _within(call, stream, args):
     """call(**args), args with stream among them, on `stream`"""
     import torch
+    if not hasattr(stream, "device"):       # (anything with a handle will do)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
     device = stream.device.index
     given = [t for t in (*args.values(), *(args.get("out") or {}).values()) if hasattr(t, "record_stream")]
     for t in given:

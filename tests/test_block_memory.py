@@ -377,3 +377,13 @@ def test_backward_calls_take_what_they_read(machine):
             with pytest.raises(ValueError):
                 call(bad.pop("x"), bad.pop("w"), **bad)
         assert len(machine.calls) == n
+
+
+@pytest.mark.parametrize("name", ("linear_fwd", "layer_fwd"))
+def test_a_stream_may_be_anything_with_a_handle(machine, monkeypatch, name):
+    class Handle:
+        cuda_stream = 96
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    call, _ = {**calls(), **cell_calls()}[name]
+    o = call(stream=Handle())
+    assert machine.calls[-1][1][-1] == 96 and all(t.pool.cuda_stream == 96 for t in tensors(o).values())
