@@ -21,7 +21,8 @@ EXPORTS = ("tfla_mlstm_fwd", "tfla_mlstm_bwd", "tfla_mlstm_step", "tfla_mlstm_wo
            "tfla_transfer_gain", "tfla_mlstm_layer_step", "tfla_tile_width", "tfla_mlstm_fwd_static",
            "tfla_static_scratch_bytes", "tfla_norm_workspace_bytes", "tfla_norm_fwd", "tfla_norm_bwd",
            "tfla_linear_workspace_bytes", "tfla_linear_fwd", "tfla_linear_bwd", "tfla_gated_workspace_bytes",
-           "tfla_gated_fwd", "tfla_gated_bwd")
+           "tfla_gated_fwd", "tfla_gated_bwd", "tfla_q8_quant", "tfla_norm_q8_fwd", "tfla_linear_q8_workspace_bytes",
+           "tfla_linear_q8_fwd", "tfla_linear_q8_bwd", "tfla_gated_q8_workspace_bytes", "tfla_gated_q8_fwd", "tfla_gated_q8_bwd")
 
 
 class TflaError(RuntimeError):
@@ -104,6 +105,22 @@ def load_library():
     lib.tfla_gated_fwd.argtypes = [vp, vp, vp, fp, fp, ci, ci, ci, ci, ci, vp, vp, vp, vp, sz, vp]
     lib.tfla_gated_bwd.restype = ci
     lib.tfla_gated_bwd.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, fp, fp, vp, sz, vp]
+    lib.tfla_q8_quant.restype = ci
+    lib.tfla_q8_quant.argtypes = [vp, ci, ci, ci, ci, vp, vp, vp, vp, vp]
+    lib.tfla_norm_q8_fwd.restype = ci
+    lib.tfla_norm_q8_fwd.argtypes = [vp, fp, fp, vp, ci, ci, ci, ci, cf, vp, vp, vp, vp, fp, fp, vp]
+    lib.tfla_linear_q8_workspace_bytes.restype = sz
+    lib.tfla_linear_q8_workspace_bytes.argtypes = [ci] * 6
+    lib.tfla_linear_q8_fwd.restype = ci
+    lib.tfla_linear_q8_fwd.argtypes = [vp, vp, vp, vp, fp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp]
+    lib.tfla_linear_q8_bwd.restype = ci
+    lib.tfla_linear_q8_bwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, fp, vp, sz, vp]
+    lib.tfla_gated_q8_workspace_bytes.restype = sz
+    lib.tfla_gated_q8_workspace_bytes.argtypes = [ci] * 6
+    lib.tfla_gated_q8_fwd.restype = ci
+    lib.tfla_gated_q8_fwd.argtypes = [vp, vp, vp, vp, vp, vp, fp, fp, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tfla_gated_q8_bwd.restype = ci
+    lib.tfla_gated_q8_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, fp, fp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -806,3 +823,241 @@ def gated_bwd(x, w_gate, w_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=Tru
     if rc != 0:
         raise TflaError(rc, "tfla_gated_bwd")
     return o
+
+
+# ---- the residual block in 8 bits ------------------------------------------------------------------------------------------
+# Codes are tensors of type float8_e4m3fn, scales of type float8_e8m0fnu: one for 128 columns of a row, (blocks of columns, rows), or for
+# a block of 128 x 128, (blocks of columns, blocks of rows).  Everything else as for the block above.
+_q8_names = None
+
+
+def _q8_types():
+    global _q8_names
+    import torch
+    _q8_names = (torch.float8_e4m3fn, torch.float8_e8m0fnu)
+    return _q8_names
+
+
+def linear_q8_workspace_bytes(direction, M, K, N, act, unaligned=False) -> int:
+    return int((_lib or load_library()).tfla_linear_q8_workspace_bytes(direction, M, K, N, act, int(unaligned)))
+
+
+def gated_q8_workspace_bytes(direction, M, K, N, act, unaligned=False) -> int:
+    return int((_lib or load_library()).tfla_gated_q8_workspace_bytes(direction, M, K, N, act, int(unaligned)))
+
+
+def _codes(q, name, e4m3):
+    """(rows, columns) and device of a dense matrix of codes"""
+    shape = q.shape
+    dev = q.get_device()
+    if q.dtype != e4m3 or len(shape) != 2 or dev < 0 or not q.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor of two dimensions and dtype float8_e4m3fn (got %s %s)" % (name, q.dtype, tuple(shape)))
+    return shape[0], shape[1], dev
+
+
+def q8_quant(x, rows=1, want_q=True, want_t=False, stream=None, out: Optional[Dict] = None) -> Dict:
+    """tfla_q8_quant on torch device tensors.  x: (M, K) in bf16 or fp32; rows: 1 (activations: a scale for 128 columns of a row) or 128
+    (weights: one for a block of 128 x 128).  Returns q, scale and, with want_t, those of the transpose, qt, scale_t."""
+    if stream is not None:
+        return _within(q8_quant, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    dtype, M, K, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(q8_quant, dev, locals())
+    if (M | K) >> 31:
+        _too_large(M, K)
+    if rows != 1 and rows != 128:
+        raise ValueError("rows must be 1 or 128 (got %s)" % (rows,))
+    o = out if out is not None else {}
+    q = scale = qt = scale_t = None
+    if want_q:
+        q, scale = _out(o, "q", (M, K), e4m3, dev), _out(o, "scale", (-(-K // 128), -(-M // rows)), e8m0, dev)
+    if want_t:
+        qt, scale_t = _out(o, "qt", (K, M), e4m3, dev), _out(o, "scale_t", (-(-M // 128), -(-K // rows)), e8m0, dev)
+    rc = (_lib or load_library()).tfla_q8_quant(x.data_ptr(), M, K, dtype, rows, q, scale, qt, scale_t, raw_stream(dev))
+    if rc != 0:
+        raise TflaError(rc, "tfla_q8_quant")
+    return o
+
+
+def norm_q8_fwd(x, gamma=None, beta=None, residual=None, norm_kind=NORM_RMS, norm_eps=1e-6, keep_y=False, stream=None,
+                out: Optional[Dict] = None) -> Dict:
+    """tfla_norm_q8_fwd on torch device tensors: norm of x + residual, quantised.  x, residual: (M, D) in bf16 or fp32; gamma, beta: (D,)
+    fp32 or None.  Returns q, scale, rstd, (LayerNorm) mean, with a residual sum, and with keep_y y, the values before quantisation.
+    The gradient of x and residual is norm_bwd's dx for x = sum."""
+    if stream is not None:
+        return _within(norm_q8_fwd, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    dtype, M, D, dev = _rows(x, "x", b16, f32)
+    if device is not None and dev != device():
+        return _elsewhere(norm_q8_fwd, dev, locals())
+    if (M | D) >> 31:
+        _too_large(M, D)
+    t = x.dtype
+    gammap = betap = res = total = y = mean = None
+    if gamma is not None:
+        _like(gamma, f32, (D,), "gamma", dev)
+        gammap = gamma.data_ptr()
+    if beta is not None:
+        _like(beta, f32, (D,), "beta", dev)
+        betap = beta.data_ptr()
+    o = out if out is not None else {}
+    q, scale = _out(o, "q", (M, D), e4m3, dev), _out(o, "scale", (-(-D // 128), M), e8m0, dev)
+    rstd = _out(o, "rstd", (M,), f32, dev)
+    if residual is not None:
+        _like(residual, t, (M, D), "residual", dev)
+        res, total = residual.data_ptr(), _out(o, "sum", (M, D), t, dev)
+    if keep_y:
+        y = _out(o, "y", (M, D), t, dev)
+    if norm_kind == NORM_LAYER:
+        mean = _out(o, "mean", (M,), f32, dev)
+    rc = (_lib or load_library()).tfla_norm_q8_fwd(x.data_ptr(), gammap, betap, res, M, D, dtype, int(norm_kind), float(norm_eps), q, scale,
+                                                   total, y, rstd, mean, raw_stream(dev))
+    if rc != 0:
+        raise TflaError(rc, "tfla_norm_q8_fwd")
+    return o
+
+
+def linear_q8_fwd(xq, x_scale, wq, w_scale, bias=None, residual=None, act=ACT_NONE, keep_pre=False, workspace=None, stream=None,
+                  out: Optional[Dict] = None) -> Dict:
+    """tfla_linear_q8_fwd on torch device tensors.  xq, x_scale: (M, K) as norm_q8_fwd or q8_quant with rows = 1 returns them; wq, w_scale:
+    (N, K) as q8_quant with rows = 128; bias: (N,) fp32; residual: (M, N) bf16.  Returns y and, with keep_pre, z, in bf16."""
+    if stream is not None:
+        return _within(linear_q8_fwd, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    M, K, dev = _codes(xq, "xq", e4m3)
+    if device is not None and dev != device():
+        return _elsewhere(linear_q8_fwd, dev, locals())
+    N = wq.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
+    kb = -(-K // 128)
+    _like(x_scale, e8m0, (kb, M), "x_scale", dev); _like(wq, e4m3, (N, K), "wq", dev); _like(w_scale, e8m0, (kb, -(-N // 128)), "w_scale", dev)
+    if bias is not None:
+        _like(bias, f32, (N,), "bias", dev)
+    if residual is not None:
+        _like(residual, b16, (M, N), "residual", dev)
+    handle = raw_stream(dev)
+    o = out if out is not None else {}
+    y = _out(o, "y", (M, N), b16, dev)
+    z = _out(o, "z", (M, N), b16, dev) if keep_pre else None
+    need = linear_q8_workspace_bytes(FWD, M, K, N, int(act), (xq.data_ptr() | wq.data_ptr()) & 15)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
+    rc = (_lib or load_library()).tfla_linear_q8_fwd(xq.data_ptr(), x_scale.data_ptr(), wq.data_ptr(), w_scale.data_ptr(), _ptr(bias),
+                                                     _ptr(residual), M, K, N, int(act), y, z, ws, wsb, handle)
+    if rc != 0:
+        raise TflaError(rc, "tfla_linear_q8_fwd")
+    return o
+
+
+def linear_q8_bwd(x, wqt, wt_scale, dy, z=None, act=ACT_NONE, want_dx=True, want_dw=True, want_db=False, workspace=None, stream=None,
+                  out: Optional[Dict] = None) -> Dict:
+    """tfla_linear_q8_bwd on torch device tensors.  x: (M, K) bf16, what the forward call's codes were made of; wqt, wt_scale: the
+    transposed weights (K, N) as q8_quant with rows = 128 returns them; dy: (M, N) bf16; z: as linear_q8_fwd with keep_pre returned it, where
+    act is not ACT_NONE.  Returns dx, dw, db (those that are wanted).  x may be None without dw, wqt and wt_scale without dx."""
+    if stream is not None:
+        return _within(linear_q8_bwd, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    dtype, M, N, dev = _rows(dy, "dy", b16, b16)
+    if device is not None and dev != device():
+        return _elsewhere(linear_q8_bwd, dev, locals())
+    K = _q8_columns(x, wqt, wt_scale, want_dx, want_dw)
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
+    _like(x, b16, (M, K), "x", dev); _like(wqt, e4m3, (K, N), "wqt", dev); _like(z, b16, (M, N), "z", dev)
+    _like(wt_scale, e8m0, (-(-N // 128), -(-K // 128)), "wt_scale", dev)
+    handle = raw_stream(dev)
+    o = out if out is not None else {}
+    dx = _out(o, "dx", (M, K), b16, dev) if want_dx else None
+    dw = _out(o, "dw", (N, K), b16, dev) if want_dw else None
+    db = _out(o, "db", (N,), f32, dev) if want_db else None
+    need = linear_q8_workspace_bytes(BWD, M, K, N, int(act), (_ptr(wqt) or 0) & 15)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
+    rc = (_lib or load_library()).tfla_linear_q8_bwd(_ptr(x), _ptr(wqt), _ptr(wt_scale), dy.data_ptr(), _ptr(z), M, K, N, int(act), dx, dw,
+                                                     db, ws, wsb, handle)
+    if rc != 0:
+        raise TflaError(rc, "tfla_linear_q8_bwd")
+    return o
+
+
+def gated_q8_fwd(xq, x_scale, wq_gate, w_scale_gate, wq_up, w_scale_up, b_gate=None, b_up=None, act=ACT_SILU, keep_pre=False, workspace=None,
+                 stream=None, out: Optional[Dict] = None) -> Dict:
+    """tfla_gated_q8_fwd on torch device tensors: h = act(x w_gate^T + b_gate) * (x w_up^T + b_up) in 8 bits.  Codes and scales as for
+    linear_q8_fwd; b_gate, b_up: (N,) fp32.  Returns hq, h_scale, which linear_q8_fwd takes, and, with keep_pre, h, a and u in bf16."""
+    if stream is not None:
+        return _within(gated_q8_fwd, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    M, K, dev = _codes(xq, "xq", e4m3)
+    if device is not None and dev != device():
+        return _elsewhere(gated_q8_fwd, dev, locals())
+    N = wq_gate.shape[0]
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
+    kb, nb = -(-K // 128), -(-N // 128)
+    _like(x_scale, e8m0, (kb, M), "x_scale", dev)
+    _like(wq_gate, e4m3, (N, K), "wq_gate", dev); _like(w_scale_gate, e8m0, (kb, nb), "w_scale_gate", dev)
+    _like(wq_up, e4m3, (N, K), "wq_up", dev); _like(w_scale_up, e8m0, (kb, nb), "w_scale_up", dev)
+    _like(b_gate, f32, (N,), "b_gate", dev); _like(b_up, f32, (N,), "b_up", dev)
+    handle = raw_stream(dev)
+    o = out if out is not None else {}
+    hq, h_scale = _out(o, "hq", (M, N), e4m3, dev), _out(o, "h_scale", (nb, M), e8m0, dev)
+    h = a = u = None
+    if keep_pre:
+        h, a, u = _out(o, "h", (M, N), b16, dev), _out(o, "a", (M, N), b16, dev), _out(o, "u", (M, N), b16, dev)
+    need = gated_q8_workspace_bytes(FWD, M, K, N, int(act), (xq.data_ptr() | wq_gate.data_ptr() | wq_up.data_ptr()) & 15)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
+    rc = (_lib or load_library()).tfla_gated_q8_fwd(xq.data_ptr(), x_scale.data_ptr(), wq_gate.data_ptr(), w_scale_gate.data_ptr(),
+                                                    wq_up.data_ptr(), w_scale_up.data_ptr(), _ptr(b_gate), _ptr(b_up), M, K, N, int(act),
+                                                    hq, h_scale, h, a, u, ws, wsb, handle)
+    if rc != 0:
+        raise TflaError(rc, "tfla_gated_q8_fwd")
+    return o
+
+
+def gated_q8_bwd(x, wqt_gate, wt_scale_gate, wqt_up, wt_scale_up, a, u, dh, act=ACT_SILU, want_dx=True, want_dw=True, want_db=False,
+                 workspace=None, stream=None, out: Optional[Dict] = None) -> Dict:
+    """tfla_gated_q8_bwd on torch device tensors.  x: (M, K) bf16, what the forward call's codes were made of; the transposed weights (K, N)
+    as q8_quant with rows = 128 returns them; a, u: as gated_q8_fwd with keep_pre returned them; dh: (M, N) bf16.  Returns dx, dw_gate,
+    dw_up, db_gate, db_up (those that are wanted).  x may be None without the weights' gradients, the weights without dx."""
+    if stream is not None:
+        return _within(gated_q8_bwd, stream, locals())
+    b16, f32, raw_stream, device = _torch_names or _torch_types()
+    e4m3, e8m0 = _q8_names or _q8_types()
+    dtype, M, N, dev = _rows(dh, "dh", b16, b16)
+    if device is not None and dev != device():
+        return _elsewhere(gated_q8_bwd, dev, locals())
+    K = _q8_columns(x, wqt_gate, wt_scale_gate, want_dx, want_dw)
+    if want_dx and (wqt_up is None or wt_scale_up is None):
+        raise ValueError("the weights are needed for dx")
+    if (M | K | N) >> 31:
+        _too_large(M, K, N)
+    blocks = (-(-N // 128), -(-K // 128))
+    _like(x, b16, (M, K), "x", dev); _like(a, b16, (M, N), "a", dev); _like(u, b16, (M, N), "u", dev)
+    _like(wqt_gate, e4m3, (K, N), "wqt_gate", dev); _like(wt_scale_gate, e8m0, blocks, "wt_scale_gate", dev)
+    _like(wqt_up, e4m3, (K, N), "wqt_up", dev); _like(wt_scale_up, e8m0, blocks, "wt_scale_up", dev)
+    handle = raw_stream(dev)
+    o = out if out is not None else {}
+    dx = _out(o, "dx", (M, K), b16, dev) if want_dx else None
+    dwg = _out(o, "dw_gate", (N, K), b16, dev) if want_dw else None
+    dwu = _out(o, "dw_up", (N, K), b16, dev) if want_dw else None
+    dbg = _out(o, "db_gate", (N,), f32, dev) if want_db else None
+    dbu = _out(o, "db_up", (N,), f32, dev) if want_db else None
+    need = gated_q8_workspace_bytes(BWD, M, K, N, int(act), ((_ptr(wqt_gate) or 0) | (_ptr(wqt_up) or 0)) & 15)
+    ws, wsb = _scratch(o, workspace, need, dev, handle)
+    rc = (_lib or load_library()).tfla_gated_q8_bwd(_ptr(x), _ptr(wqt_gate), _ptr(wt_scale_gate), _ptr(wqt_up), _ptr(wt_scale_up), _ptr(a),
+                                                    _ptr(u), dh.data_ptr(), M, K, N, int(act), dx, dwg, dwu, dbg, dbu, ws, wsb, handle)
+    if rc != 0:
+        raise TflaError(rc, "tfla_gated_q8_bwd")
+    return o
+
+
+def _q8_columns(x, wqt, wt_scale, want_dx, want_dw):
+    """input columns of a backward call by the tensors that it reads"""
+    if (want_dw and x is None) or (want_dx and (wqt is None or wt_scale is None)):
+        raise ValueError("%s needed for the gradients that are wanted" % ("x is" if want_dw and x is None else "the weights and their scales are"))
+    return x.shape[-1] if x is not None else (1 if wqt is None else wqt.shape[0])

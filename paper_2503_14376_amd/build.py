@@ -19,6 +19,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 # vector ALU instructions, which cannot read accumulation registers)
 UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "step.o", []), ("norm.hip", "norm.o", []),
          ("block_api.hip", "block_api.o", []), ("block_elem.hip", "block_elem.o", []), ("rownorm.hip", "rownorm.o", []),
+         ("q8_api.hip", "q8_api.o", []), ("q8_quant.hip", "q8_quant.o", []),
+         ("q8_rows.hip", "q8_rows.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
          ("gemm_rows.hip", "gemm_rows.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
          ("recurrent.hip", "recurrent.o", ["-mllvm", "-amdgpu-mfma-vgpr-form"])] + [
     # tile kernels: the start-up loop over X and state slices must unroll completely (its items differ in kind and
@@ -29,7 +31,9 @@ UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "s
     ("tile_grads.hip", "tile_grads%d.o" % w, ["-DTFLA_GRADS_DQK=%d" % w, "-mllvm", "-pragma-unroll-threshold=200000",
                                               "-mllvm", "-amdgpu-mfma-vgpr-form"]) for w in (64, 128, 256)] + [
     # matrix products: operand layouts 0 - 2, two products in one launch 3, + 4 for fp32
-    ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l]) for l in range(8)]
+    ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l]) for l in range(8)] + [
+    # products in 8 bits, by what follows them
+    ("q8_gemm_inst.hip", "q8_gemm%d.o" % v, ["-DTFLA_Q8=%d" % v]) for v in range(4)]
 
 
 def _compile(unit):

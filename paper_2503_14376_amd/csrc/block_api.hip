@@ -2,6 +2,7 @@
 // columns, the linear projection and the gated projection pair.  See include/tfla_mlstm.h for the contract.
 #include "../../include/tfla_mlstm.h"
 #include "block_internal.h"
+#include "host_util.h"
 #include "profiler.h"
 
 using namespace tfla;
@@ -11,24 +12,12 @@ namespace {
 constexpr int MAX_ROWS = 1 << 24, MAX_COLS = 1 << 20, MAX_NORM_COLS = 16384;
 constexpr long MAX_ELEMS = 1L << 36;
 
-inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 inline size_t esize(int dtype) { return dtype == TFLA_BF16 ? 2 : 4; }
 // pitch of a row in the workspace: the passes that write there store eight elements at a time
 inline long padded(int n) { return (n + 7L) & ~7L; }
-inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 // whether a product's operand is copied into the workspace: the bf16 kernels bring rows into LDS by 16-byte requests, which
 // want addresses in multiples of that; the fp32 kernels read any rows in place (bwd 14251 x 5170 x 84: 359 us, 495 with a copy)
 inline bool moved(int cols, bool off, int dtype) { return dtype == TFLA_BF16 && (cols % 8 != 0 || off); }
-
-struct Carver {
-    char* base; size_t off = 0;
-    explicit Carver(void* p) : base(reinterpret_cast<char*>(p)) {}
-    char* take(size_t bytes) {
-        char* r = base ? base + off : nullptr;
-        off = align_up(off + bytes);
-        return r;
-    }
-};
 
 int check_norm(int M, int D, int dtype, int kind) {
     if (dtype != TFLA_F32 && dtype != TFLA_BF16) return TFLA_ERR_ENUM;
@@ -106,12 +95,6 @@ BwdLayout bwd_layout(int M, int K, int N, int act, int dtype, bool pair, bool dy
     l.part = c.off; c.take(pdx > pdw ? pdx : pdw);
     l.bytes = c.off;
     return l;
-}
-
-int check_workspace(const void* ws, size_t have, size_t need) {
-    if (need == 0) return TFLA_OK;
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || have < need) return TFLA_ERR_WORKSPACE;
-    return TFLA_OK;
 }
 
 int product_fwd(const void* x, const void* const (&w)[2], const float* const (&bias)[2], const void* residual, int M, int K, int N, int act,

@@ -150,8 +150,10 @@ hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_t
     if (a.dtype == 1) rc = !b_tr ? launch_gemm_layout<0>(a, p, e, s) : (!a_tr ? launch_gemm_layout<1>(a, p, e, s) : launch_gemm_layout<2>(a, p, e, s));
     else rc = !b_tr ? launch_gemm_layout<4>(a, p, e, s) : (!a_tr ? launch_gemm_layout<5>(a, p, e, s) : launch_gemm_layout<6>(a, p, e, s));
     if (rc != hipSuccess || e != EPI_PART) return rc;
-    return a.dtype == 1 ? reduce<bf16_t>(a, epi, s) : reduce<float>(a, epi, s);
+    return launch_gemm_reduce(a, epi, s);
 }
+
+hipError_t launch_gemm_reduce(const GemmArgs& a, int epi, hipStream_t s) { return a.dtype == 1 ? reduce<bf16_t>(a, epi, s) : reduce<float>(a, epi, s); }
 
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s) {
     return x.dtype == 1 ? launch_gemm_both_as<1>(x, w, 64, s) : launch_gemm_both_as<0>(x, w, p.bm, s);

@@ -50,6 +50,8 @@ struct GemmArgs {
 // Few rows against plain weights at any address and pitch (forward calls of up to GEMM_ROWS_MAX tokens, where gemm_rows_applies)
 hipError_t launch_gemm_rows(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm(const GemmArgs& a, const GemmPlan& p, bool a_tr, bool b_tr, int epi, hipStream_t s);
+// the parts of a contraction (EPI_PART), added in order, and the epilogue
+hipError_t launch_gemm_reduce(const GemmArgs& a, int epi, hipStream_t s);
 
 // dx = dz W and dw = dz^T x in one launch, where gemm_both_applies: both whole, in the same small tiles
 hipError_t launch_gemm_both(const GemmArgs& x, const GemmArgs& w, const GemmPlan& p, hipStream_t s);

@@ -3,7 +3,8 @@
 // workgroup, its statistics are formed there in fp32, and it is written once.  Rows of 4096 in bf16, 16384 of them: forward 51.5 us,
 // backward with residual and both sums 103.5, 5.2 TB/s each, the rate of a copy.  Rows that do not begin at multiples of 16 bytes
 // take twice the accesses: 2999 rows of 1365 in fp32, backward, 14.6 us for 49 MB (3.4 TB/s).
-#include "block_internal.h"
+#include "q8.h"
+#include "q8_internal.h"
 #include "row8.h"
 
 namespace tfla {
@@ -146,6 +147,64 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_fwd_kernel(RowNormA
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = (x[j][e] - mean) * rstd * g[j][e] + be[j][e];
             store8<DT>(a.y, row * a.D + c, a.D - c, y);
+        }
+        if (t == 0) {
+            if (a.rstd) a.rstd[row] = rstd;
+            if (a.mean) a.mean[row] = mean;
+        }
+    }
+}
+
+// y = norm(x + residual) in 8 bits: the sum is formed once, in fp32, for the statistics and for y, and rounded only where it is stored.
+// Sixteen lanes hold 128 columns side by side, the group of a scale.
+template <typename DT, int T, int J>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_q8_kernel(Q8NormArgs a) {
+    constexpr int G = T < 256 ? 256 / T : 1;            // rows at a time
+    __shared__ float slots[2][WIDEST][2];
+    const int t = threadIdx.x % T, grp = threadIdx.x / T;
+    const bool layer = a.kind == 1;
+    float g[J][8], be[J][8];
+    load_vector<T, J>(a.gamma, g, a.D, t, 1.0f);
+    load_vector<T, J>(layer ? a.beta : nullptr, be, a.D, t, 0.0f);
+    const long step = (long)gridDim.x * G;
+    long row = (long)blockIdx.x * G + grp;
+    if (T <= 64 && row >= a.M) return;
+    constexpr bool AHEAD = T * J < 2048;
+    RowPart<DT, T, J> next, add;
+    auto fetch = [&](long r) {
+        next.load(a.x, r, a.D, t);
+        if (a.residual) add.load(a.residual, r, a.D, t);
+    };
+    if (AHEAD) fetch(row);
+    for (int par = 0; row < a.M; row += step, par ^= 1) {
+        float x[J][8];
+        if (!AHEAD) fetch(row);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            next.v[j].get(x[j]);
+            if (a.residual) {
+                float r[8];
+                add.v[j].get(r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] += r[e];
+            }
+        }
+        if (AHEAD && row + step < a.M) fetch(row + step);
+        float mean, rstd;
+        row_stats<T, J>(x, a.D, t, layer, a.eps, mean, rstd, slots[par]);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int c = (t + T * j) * 8, left = a.D - c;
+            if (a.sum) store8<DT>(a.sum, row * a.D + c, left, x[j]);
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = e < left ? (x[j][e] - mean) * rstd * g[j][e] + be[j][e] : 0.0f;
+            if (a.y) store8<DT>(a.y, row * a.D + c, left, y);
+            const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(y)));
+            if (left > 0) {
+                q8_store8(a.q + row * a.D + c, q8_codes8(y, q8_inverse(s)), left);
+                if ((t & 15) == 0) a.s[(long)(c / Q8_GROUP) * a.M + row] = (uint8_t)s;
+            }
         }
         if (t == 0) {
             if (a.rstd) a.rstd[row] = rstd;
@@ -302,6 +361,11 @@ template <typename DT, int T, int J> void fwd(const RowNormArgs& a, hipStream_t 
     const long need = (a.M + G - 1) / G, most = 256L * (2048 / NT);
     hipLaunchKernelGGL((rownorm_fwd_kernel<DT, T, J>), dim3((unsigned)(need < most ? need : most)), dim3(NT), 0, s, a);
 }
+template <typename DT, int T, int J> void fwd_q8(const Q8NormArgs& a, hipStream_t s) {
+    constexpr int NT = T < 256 ? 256 : T, G = NT / T;
+    const long need = (a.M + G - 1) / G, most = 256L * (2048 / NT);
+    hipLaunchKernelGGL((rownorm_q8_kernel<DT, T, J>), dim3((unsigned)(need < most ? need : most)), dim3(NT), 0, s, a);
+}
 template <typename DT, int T, int J> void bwd(const RowNormBwdArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((rownorm_bwd_kernel<DT, T, J>), dim3((unsigned)a.blocks), dim3(T < 256 ? 256 : T), 0, s, a);
 }
@@ -332,6 +396,11 @@ int rownorm_bwd_blocks(long M, int D) {
 hipError_t launch_rownorm_fwd(const RowNormArgs& a, hipStream_t s) {
     if (a.dtype == 1) TFLA_BY_WIDTH(fwd, bf16_t, 512, 2);
     else TFLA_BY_WIDTH(fwd, float, 512, 2);
+    return hipGetLastError();
+}
+hipError_t launch_rownorm_q8(const Q8NormArgs& a, hipStream_t s) {
+    if (a.dtype == 1) TFLA_BY_WIDTH(fwd_q8, bf16_t, 512, 2);
+    else TFLA_BY_WIDTH(fwd_q8, float, 512, 2);
     return hipGetLastError();
 }
 hipError_t launch_rownorm_bwd(const RowNormBwdArgs& a, hipStream_t s) {

@@ -1,0 +1,253 @@
+"""The residual block in 8 bits against its 64-bit forms: quantiser, norm with the residual's addition, linear and gated products."""
+import pytest
+import torch
+
+from tests import q8_util as ref
+from tests.block_util import F64, norm as norm64, norm_back, within
+from tests.q8_util import E4M3, E8M0
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def tfla():
+    import paper_2503_14376_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+def generator(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(gen, *shape, std=1.0, dtype=BF16):
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def wide(gen, M, K, dtype):
+    """values over many powers of two, so that groups differ and small codes are subnormal"""
+    x = torch.randn((M, K), generator=gen, device="cuda") * torch.exp2(torch.randint(-12, 13, (M, K), generator=gen, device="cuda").float())
+    return x.to(dtype)
+
+
+KINDS = {"none": "ACT_NONE", "silu": "ACT_SILU", "gelu": "ACT_GELU", "relu": "ACT_RELU"}
+
+
+# ---- quantiser --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 128), (3, 127), (128, 128), (129, 257), (130, 64), (257, 1000), (77, 2056)])
+def test_quantiser(tfla, M, K, dtype, rows):
+    print("quantiser", M, K, dtype, rows, flush=True)
+    x = wide(generator(M * K + rows), M, K, dtype)
+    o = tfla.q8_quant(x, rows=rows, want_t=True)
+    ref.same_codes(o["q"], o["scale"], *ref.quant(x, rows), "plain")
+    ref.same_codes(o["qt"], o["scale_t"], *ref.quant(x.t().contiguous(), rows), "transposed")
+    one, two = tfla.q8_quant(x, rows=rows), tfla.q8_quant(x, rows=rows, want_q=False, want_t=True)
+    assert set(one) == {"q", "scale"} and set(two) == {"qt", "scale_t"}
+    for a, b in ((one, o), (two, o)):
+        for k in a:
+            assert torch.equal(a[k].view(torch.uint8), b[k].view(torch.uint8)), k
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantiser_at_its_borders(tfla, rows):
+    """largest magnitudes next to 448 2^e, ties between codes, subnormal and the largest numbers, zeros, what is not finite"""
+    print("borders", rows, flush=True)
+    x = torch.zeros(260, 384, device="cuda")
+    x[0, 0], x[1, 0], x[2, 0] = 448.0, 448.00003, 447.99997
+    x[3, :128] = torch.arange(128, device="cuda") * 2.0 ** -10 * 0.5            # ties of the subnormal codes and of the first normal ones
+    x[3, 127] = 400.0
+    x[4, :128] = 1 + torch.arange(128, device="cuda") / 16.0                     # ties of normal codes
+    x[128, 5], x[129, 200] = 1e-45, 1e-40                                          # subnormal numbers
+    x[130, 7], x[131, 300] = torch.finfo(F32).max, torch.finfo(F32).tiny
+    x[140, 3], x[140, 4], x[140, 5], x[140, 6] = float("inf"), float("-inf"), float("nan"), 3.0
+    x[256, 130:133] = torch.tensor([float("nan"), float("nan"), -0.0], device="cuda")
+    o = tfla.q8_quant(x, rows=rows, want_t=True)
+    ref.same_codes(o["q"], o["scale"], *ref.quant(x, rows), "plain")
+    ref.same_codes(o["qt"], o["scale_t"], *ref.quant(x.t().contiguous(), rows), "transposed")
+    if rows == 1:
+        assert o["scale"].view(torch.uint8)[0, :3].tolist() == [127, 128, 127] and int(o["scale"].view(torch.uint8)[0, 5]) == 0
+
+
+# ---- norm ----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("M,D", [(1, 1), (1, 4096), (5, 127), (7, 512), (33, 1000), (9, 1365), (300, 2048), (6, 8192), (3, 16384), (2500, 264)])
+def test_norm(tfla, M, D, kind, residual):
+    print("norm", M, D, kind, residual, flush=True)
+    gen, layer = generator(M + D), kind == "layer"
+    x, r = normal(gen, M, D, std=2.0), normal(gen, M, D) if residual else None
+    gamma, beta = normal(gen, D, dtype=F32), normal(gen, D, dtype=F32) if layer else None
+    code = tfla.NORM_LAYER if layer else tfla.NORM_RMS
+    o = tfla.norm_q8_fwd(x.float(), gamma, beta, None if r is None else r.float(), norm_kind=code, keep_y=True)
+    total = x.to(F64) + (0 if r is None else r.to(F64))             # (sums of two bf16 values next to each other are exact in fp32 or off by half a step)
+    if residual:
+        within("sum", o["sum"], total, torch.zeros_like(total))
+        total = o["sum"].to(F64)
+    (mean, em), (rstd, er), (y, ey) = norm64(total, gamma, beta, layer, 1e-6)
+    within("rstd", o["rstd"], rstd, er)
+    if layer:
+        within("mean", o["mean"], mean, em)
+    within("y", o["y"], y, ey)
+    # the codes are exactly those of y as it left in single precision
+    ref.same_codes(o["q"], o["scale"], *ref.quant(o["y"]), "codes")
+    # in bf16 the same arithmetic, with what is stored rounded once
+    b = tfla.norm_q8_fwd(x, gamma, beta, r, norm_kind=code, keep_y=True)
+    for k in ("q", "scale"):
+        assert torch.equal(b[k].view(torch.uint8), o[k].view(torch.uint8)), k
+    assert torch.equal(b["rstd"], o["rstd"]) and torch.equal(b["y"], o["y"].to(BF16))
+    if residual:
+        assert torch.equal(b["sum"], o["sum"].to(BF16))
+    plain = tfla.norm_q8_fwd(x, gamma, beta, r, norm_kind=code)
+    assert "y" not in plain and torch.equal(plain["q"].view(torch.uint8), b["q"].view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_and_its_backward(tfla, dtype):
+    """the gradient of x and of the residual is norm_bwd's for the sum, the sum's own gradient going round the norm"""
+    print("norm backward", dtype, flush=True)
+    gen, M, D = generator(5), 40, 520
+    x, r, dy, ds = (normal(gen, M, D, dtype=dtype) for _ in range(4))
+    gamma = normal(gen, D, dtype=F32)
+    o = tfla.norm_q8_fwd(x, gamma, residual=r)
+    g = tfla.norm_bwd(o["sum"], dy, o["rstd"], gamma=gamma, d_residual=ds)
+    (dx, edx), (dg, edg), _ = norm_back(o["sum"], dy, o["rstd"], None, gamma, ds, False)
+    within("dx", g["dx"], dx, edx)
+    within("dgamma", g["dgamma"], dg, edg)
+
+
+def test_norm_in_place(tfla):
+    gen = generator(6)
+    x, r = normal(gen, 50, 264), normal(gen, 50, 264)
+    a = tfla.norm_q8_fwd(x, residual=r)
+    for which in (0, 1):
+        t = [x.clone(), r.clone()]
+        b = tfla.norm_q8_fwd(t[0], residual=t[1], out={"sum": t[which]})
+        assert torch.equal(t[which], a["sum"]) and torch.equal(b["q"].view(torch.uint8), a["q"].view(torch.uint8))
+
+
+# ---- products ----------------------------------------------------------------------------------------------------------
+SIZES = [(1, 1, 1), (1, 128, 16), (1, 4096, 300), (2, 129, 130), (3, 1000, 77), (4, 512, 1030), (5, 512, 512), (8, 257, 200), (17, 64, 129),
+         (32, 300, 260), (33, 128, 64), (64, 1024, 64), (65, 640, 200), (128, 128, 128), (129, 384, 257), (300, 1000, 333), (513, 2048, 520),
+         (40, 4096, 256)]
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_linear_of_codes_that_add_exactly(tfla, M, K, N):
+    """no rounding but the result's: equal to the 64-bit sum in bf16"""
+    print("linear exact", M, K, N, flush=True)
+    gen = generator(M * 3 + K * 5 + N)
+    x, w = ref.small_codes(gen, M, K, 1), ref.small_codes(gen, N, K, 128)
+    z = ref.stands(*x) @ ref.stands(*w).t()
+    y = tfla.linear_q8_fwd(*x, *w)["y"]
+    assert torch.equal(y, z.float().to(BF16)), float((y.to(F64) - z).abs().max())
+    bias = torch.randint(-64, 65, (N,), generator=gen, device="cuda").float()
+    residual = torch.randint(-64, 65, (M, N), generator=gen, device="cuda").to(BF16)
+    o = tfla.linear_q8_fwd(*x, *w, bias, residual, act=tfla.ACT_RELU, keep_pre=True)
+    assert torch.equal(o["z"], (z + bias).float().to(BF16))
+    assert torch.equal(o["y"], ((z + bias).clamp_min(0) + residual.to(F64)).float().to(BF16))
+
+
+@pytest.mark.parametrize("kind", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("M,K,N", [(1, 4096, 300), (3, 1000, 77), (33, 300, 130), (150, 520, 260), (300, 1000, 333)])
+def test_linear(tfla, M, K, N, kind):
+    print("linear", M, K, N, kind, flush=True)
+    gen = generator(M + K + N)
+    x, w = ref.to_codes(normal(gen, M, K)), ref.to_codes(normal(gen, N, K, std=K ** -0.5), 128)
+    bias, residual = normal(gen, N, dtype=F32), normal(gen, M, N)
+    o = tfla.linear_q8_fwd(*x, *w, bias, residual, act=getattr(tfla, KINDS[kind]), keep_pre=True)
+    (z, ez), (y, ey) = ref.linear(ref.stands(*x), ref.stands(*w), bias, residual, kind)
+    within("z", o["z"], z, ez)
+    within("y", o["y"], y, ey)
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_gated_of_codes_that_add_exactly(tfla, M, K, N):
+    print("gated exact", M, K, N, flush=True)
+    gen = generator(M * 3 + K * 5 + N)
+    x, g, u = ref.small_codes(gen, M, K, 1), ref.small_codes(gen, N, K, 128), ref.small_codes(gen, N, K, 128)
+    a, b = (ref.stands(*x) @ ref.stands(*w).t() for w in (g, u))
+    o = tfla.gated_q8_fwd(*x, *g, *u, act=tfla.ACT_RELU, keep_pre=True)
+    assert torch.equal(o["a"], a.float().to(BF16)) and torch.equal(o["u"], b.float().to(BF16))
+    h = (a.clamp_min(0).float() * b.float())            # (one rounding in fp32, as in the kernel)
+    assert torch.equal(o["h"], h.to(BF16))
+    ref.same_codes(o["hq"], o["h_scale"], *ref.quant(h), "h")
+    plain = tfla.gated_q8_fwd(*x, *g, *u, act=tfla.ACT_RELU)
+    assert set(plain) - {"workspace"} == {"hq", "h_scale"}
+    for k in ("hq", "h_scale"):
+        assert torch.equal(plain[k].view(torch.uint8), o[k].view(torch.uint8))
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu", "relu", "none"])
+@pytest.mark.parametrize("M,K,N", [(1, 1000, 300), (4, 512, 130), (33, 300, 130), (150, 520, 260)])
+def test_gated(tfla, M, K, N, kind):
+    print("gated", M, K, N, kind, flush=True)
+    gen = generator(M + K + N)
+    x, g, u = ref.to_codes(normal(gen, M, K)), *(ref.to_codes(normal(gen, N, K, std=K ** -0.5), 128) for _ in range(2))
+    bg, bu = normal(gen, N, dtype=F32), normal(gen, N, dtype=F32)
+    o = tfla.gated_q8_fwd(*x, *g, *u, bg, bu, act=getattr(tfla, KINDS[kind]), keep_pre=True)
+    (a, ea), (b, eb), (h, eh) = ref.gated(ref.stands(*x), ref.stands(*g), ref.stands(*u), bg, bu, kind)
+    within("a", o["a"], a, ea)
+    within("u", o["u"], b, eb)
+    within("h", o["h"], h, eh)
+    ref.coded("hq", o["hq"], o["h_scale"], h, eh)
+
+
+def transposed(w):
+    """codes and scales of the transpose of a matrix whose blocks are given"""
+    q, s = ref.to_codes(w.t().contiguous(), 128)
+    return q, s
+
+
+@pytest.mark.parametrize("kind", ["none", "silu", "gelu", "relu"])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 16), (3, 200, 130), (33, 300, 129), (128, 128, 128), (150, 520, 260), (260, 333, 200)])
+def test_linear_backward(tfla, M, K, N, kind):
+    print("linear backward", M, K, N, kind, flush=True)
+    gen = generator(M + K + N)
+    x, w, dy, z = normal(gen, M, K), normal(gen, N, K, std=K ** -0.5), normal(gen, M, N), normal(gen, M, N, std=2.0)
+    wt = transposed(w)
+    o = tfla.linear_q8_bwd(x, *wt, dy, None if kind == "none" else z, act=getattr(tfla, KINDS[kind]), want_db=True)
+    dz, ez = ref.gradients(kind, dy, z)
+    (dx, edx), dws, dbs = ref.back(dz, ez, x, [ref.stands(*wt).t().contiguous()])
+    within("dx", o["dx"], dx, edx)
+    within("dw", o["dw"], *dws[0])
+    within("db", o["db"], *dbs[0])
+    one = tfla.linear_q8_bwd(x, *wt, dy, None if kind == "none" else z, act=getattr(tfla, KINDS[kind]), want_dw=False)
+    two = tfla.linear_q8_bwd(x, None, None, dy, None if kind == "none" else z, act=getattr(tfla, KINDS[kind]), want_dx=False)
+    three = tfla.linear_q8_bwd(None, None, None, dy, None if kind == "none" else z, act=getattr(tfla, KINDS[kind]), want_dx=False, want_dw=False, want_db=True)
+    assert torch.equal(one["dx"], o["dx"]) and torch.equal(two["dw"], o["dw"]) and torch.equal(three["db"], o["db"])
+    assert "dw" not in one and "dx" not in two and "dx" not in three
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu", "relu", "none"])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 16), (33, 300, 129), (128, 128, 128), (150, 520, 260)])
+def test_gated_backward(tfla, M, K, N, kind):
+    print("gated backward", M, K, N, kind, flush=True)
+    gen = generator(M + K + N)
+    x, dh, a, u = normal(gen, M, K), normal(gen, M, N), normal(gen, M, N, std=2.0), normal(gen, M, N)
+    ws = [normal(gen, N, K, std=K ** -0.5) for _ in range(2)]
+    wt = [transposed(w) for w in ws]
+    o = tfla.gated_q8_bwd(x, *wt[0], *wt[1], a, u, dh, act=getattr(tfla, KINDS[kind]), want_db=True)
+    dz, ez = ref.gradients(kind, dh, a, u)
+    (dx, edx), dws, dbs = ref.back(dz, ez, x, [ref.stands(*w).t().contiguous() for w in wt])
+    within("dx", o["dx"], dx, edx)
+    for i, n in enumerate(("gate", "up")):
+        within("dw_" + n, o["dw_" + n], *dws[i])
+        within("db_" + n, o["db_" + n], *dbs[i])
+
+
+def test_no_tokens(tfla):
+    gen = generator(1)
+    x, w = ref.to_codes(torch.zeros(0, 256, device="cuda")), ref.to_codes(normal(gen, 136, 256), 128)
+    assert tfla.linear_q8_fwd(*x, *w)["y"].shape == (0, 136)
+    assert tfla.gated_q8_fwd(*x, *w, *w)["hq"].shape == (0, 136)
+    wt = transposed(normal(gen, 136, 256))
+    e = torch.empty(0, 136, device="cuda", dtype=BF16)
+    o = tfla.linear_q8_bwd(torch.empty(0, 256, device="cuda", dtype=BF16), *wt, e, want_db=True)
+    assert o["dx"].shape == (0, 256) and not o["dw"].any() and not o["db"].any()
+    o = tfla.gated_q8_bwd(torch.empty(0, 256, device="cuda", dtype=BF16), *wt, *wt, e, e, e, want_db=True)
+    assert not any(o[k].any() for k in ("dw_gate", "dw_up", "db_gate", "db_up"))
+    assert tfla.q8_quant(torch.empty(0, 256, device="cuda"), want_t=True)["qt"].shape == (256, 0)
+    assert tfla.norm_q8_fwd(torch.empty(0, 256, device="cuda"))["q"].shape == (0, 256)
