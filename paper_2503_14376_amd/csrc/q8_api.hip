@@ -28,7 +28,7 @@ int check_product(int direction, int M, int K, int N, int act) {
 
 struct FwdLayout {
     size_t x, w0, w1, part, bytes;
-    GemmPlan plan; bool rows, move_x, move_w;
+    GemmPlan plan; bool rows, join, move_x, move_w;     // join: a pair's gate is a launch of its own
 };
 FwdLayout fwd_layout(int M, int K, int N, bool pair, bool x_off, bool w_off) {
     FwdLayout l{};
@@ -47,8 +47,9 @@ FwdLayout fwd_layout(int M, int K, int N, bool pair, bool x_off, bool w_off) {
             if (pair) { l.w1 = c.off; c.take(N * up16(K)); }
         }
     }
+    l.join = pair && (l.rows || !q8_gate_inside(l.plan));
     l.part = c.off;
-    if (l.plan.split > 1 || pair) c.take((size_t)l.plan.split * (pair ? 2 : 1) * M * (((size_t)N + 7) & ~(size_t)7) * sizeof(float));
+    if (l.plan.split > 1 || l.join) c.take((size_t)l.plan.split * (pair ? 2 : 1) * M * (((size_t)N + 7) & ~(size_t)7) * sizeof(float));
     l.bytes = c.off;
     return l;
 }
@@ -130,9 +131,9 @@ int product_fwd(const void* xq, const void* x_scale, const void* const (&wq)[2],
             g.B[0] = ws + l.w0; g.B[1] = pair ? ws + l.w1 : nullptr; g.ldb = pitch / 2;
         }
         if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_q8_repack(rp, s));
-        TFLA_LAUNCH(K_GEMM, launch_q8_gemm(q, l.plan, pair ? EPI_GATED : EPI_LINEAR, s));
+        TFLA_LAUNCH(K_GEMM, launch_q8_gemm(q, l.plan, l.join ? EPI_PART : (pair ? EPI_GATED : EPI_LINEAR), s));
     }
-    if (pair) TFLA_LAUNCH(K_ACT_BWD, launch_q8_gated_join(q, s));
+    if (l.join) TFLA_LAUNCH(K_ACT_BWD, launch_q8_gated_join(q, s));
     return TFLA_OK;
 }
 
@@ -206,7 +207,7 @@ namespace tfla {
 template <int V> hipError_t launch_q8_gemm_as(const Q8GemmArgs& a, const GemmPlan& p, hipStream_t s);
 
 hipError_t launch_q8_gemm(const Q8GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s) {
-    if (epi == EPI_GATED) return launch_q8_gemm_as<3>(a, p, s);
+    if (a.g.pair) return epi == EPI_GATED ? launch_q8_gemm_as<4>(a, p, s) : launch_q8_gemm_as<3>(a, p, s);
     if (a.g.split == 1) return epi == EPI_LINEAR ? launch_q8_gemm_as<0>(a, p, s) : launch_q8_gemm_as<1>(a, p, s);
     const hipError_t rc = launch_q8_gemm_as<2>(a, p, s);
     return rc != hipSuccess ? rc : launch_gemm_reduce(a.g, epi, s);

@@ -52,6 +52,7 @@ struct Q8GemmArgs {
     int k;
     Q8Out h; void* hc;                 // EPI_GATED: codes and scales of h; hc: h in bf16 or NULL
 };
+// (a pair: EPI_GATED where q8_gate_inside, otherwise EPI_PART, which leaves the parts to launch_q8_gated_join)
 hipError_t launch_q8_gemm(const Q8GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);
 hipError_t launch_q8_rows(const Q8GemmArgs& a, hipStream_t s);
 // h = act(a) u of a pair whose products lie in g.part (split parts of two planes), its codes and scales; stores a, u, h where wanted

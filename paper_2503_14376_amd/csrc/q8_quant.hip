@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
     }
     float h[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = e < left ? act_value<float>(v[0][e], x.act) * v[1][e] : 0.0f;
+    for (int e = 0; e < 8; ++e) h[e] = e < left ? act_value<bf16_t>(v[0][e], x.act) * v[1][e] : 0.0f;
     const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(h)));
     if (left <= 0) return;
     q8_store8(a.h.q + m * x.N + n, q8_codes8(h, q8_inverse(s)), left);

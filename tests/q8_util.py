@@ -10,6 +10,8 @@ from tests.block_util import F64, FN, U, act, act_grad
 
 E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 DROP = 7 * 2.0 ** -13
+# forward activations are those of the products in bf16: sigma to 2^-16 of its value, Phi to 2^-13 of it and 1.2e-7 < 2^-22 absolute
+ACT = 2.0 ** -13 + 2.0 ** -22
 
 
 def padded(x, rows, cols):
@@ -97,7 +99,7 @@ def linear(x, w, bias, residual, kind):
         z = z + bias.to(F64)
         ez = ez + U * z.abs()
     y = act(z, kind)
-    ey = 1.2 * ez + (FN if kind == "relu" else 2.0 ** -13) * z.abs() if kind != "none" else ez    # (gelu in bf16: 2^-13 of its value)
+    ey = 1.2 * ez + ACT * z.abs() if kind != "none" else ez
     if residual is not None:
         y = y + residual.to(F64)
         ey = ey + U * y.abs()
@@ -108,7 +110,7 @@ def gated(x, wg, wu, bg, bu, kind):
     (a, ea), _ = linear(x, wg, bg, None, "none")
     (u, eu), _ = linear(x, wu, bu, None, "none")
     h = act(a, kind) * u
-    eh = (1.2 * ea + FN * a.abs()) * (u.abs() + eu) + act(a, kind).abs() * eu + 2 * U * h.abs()
+    eh = (1.2 * ea + (ACT if kind != "none" else 0) * a.abs()) * (u.abs() + eu) + act(a, kind).abs() * eu + 2 * U * h.abs()
     return (a, ea), (u, eu), (h, eh)
 
 

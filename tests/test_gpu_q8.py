@@ -131,7 +131,7 @@ def test_norm_in_place(tfla):
 # ---- products ----------------------------------------------------------------------------------------------------------
 SIZES = [(1, 1, 1), (1, 128, 16), (1, 4096, 300), (2, 129, 130), (3, 1000, 77), (4, 512, 1030), (5, 512, 512), (8, 257, 200), (17, 64, 129),
          (32, 300, 260), (33, 128, 64), (64, 1024, 64), (65, 640, 200), (128, 128, 128), (129, 384, 257), (300, 1000, 333), (513, 2048, 520),
-         (40, 4096, 256)]
+         (40, 4096, 256), (4100, 2600, 2000), (2000, 1100, 4200), (4090, 1500, 3000)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
@@ -236,6 +236,43 @@ def test_gated_backward(tfla, M, K, N, kind):
     for i, n in enumerate(("gate", "up")):
         within("dw_" + n, o["dw_" + n], *dws[i])
         within("db_" + n, o["db_" + n], *dbs[i])
+
+
+def few_values(gen, R, C, most=2):
+    """0, +-1, ..., +-2^most: codes stand for them exactly, and sums of products are exact"""
+    v = torch.exp2(torch.randint(0, most + 1, (R, C), generator=gen, device="cuda").float())
+    return (v * torch.randint(-1, 2, (R, C), generator=gen, device="cuda")).to(BF16)
+
+
+LARGE = [(300, 200, 260), (1000, 1100, 1365), (4100, 2600, 2000), (2000, 4200, 2600), (4096, 4096, 2048)]
+
+
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_linear_backward_of_values_that_add_exactly(tfla, M, K, N):
+    print("linear backward exact", M, K, N, flush=True)
+    gen = generator(M + K + N)
+    x, w, dy = few_values(gen, M, K), few_values(gen, N, K), few_values(gen, M, N)
+    wt = tfla.q8_quant(w, rows=128, want_q=False, want_t=True)
+    o = tfla.linear_q8_bwd(x, wt["qt"], wt["scale_t"], dy, want_db=True)
+    assert torch.equal(o["dx"], (dy.to(F64) @ w.to(F64)).float().to(BF16))
+    assert torch.equal(o["dw"], (dy.to(F64).t() @ x.to(F64)).float().to(BF16))
+    assert torch.equal(o["db"], dy.to(F64).sum(0).float())
+
+
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_gated_backward_of_values_that_add_exactly(tfla, M, K, N):
+    print("gated backward exact", M, K, N, flush=True)
+    gen = generator(M + K + N)
+    x, dh, a, u = few_values(gen, M, K), few_values(gen, M, N, 1), few_values(gen, M, N, 1), few_values(gen, M, N, 1)
+    ws = [few_values(gen, N, K) for _ in range(2)]
+    wt = [tfla.q8_quant(w, rows=128, want_q=False, want_t=True) for w in ws]
+    o = tfla.gated_q8_bwd(x, wt[0]["qt"], wt[0]["scale_t"], wt[1]["qt"], wt[1]["scale_t"], a, u, dh, act=tfla.ACT_RELU, want_db=True)
+    d, a, u = dh.to(F64), a.to(F64), u.to(F64)
+    dz = [d * u * (a > 0), d * a.clamp_min(0)]
+    assert torch.equal(o["dx"], (dz[0] @ ws[0].to(F64) + dz[1] @ ws[1].to(F64)).float().to(BF16))
+    for n, z in zip(("gate", "up"), dz):
+        assert torch.equal(o["dw_" + n], (z.t() @ x.to(F64)).float().to(BF16)), n
+        assert torch.equal(o["db_" + n], z.sum(0).float())
 
 
 def test_no_tokens(tfla):
