@@ -159,7 +159,13 @@ int product_bwd(const void* x, const void* const (&wqt)[2], const void* const (&
         const bool one = blocks(M) == 1;
         if (want_db && !one) { a.part = reinterpret_cast<float*>(ws + l.dbpart); a.ldp = N; }
         if (one) { a.db[0] = db[0]; a.db[1] = db[1]; }
-        TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, s));
+        Q8TileArgs b{};
+        if (want_dw) {      // x along the tokens
+            b.x = x; b.M = M; b.N = K; b.dtype = TFLA_BF16; b.rows = 1; b.mode = Q8_VALUES;
+            Q8Out& o = b.out[0];
+            o.qt = ws + l.xt; o.st = ws + l.sx; o.ldt = Mp; o.ldst = K; o.wt = (int)Mp;
+        }
+        TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, b, s));
     }
     if (want_db && blocks(M) != 1)
         TFLA_LAUNCH(K_ACT_BWD, launch_sum_rows(reinterpret_cast<float*>(ws + l.dbpart), (int)blocks(M), (long)P * N, N, N, db[0], db[1], s));
@@ -182,13 +188,6 @@ int product_bwd(const void* x, const void* const (&wqt)[2], const void* const (&
         TFLA_LAUNCH(K_GEMM, launch_q8_gemm(q, l.plan_dx, EPI_STORE, s));
     }
     if (want_dw) {
-        if (M > 0) {
-            Q8TileArgs a{};
-            a.x = x; a.M = M; a.N = K; a.dtype = TFLA_BF16; a.rows = 1; a.mode = Q8_VALUES;
-            Q8Out& o = a.out[0];
-            o.qt = ws + l.xt; o.st = ws + l.sx; o.ldt = Mp; o.ldst = K; o.wt = (int)Mp;
-            TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, s));
-        }
         Q8GemmArgs q{};
         operands(q, Mp, Mp, N, K, M);
         q.lsa = N; q.lsb = K; q.shb = 0;
@@ -228,7 +227,7 @@ int tfla_q8_quant(const void* x, int M, int K, int dtype, int rows, void* q, voi
     Q8TileArgs a{};
     a.x = x; a.M = M; a.N = K; a.dtype = dtype; a.rows = rows; a.mode = Q8_VALUES;
     a.out[0] = {u8(q), u8(scale), u8(qt), u8(scale_t), K, rows == 1 ? M : blocks(M), M, rows == 1 ? K : blocks(K), K, M};
-    TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, s));
+    TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, {}, s));
     return TFLA_OK;
 }
 

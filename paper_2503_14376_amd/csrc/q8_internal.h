@@ -25,7 +25,8 @@ struct Q8TileArgs {
     float* part; float* db[2];
     long M; int N; long ldp; int act, dtype, mode, rows;
 };
-hipError_t launch_q8_tiles(const Q8TileArgs& a, hipStream_t s);
+// b: plain values in the same launch, none where b.M is 0
+hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s);
 
 // y = norm(x + residual), its codes and scales; sum, y, rstd, mean may be NULL
 struct Q8NormArgs : RowNormArgs {

@@ -9,147 +9,251 @@ namespace tfla {
 
 namespace {
 
-constexpr int TILE = 128, NT = 512, R = 4, WAVES = NT / 64;
+constexpr int TILE = 128, NT = 512, WAVES = NT / 64, RPI = NT / 16;
 
-// Thread (g = t % 16, r = t / 16) holds the columns 8 g ... of the rows 4 r ... 4 r + 3 of the tile.
-template <typename DT, int MODE> __global__ void __launch_bounds__(NT, 2) q8_tile_kernel(Q8TileArgs a) {
-    constexpr int P = MODE == Q8_PAIR ? 2 : 1, PITCH = TILE + 4;
-    __shared__ uint32_t colmax[WAVES][TILE];
-    __shared__ float colsum[WAVES][TILE];
-    __shared__ uint32_t turn[TILE * PITCH / 4];
-    const int t = threadIdx.x, g = t & 15, rg = t >> 4, wave = t >> 6;
-    const long r0 = (long)blockIdx.x * TILE;
-    const int c0 = blockIdx.y * TILE, c = c0 + g * 8, left = a.N - c;
-    float v[P][R][8];
-    {
-        Vec8<DT> x[R], z[R], u[R];
+// act(z) and act'(z) of a bf16 value, to 2^-20 (1 + |z|) of it: of a gradient that is rounded to 8 bits a value next to the border between
+// two codes is worth a sixteenth of itself, so that an error of 2^-13, as the bf16 products' gelu has, would show in dx, dw and the sums.  (The
+// library's functions for fp32 bound the pass instead: gated pair backward, 8192 x 10944, 406 us.)
+// silu: sigma by the hardware's exponential and reciprocal.  gelu: Phi(-|z|) = exp(-z^2 / 2) h(|z|), h = t P(t), t = 1 / (1 + c |z|), P of
+// degree 8 fitted to the smallest relative error over |z| <= 14.5 (2^-25.1, evaluated in fp32 2^-21.3; beyond, exp(-z^2 / 2)
+// leaves fp32).  z^2 is exact.
+template <int ACT> __device__ __forceinline__ float act_fine(float z, float& slope) {
+    if constexpr (ACT == ACT_SILU) {
+        const float g = __builtin_amdgcn_rcpf(1.0f + fast_exp2(-1.44269504f * z));
+        slope = g * (1.0f + z * (1.0f - g));
+        return z * g;
+    } else if constexpr (ACT == ACT_GELU) {
+        const float e = fast_exp2(-0.72134752f * (z * z));
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.26f, fabsf(z), 1.0f));
+        constexpr float P[9] = {0.10375702f, 0.10305099f, 0.10278856f, 0.05196531f, 0.1587576f, -0.14778766f, 0.24873173f, -0.15149373f, 0.030230155f};
+        float p = P[8];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const long row = r0 + rg * R + i;
-            const int n = row < a.M ? left : 0;
-            x[i] = load8<DT>(a.x, row * a.N + c, n);
-            if constexpr (MODE != Q8_VALUES) z[i] = load8<DT>(a.z, row * a.N + c, n);
-            if constexpr (MODE == Q8_PAIR) u[i] = load8<DT>(a.u, row * a.N + c, n);
+        for (int k = 7; k >= 0; --k) p = __builtin_fmaf(t, p, P[k]);
+        const float h = t * p * e, c = z < 0.0f ? h : 1.0f - h;
+        slope = __builtin_fmaf(z * 0.39894228f, e, c);
+        return z * c;
+    } else return act_both<float>(z, ACT, slope);
+}
+
+// maximum (sum) over the lanes 16 and 32 apart, which hold other rows of the same columns
+__device__ __forceinline__ uint32_t rows_max(uint32_t x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t p0 = p[0], p1 = p[1], y = max(p0, p1);
+    const auto q = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    const uint32_t q0 = q[0], q1 = q[1];
+    return max(q0, q1);
+}
+__device__ __forceinline__ float rows_sum(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned p0 = p[0], p1 = p[1];
+    const float y = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
+    const unsigned w = __builtin_bit_cast(unsigned, y);
+    const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const unsigned q0 = q[0], q1 = q[1];
+    return __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
+}
+
+// A tile's values, for what has to wait for its scale: bf16 where they are bf16, else fp32.  A row's columns are turned by 32 bytes from one
+// block of 16 rows to the next, so that the transposed reads, 8 columns of 8 such blocks at a time, meet no bank twice.
+template <typename VT> struct TileValues {
+    static constexpr int PITCH = TILE + 16 / (int)sizeof(VT), STEP = 32 / (int)sizeof(VT);
+    VT v[TILE * PITCH];
+    static __device__ __forceinline__ int place(int row, int c) { return row * PITCH + ((c + STEP * (row >> 4)) & (TILE - 1)); }
+};
+template <typename VT> struct TileMemory {
+    TileValues<VT> values;
+    float colsum[WAVES][TILE];
+    uint32_t colmax[TILE];
+};
+template <typename DT, int MODE> struct Kept { typedef float type; };
+template <> struct Kept<bf16_t, Q8_VALUES> { typedef bf16_t type; };
+
+// Tile (bx, by) of matrix p.  Thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r, r + 32, r + 64, r + 96: what a row
+// needs is done there, from registers; what a column needs is kept in LDS until the column's scale is known.  All rows are requested at once.
+// Where an activation follows, their loop is not unrolled (a switch picks the registers): code that a workgroup runs through once is waited
+// for line by line (unrolled, 28 KB, a pair of 1000 x 1365 took 32 us).
+template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline__ void q8_tile(const Q8TileArgs& a, int bx, int by, int p, MEM& m) {
+    typedef typename Kept<DT, MODE>::type VT;
+    typedef TileValues<VT> Values;
+    constexpr int ROWS = TILE / RPI;
+    static_assert(ROWS == 4, "the cases of the switch below");
+    const int t = threadIdx.x, g = t & 15, wave = t >> 6;
+    const long r0 = (long)bx * TILE;
+    const int c0 = by * TILE, c = c0 + g * 8, left = a.N - c;
+    const Q8Out& o = a.out[p];
+    float* db = a.part ? a.part + ((long)bx * (MODE == Q8_PAIR ? 2 : 1) + p) * a.ldp : a.db[p];
+    const bool blocks = a.rows > 1, columns = o.qt != nullptr, keep = columns || blocks;
+    VT* const kept = reinterpret_cast<VT*>(&m);
+    if (t < TILE) m.colmax[t] = 0;
+    __syncthreads();
+    Vec8<DT> x[ROWS], z[ROWS], u[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+        const long row = r0 + (t >> 4) + k * RPI;
+        const int n = row < a.M ? left : 0;
+        x[k] = load8<DT>(a.x, row * a.N + c, n);
+        if constexpr (MODE != Q8_VALUES) z[k] = load8<DT>(a.z, row * a.N + c, n);
+        if constexpr (MODE == Q8_PAIR) u[k] = load8<DT>(a.u, row * a.N + c, p == 0 ? n : 0);
+    }
+    uint32_t cm[8];
+    float cs[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { cm[e] = 0; cs[e] = 0.0f; }
+    auto take = [&](int i, const Vec8<DT>& xk, const Vec8<DT>& zk, const Vec8<DT>& uk) {
+        float v[8];
+        xk.get(v);
+        if constexpr (sizeof(VT) == 2) {
+            if (keep) *reinterpret_cast<u32x4*>(kept + Values::place(i, g * 8)) = xk.w;
+        }
+        if constexpr (MODE != Q8_VALUES) {
+            float zf[8], uf[8];
+            zk.get(zf);
+            if (MODE == Q8_PAIR && p == 0) uk.get(uf);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float slope;
+                const float value = act_fine<ACT>(zf[e], slope);
+                if (MODE == Q8_PAIR) v[e] = p > 0 ? v[e] * value : v[e] * uf[e] * slope;
+                else v[e] *= slope;
+            }
+        }
+        uint32_t w[8], most = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+            most = max(most, w[e]);
+        }
+        if (__any(most >= 0x7f800000u)) {       // (rare: what is not finite does not count)
+            most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = w[e] < 0x7f800000u ? w[e] : 0u;
+                most = max(most, w[e]);
+            }
+        }
+        const long row = r0 + i;
+        if (o.q && !blocks) {
+            const uint32_t s = q8_scale(lanes_max<16>(most));
+            if (row < a.M) {
+                q8_store8(o.q + row * o.ldq + c, q8_codes8(v, q8_inverse(s)), o.wq - c);
+                if (g == 0) o.s[(long)by * o.lds + row] = (uint8_t)s;
+            }
+        }
+        if constexpr (sizeof(VT) == 4) {
+            if (keep) {
+                float* d = kept + Values::place(i, g * 8);
+                *reinterpret_cast<f32x4*>(d) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(d + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            }
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            x[i].get(v[0][i]);
-            if constexpr (MODE != Q8_VALUES) {
-                float zf[8], uf[8];
-                z[i].get(zf);
-                if constexpr (MODE == Q8_PAIR) u[i].get(uf);
-                // (the activation as for fp32: a value next to a border between two codes is worth a sixteenth of itself)
+        for (int e = 0; e < 8; ++e) {
+            cm[e] = max(cm[e], w[e]);
+            cs[e] += v[e];
+        }
+    };
+    if constexpr (MODE == Q8_VALUES) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float slope;
-                    const float value = act_both<float>(zf[e], a.act, slope), d = v[0][i][e];
-                    if constexpr (MODE == Q8_PAIR) {
-                        v[0][i][e] = d * uf[e] * slope;
-                        v[1][i][e] = d * value;
-                    } else {
-                        v[0][i][e] = d * slope;
-                    }
-                }
+        for (int k = 0; k < ROWS; ++k) take((t >> 4) + k * RPI, x[k], z[k], u[k]);
+    } else {
+        int rows = ROWS;
+        asm("" : "+s"(rows));
+#pragma unroll 1
+        for (int k = 0; k < rows; ++k) {
+            Vec8<DT> xk, zk, uk;
+#define TFLA_PICK(K)                                    \
+    case K:                                             \
+        xk = x[K];                                      \
+        zk = z[K];                                      \
+        if constexpr (MODE == Q8_PAIR) uk = u[K];       \
+        break;
+            switch (k) {
+                TFLA_PICK(0) TFLA_PICK(1) TFLA_PICK(2) TFLA_PICK(3)
+                default: __builtin_unreachable();
+            }
+#undef TFLA_PICK
+            take((t >> 4) + k * RPI, xk, zk, uk);
+        }
+    }
+    if (keep) {
+        // (the largest of a set does not depend on the order in which the wavefronts come)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cm[e] = rows_max(cm[e]);
+            if ((t & 48) == 0) atomicMax(&m.colmax[g * 8 + e], cm[e]);
+        }
+    }
+    if (db) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cs[e] = rows_sum(cs[e]);
+            if ((t & 48) == 0) m.colsum[wave][g * 8 + e] = cs[e];
+        }
+    }
+    __syncthreads();
+    if (db && t < TILE && c0 + t < a.N) {
+        float s = m.colsum[0][t];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += m.colsum[w][t];
+        db[c0 + t] = s;
+    }
+    uint32_t whole = 0;         // the scale of a block
+    if (blocks) {
+        whole = q8_scale(lanes_max<64>(max(m.colmax[t & 63], m.colmax[64 + (t & 63)])));
+        if (t == 0 && o.q) o.s[(long)by * o.lds + bx] = (uint8_t)whole;
+        if (t == 0 && columns) o.st[(long)bx * o.ldst + by] = (uint8_t)whole;
+        if (o.q) {
+#pragma unroll 1
+            for (int i = t >> 4; i < TILE && r0 + i < a.M; i += RPI) {
+                float v[8];
+                load8<VT>(kept, Values::place(i, g * 8), 8).get(v);
+                q8_store8(o.q + (r0 + i) * o.ldq + c, q8_codes8(v, q8_inverse(whole)), o.wq - c);
             }
         }
     }
+    if (!columns) return;
+    // rows of the transpose: eight pieces of 16 codes each
+#pragma unroll 1
+    for (int i = t; i < TILE * 8; i += NT) {
+        const int col = i >> 3, at = (i & 7) * 16;
+        const long n = o.wt - r0 - at;
+        if (c0 + col >= a.N || n <= 0) continue;
+        const uint32_t s = blocks ? whole : q8_scale(m.colmax[col]);
+        const float inv = q8_inverse(s);
+        const VT* d = kept + Values::place(at, col);        // (whole blocks of 16 rows are turned alike)
+        auto at_row = [&](int r) { return (float)d[r * Values::PITCH]; };
+        uint32_t w[4];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const Q8Out& o = a.out[p];
-        float* db = a.part ? a.part + ((long)blockIdx.x * P + p) * a.ldp : a.db[p];
-        if (p > 0) __syncthreads();
-        uint32_t cm[8];
-        if (db || o.qt || a.rows > 1) {
-            float cs[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                cm[e] = 0;
-                cs[e] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    cm[e] = max(cm[e], q8_magnitude(v[p][i][e]));
-                    cs[e] += v[p][i][e];
-                }
-            }
-            if (db) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    cs[e] += __shfl_xor(cs[e], 16, 64);
-                    cs[e] += __shfl_xor(cs[e], 32, 64);
-                    if ((t & 48) == 0) colsum[wave][g * 8 + e] = cs[e];
-                }
-            }
-            if (o.qt || a.rows > 1) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    cm[e] = max(cm[e], (uint32_t)__shfl_xor((int)cm[e], 16, 64));
-                    cm[e] = max(cm[e], (uint32_t)__shfl_xor((int)cm[e], 32, 64));
-                    if ((t & 48) == 0) colmax[wave][g * 8 + e] = cm[e];
-                }
-            }
-            __syncthreads();
-            if (o.qt || a.rows > 1) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    cm[e] = colmax[0][g * 8 + e];
-#pragma unroll
-                    for (int w = 1; w < WAVES; ++w) cm[e] = max(cm[e], colmax[w][g * 8 + e]);
-                }
-            }
-            if (db && t < TILE && c0 + t < a.N) {
-                float s = colsum[0][t];
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w) s += colsum[w][t];
-                db[c0 + t] = s;
+        for (int e = 0; e < 4; ++e) w[e] = q8_codes(at_row(4 * e), at_row(4 * e + 1), at_row(4 * e + 2), at_row(4 * e + 3), inv);
+        uint8_t* to = o.qt + (long)(c0 + col) * o.ldt + r0 + at;
+        if (n >= 16) __builtin_memcpy(to, w, 16);
+        else {
+            for (int e = 0; e < n; ++e) {
+                uint32_t q = w[0];
+                q = e >= 4 ? w[1] : q;
+                q = e >= 8 ? w[2] : q;
+                q = e >= 12 ? w[3] : q;
+                to[e] = (uint8_t)(q >> (8 * (e & 3)));
             }
         }
-        uint32_t whole = 0;         // rows = 128: the tile's largest magnitude
-        if (a.rows > 1) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) whole = max(whole, cm[e]);
-            whole = lanes_max<16>(whole);
-        }
-        if (o.q) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const long row = r0 + rg * R + i;
-                const uint32_t s = q8_scale(a.rows > 1 ? whole : lanes_max<16>(q8_magnitude8(v[p][i])));
-                const u32x2 w = q8_codes8(v[p][i], q8_inverse(s));
-                if (row < a.M) {
-                    q8_store8(o.q + row * o.ldq + c, w, o.wq - c);
-                    if (g == 0 && a.rows == 1) o.s[(long)blockIdx.y * o.lds + row] = (uint8_t)s;
-                }
-            }
-            if (a.rows > 1 && t == 0) o.s[(long)blockIdx.y * o.lds + blockIdx.x] = (uint8_t)q8_scale(whole);
-        }
-        if (o.qt) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t s = q8_scale(a.rows > 1 ? whole : cm[e]);
-                static_assert(R == 4, "a word of four rows");
-                turn[((g * 8 + e) * PITCH + rg * R) / 4] = q8_codes(v[p][0][e], v[p][1][e], v[p][2][e], v[p][3][e], q8_inverse(s));
-                if (rg == 0 && a.rows == 1 && c + e < a.N) o.st[(long)blockIdx.x * o.ldst + c + e] = (uint8_t)s;
-            }
-            if (a.rows > 1 && t == 0) o.st[(long)blockIdx.x * o.ldst + blockIdx.y] = (uint8_t)q8_scale(whole);
-            __syncthreads();
-            // rows of the transpose: eight pieces of 16 codes each
-#pragma unroll
-            for (int k = 0; k < TILE * 8 / NT; ++k) {
-                const int i = t + k * NT, col = i >> 3, at = (i & 7) * 16;
-                if (c0 + col >= a.N || r0 + at >= o.wt) continue;
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = turn[(col * PITCH + at) / 4 + e];
-                uint8_t* d = o.qt + (long)(c0 + col) * o.ldt + r0 + at;
-                const long n = o.wt - r0 - at;
-                if (n >= 16) __builtin_memcpy(d, w, 16);
-                else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (e < n) d[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
-                }
-            }
-        }
+        if (at == 0 && !blocks) o.st[(long)bx * o.ldst + c0 + col] = (uint8_t)s;
+    }
+}
+
+// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0).  A pair's two
+// gradients of a tile are two workgroups that read the same tensors at about the same time on the same XCD (ids 8 apart).
+template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, unsigned na) {
+    __shared__ __align__(16) TileMemory<typename Kept<DT, MODE>::type> m;
+    const unsigned i = blockIdx.x;
+    if (i < na) {
+        const unsigned across = (a.N + TILE - 1) / TILE;
+        const unsigned tile = MODE == Q8_PAIR ? (i >> 4) * 8 + (i & 7) : i;
+        if (MODE == Q8_PAIR && tile >= across * (unsigned)((a.M + TILE - 1) / TILE)) return;
+        q8_tile<DT, MODE, ACT>(a, tile / across, tile % across, MODE == Q8_PAIR ? (i >> 3) & 1 : 0, m);
+    } else {
+        const unsigned across = (b.N + TILE - 1) / TILE;
+        q8_tile<DT, Q8_VALUES, ACT_NONE>(b, (i - na) / across, (i - na) % across, 0, m);
     }
 }
 
@@ -212,19 +316,27 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
     if (a.hc) store8<bf16_t>(a.hc, m * x.N + n, left, h);
 }
 
-template <typename DT> hipError_t tiles(const Q8TileArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.M + TILE - 1) / TILE), (unsigned)((a.N + TILE - 1) / TILE));
-    if (a.mode == Q8_VALUES) hipLaunchKernelGGL((q8_tile_kernel<DT, Q8_VALUES>), grid, dim3(NT), 0, s, a);
-    else if constexpr (sizeof(DT) == 2) {
-        if (a.mode == Q8_ACT) hipLaunchKernelGGL((q8_tile_kernel<DT, Q8_ACT>), grid, dim3(NT), 0, s, a);
-        else hipLaunchKernelGGL((q8_tile_kernel<DT, Q8_PAIR>), grid, dim3(NT), 0, s, a);
-    }
-    return hipGetLastError();
+unsigned tiles_of(const Q8TileArgs& a) { return (unsigned)((a.M + TILE - 1) / TILE * ((a.N + TILE - 1) / TILE)); }
+template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
+    const unsigned na = MODE == Q8_PAIR ? (tiles_of(a) + 7) / 8 * 16 : tiles_of(a), nb = tiles_of(b);
+    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb), dim3(NT), 0, s, a, b, na);
+}
+template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
+    if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, s);
+    else if (a.act == ACT_GELU) tiles<bf16_t, MODE, ACT_GELU>(a, b, s);
+    else if (a.act == ACT_RELU) tiles<bf16_t, MODE, ACT_RELU>(a, b, s);
+    else tiles<bf16_t, MODE, ACT_NONE>(a, b, s);
 }
 
 }  // namespace
 
-hipError_t launch_q8_tiles(const Q8TileArgs& a, hipStream_t s) { return a.dtype == 1 ? tiles<bf16_t>(a, s) : tiles<float>(a, s); }
+hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
+    if (a.dtype != 1) tiles<float, Q8_VALUES, ACT_NONE>(a, b, s);
+    else if (a.mode == Q8_PAIR) by_act<Q8_PAIR>(a, b, s);
+    else if (a.mode == Q8_ACT) by_act<Q8_ACT>(a, b, s);
+    else tiles<bf16_t, Q8_VALUES, ACT_NONE>(a, b, s);
+    return hipGetLastError();
+}
 
 hipError_t launch_q8_repack(const Q8RepackArgs& a, hipStream_t s) {
     if (a.count == 0) return hipSuccess;
