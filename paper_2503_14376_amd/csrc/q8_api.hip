@@ -34,7 +34,7 @@ FwdLayout fwd_layout(int M, int K, int N, bool pair, bool x_off, bool w_off) {
     FwdLayout l{};
     l.move_x = moved(K, x_off);
     l.move_w = moved(K, w_off);
-    l.rows = q8_rows_applies(M, l.move_x || l.move_w);
+    l.rows = q8_rows_applies(M);
     Carver c(nullptr);
     if (l.rows) {       // that kernel reads the codes where they are
         l.move_x = l.move_w = false;

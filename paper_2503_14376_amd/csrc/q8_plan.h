@@ -32,6 +32,26 @@ inline bool q8_gate_inside(const GemmPlan& p) { return p.bn == 256 && p.split ==
 
 // ---- few rows -----------------------------------------------------------------------------------
 constexpr int Q8_ROWS_MAX = 32;
-inline bool q8_rows_applies(long M, bool copies) { return M <= 4 || (copies && M <= Q8_ROWS_MAX); }
+inline bool q8_rows_applies(long M) { return M <= Q8_ROWS_MAX; }
+// Slices as in gemm_plan.h, wherever the rows of x leave room for them: a block of work is 16 / slices rows of weights.  A slice's pieces of
+// 128 codes go round the wavefronts, `ahead` of them per wavefront in flight, so that few places stay empty: a place without a piece costs
+// what one with a piece does (4 tokens through a pair of 10944 x 4096, 8 pieces a slice: four wavefronts with two pieces 18.4 us, with four
+// 37.2; through 4096 x 10944, 22 pieces: eight wavefronts with one 11.0, with two 13.3).  hold: a wavefront's share of x is one turn, and
+// there are more blocks than the chip runs at a time.
+struct Q8RowsPlan { int row_blocks, slices, waves, ahead, blocks, grid; bool hold; };
+inline Q8RowsPlan q8_rows_plan(long M, int N, int K) {
+    Q8RowsPlan p{};
+    p.row_blocks = M <= 16 ? 1 : 2;
+    p.slices = M <= 4 ? 4 : (M <= 8 ? 2 : 1);
+    p.blocks = (N + 16 / p.slices - 1) / (16 / p.slices);
+    const int pieces = ((K + 127) / 128 + p.slices - 1) / p.slices;
+    p.waves = pieces < 16 ? 4 : (pieces >= 32 && p.blocks <= 256 ? 16 : 8);
+    const int one = (pieces + p.waves - 1) / p.waves, two = (pieces + 2 * p.waves - 1) / (2 * p.waves);
+    p.ahead = 2 * two <= one ? 2 : 1;
+    const int most = 256 * (p.waves == 4 ? 4 : 2);
+    p.hold = p.waves <= 8 && p.ahead == 2 && two == 1 && p.blocks > most;
+    p.grid = p.hold ? most : p.blocks;
+    return p;
+}
 
 }  // namespace tfla

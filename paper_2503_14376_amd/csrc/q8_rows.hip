@@ -149,24 +149,23 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
     }
 }
 
-// As many pieces in flight as the wavefronts' registers hold (of eight wavefronts U8, of sixteen U16).
-template <int MB, int SL, bool PAIR, int NW, int U> void launch(const Q8GemmArgs& a, const RowsPlan& p, hipStream_t s) {
+template <int MB, int SL, bool PAIR, int NW> void launch(const Q8GemmArgs& a, const Q8RowsPlan& p, hipStream_t s) {
     if constexpr (NW <= 8) {
         if (p.hold) {
-            hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, U, true>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+            hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, true>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
             return;
         }
     }
-    hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, U, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+    if (p.ahead == 2) hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+    else hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 1, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
 }
-template <int MB, int SL, bool PAIR> void go(const Q8GemmArgs& a, const RowsPlan& p, hipStream_t s) {
-    constexpr int V = rows_registers(2, MB, PAIR), U8 = rows_pieces(V, 8), U16 = rows_pieces(V, 16);
-    if (p.waves == 4) launch<MB, SL, PAIR, 4, U8>(a, p, s);
-    else if (p.waves == 8) launch<MB, SL, PAIR, 8, U8>(a, p, s);
-    else launch<MB, SL, PAIR, 16, U16>(a, p, s);
+template <int MB, int SL, bool PAIR> void go(const Q8GemmArgs& a, const Q8RowsPlan& p, hipStream_t s) {
+    if (p.waves == 4) launch<MB, SL, PAIR, 4>(a, p, s);
+    else if (p.waves == 8) launch<MB, SL, PAIR, 8>(a, p, s);
+    else launch<MB, SL, PAIR, 16>(a, p, s);
 }
 template <bool PAIR> void by_rows(const Q8GemmArgs& a, hipStream_t s) {
-    const RowsPlan p = rows_plan(a.g.M, a.g.N, (a.k + 1) / 2, PAIR, 2);      // (128 codes are as many bytes as 64 elements of bf16)
+    const Q8RowsPlan p = q8_rows_plan(a.g.M, a.g.N, a.k);
     if (p.slices == 4) go<1, 4, PAIR>(a, p, s);
     else if (p.slices == 2) go<1, 2, PAIR>(a, p, s);
     else if (p.row_blocks == 1) go<1, 1, PAIR>(a, p, s);

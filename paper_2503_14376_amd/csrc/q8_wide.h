@@ -8,27 +8,167 @@
 
 namespace tfla {
 
-// The pair's results, 32 rows at a time: bias, a and u where wanted, h = act(a) u, its scale and codes.  The 128 columns that share a scale
+// Results.  The matrix unit leaves a lane one column of a block of 32, rows in its registers.  Which column of the tile that is, the rows of
+// B in LDS decide: of a wavefront's W blocks lane n has the columns W n ... W n + W - 1, so that a row leaves as 32 neighbouring lanes with W
+// columns each, whole cache lines (16 lanes on one line a clock; with 16 rows of 16 bytes side by side, as gemm.h turns its blocks, a store
+// took 64 clocks of the address unit, 7 us of a pair's tile with a, u and h).
+//
+// One wavefront's MB x W blocks, 32 rows at a time; row0, col0: its first row and column.  Of the rows' registers a switch picks those of
+// a block: unrolled, what follows a product is code that a wavefront waits for line by line.
+template <int W> struct Columns { float v[W]; };
+template <int W> __device__ __forceinline__ Columns<W> load_columns(const float* p, long at, int left) {
+    Columns<W> r;
+    if (left >= W) __builtin_memcpy(&r, p + at, 4 * W);
+    else {
+#pragma unroll
+        for (int c = 0; c < W; ++c) r.v[c] = c < left ? p[at + c] : 0.0f;
+    }
+    return r;
+}
+template <int W> struct Packed { uint32_t w[W / 2]; };
+template <int W> __device__ __forceinline__ void store_columns(uint16_t* base, uint32_t at, int left, const float (&x)[W]) {
+    uint16_t* p = base + at;
+    Packed<W> k;
+#pragma unroll
+    for (int c = 0; c < W / 2; ++c) k.w[c] = pack_bf16x2(x[2 * c], x[2 * c + 1]);
+    if (left >= W) __builtin_memcpy(p, &k, 2 * W);
+    else {
+#pragma unroll
+        for (int c = 0; c < W; ++c)
+            if (c < left) p[c] = (uint16_t)(k.w[c / 2] >> (16 * (c & 1)));
+    }
+}
+// f(kind) with the activation as a constant: one branch for all values of a block
+template <typename F> __device__ __forceinline__ void by_activation(int act, F f) {
+    struct None { __device__ constexpr int operator()() const { return ACT_NONE; } };
+    struct Silu { __device__ constexpr int operator()() const { return ACT_SILU; } };
+    struct Gelu { __device__ constexpr int operator()() const { return ACT_GELU; } };
+    struct Relu { __device__ constexpr int operator()() const { return ACT_RELU; } };
+    if (act == ACT_SILU) f(Silu());
+    else if (act == ACT_GELU) f(Gelu());
+    else if (act == ACT_RELU) f(Relu());
+    else f(None());
+}
+#define TFLA_PICK(I)                                                            \
+    case I:                                                                     \
+        _Pragma("unroll") for (int j = 0; j < NA; ++j) cur[j] = acc[I][j];      \
+        break;
+#define TFLA_PICK_BLOCK(mb)                                        \
+    switch (mb) {                                                  \
+        TFLA_PICK(0) TFLA_PICK(1) TFLA_PICK(2) TFLA_PICK(3)        \
+        default: __builtin_unreachable();                          \
+    }
+
+// EPI_LINEAR, EPI_STORE, EPI_PART.  NA: blocks of columns, those of a pair's two matrices in turn (EPI_PART)
+template <int EPI, bool PAIR, int NA, bool FULL>
+__device__ __forceinline__ void q8_epilogue(const GemmArgs& a, const GemmWork& w, long row0, int col0, f32x16 (&acc)[4][NA], int lane) {
+    constexpr int W = PAIR ? NA / 2 : NA;
+    const int n = col0 + (lane & 31) * W, g = lane >> 5, left = FULL ? W : a.N - n;
+    // where register v's row begins, the same for all lanes, and a lane's place behind that: one address register, not one per row
+    const uint32_t place = (uint32_t)(4 * g * a.N + (lane & 31) * W), place_part = (uint32_t)(4 * g * a.ld_part + (lane & 31) * W);
+    Columns<W> bias;
+    if (EPI == EPI_LINEAR && a.bias[0]) bias = load_columns<W>(a.bias[0], n, left);
+    int blocks = 4;
+    asm("" : "+s"(blocks));
+#pragma unroll 1
+    for (int mb = 0; mb < blocks; ++mb) {
+        f32x16 cur[NA];
+        TFLA_PICK_BLOCK(mb)
+        const long m0 = row0 + mb * 32;
+        auto exists = [&](int v) { return FULL || (left > 0 && m0 + acc_row(v, g) < a.M); };
+        if constexpr (EPI == EPI_PART) {
+            const int planes = PAIR ? 2 : a.batch;
+#pragma unroll
+            for (int p = 0; p < (PAIR ? 2 : 1); ++p) {
+                float* to = partial_plane(a, planes, w.part, PAIR ? p : w.b) + m0 * a.ld_part + col0;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    Columns<W> x;
+#pragma unroll
+                    for (int c = 0; c < W; ++c) x.v[c] = cur[PAIR ? 2 * c + p : c][v];
+                    if (exists(v)) {
+                        float* d = to + acc_row(v, 0) * a.ld_part + place_part;
+                        if (left >= W) __builtin_memcpy(d, &x, 4 * W);
+                        else {
+#pragma unroll
+                            for (int c = 0; c < W; ++c)
+                                if (c < left) d[c] = x.v[c];
+                        }
+                    }
+                }
+            }
+        } else {
+            auto at = [&](int v) { return (m0 + acc_row(v, 0)) * a.N + col0; };
+            auto put = [&](void* p, int v0, int v1) {
+#pragma unroll
+                for (int v = v0; v < v1; ++v) {
+                    float x[W];
+#pragma unroll
+                    for (int c = 0; c < W; ++c) x[c] = cur[c][v];
+                    if (exists(v)) store_columns<W>(reinterpret_cast<uint16_t*>(p) + at(v), place, left, x);
+                }
+            };
+            if constexpr (EPI == EPI_LINEAR) {
+                if (a.bias[0]) {
+#pragma unroll
+                    for (int c = 0; c < W; ++c)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) cur[c][v] += bias.v[c];
+                }
+                if (a.z[0]) put(a.z[0], 0, 16);
+                if (a.act != ACT_NONE)
+                    by_activation(a.act, [&](auto kind) {
+#pragma unroll
+                        for (int c = 0; c < W; ++c)
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) cur[c][v] = act_value<bf16_t>(cur[c][v], kind());
+                    });
+                if (a.residual) {
+                    // (eight rows at a time: the registers hold no more beside the results)
+#pragma unroll
+                    for (int v0 = 0; v0 < 16; v0 += 8) {
+                        Packed<W> r[8];
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) {
+                            const uint16_t* p = reinterpret_cast<const uint16_t*>(a.residual) + at(v0 + v) + place;
+#pragma unroll
+                            for (int c = 0; c < W / 2; ++c) r[v].w[c] = 0;
+                            if (exists(v0 + v)) {
+                                if (left >= W) __builtin_memcpy(&r[v], p, 2 * W);
+                                else {
+#pragma unroll
+                                    for (int c = 0; c < W; ++c)
+                                        if (c < left) r[v].w[c / 2] |= (uint32_t)p[c] << (16 * (c & 1));
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < W; ++c)
+#pragma unroll
+                            for (int v = 0; v < 8; ++v) cur[c][v0 + v] += c & 1 ? bf16_hi_to_f32(r[v].w[c / 2]) : bf16_lo_to_f32(r[v].w[c / 2]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
+            put(a.out[EPI == EPI_STORE ? w.b : 0], 0, 16);
+        }
+    }
+}
+
+// A pair's results, 32 rows at a time, in transposed blocks as gemm.h turns them (two columns a lane, as above, are four times the stores: 651 -> 725 us): bias, a and u where wanted, h = act(a) u, its scale and codes.  The 128 columns that share a scale
 // are this tile's: two wavefronts hold 64 each and meet in `meet` (two areas in turn, so that one meeting per 32 rows is enough).
 template <bool FULL>
 __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0, int col0, int wm, int wn, f32x16 (&acc)[4][4], int lane,
                                                   uint32_t (*meet)[2][2][32]) {
+    constexpr int NA = 4;
     const GemmArgs& a = q.g;
     const int c = lane & 31, g = lane >> 5;
     int rows = 4;
     asm("" : "+s"(rows));
 #pragma unroll 1
     for (int mb = 0; mb < rows; ++mb) {
-        f32x16 cur[4];
-#define TFLA_PICK(I)                                                          \
-    case I:                                                                   \
-        _Pragma("unroll") for (int j = 0; j < 4; ++j) cur[j] = acc[I][j];     \
-        break;
-        switch (mb) {
-            TFLA_PICK(0) TFLA_PICK(1) TFLA_PICK(2) TFLA_PICK(3)
-            default: __builtin_unreachable();
-        }
-#undef TFLA_PICK
+        f32x16 cur[NA];
+        TFLA_PICK_BLOCK(mb)
         float v[4][8], u[4][8];
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
@@ -57,13 +197,16 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
         };
         ready(v, a.bias[0], a.z[0]);
         ready(u, a.bias[1], a.z[1]);
+        // (with a branch for each value the epilogue of a tile took 11 us of 55)
+        by_activation(a.act, [&](auto kind) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float h = act_value<bf16_t>(v[i][e], a.act) * u[i][e];
-                v[i][e] = FULL || e < left(i) ? h : 0.0f;
-            }
+                for (int e = 0; e < 8; ++e) {
+                    const float h = act_value<bf16_t>(v[i][e], kind()) * u[i][e];
+                    v[i][e] = FULL || e < left(i) ? h : 0.0f;
+                }
+        });
         if (q.hc) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) store8<bf16_t>(q.hc, at(i), left(i), v[i]);
@@ -100,6 +243,9 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
     }
 }
 
+#undef TFLA_PICK
+#undef TFLA_PICK_BLOCK
+
 template <int BN, bool PAIR, int EPI>
 __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int tms, int tns) {
     static_assert(EPI != EPI_GATED || (PAIR && BN == 256), "the tile holds the 128 columns of a scale");
@@ -114,7 +260,11 @@ __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1, l32 = lane & 31;
     OperandStream<128, false, 64, 256, 2, false> oa;
-    OperandStream<HB, false, PAIR ? HB : HB / 2, 256, 2, PAIR> ob;
+    // Row r of half H of B stands for the column of the tile that its place in the results has: of block j = r / 32 % NB of wavefront
+    // r / (32 NB) lane r % 32's column j (a pair's) or NB H + j among the W that are the lane's.  (A gate's blocks: rows in their order.)
+    constexpr int W = PAIR ? NB : 2 * NB;
+    constexpr bool TURNED = EPI == EPI_GATED;
+    OperandStream<HB, false, PAIR ? HB : NB, 256, 2, PAIR> ob;
     Scales sc;
     constexpr int NA = oa.N, NBQ = ob.N, LOADS = NA + NBQ;  // requests of a wavefront per phase, beside those of scales
     Q8StepStream<PAIR, 1> qs;
@@ -134,6 +284,11 @@ __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int 
     };
     oa.init(a.lda, tid);
     ob.init(a.ldb, tid);
+#pragma unroll
+    for (int j = 0; j < (TURNED ? 0 : NBQ); ++j) {
+        const int r = (wave + j * 4) * 8 + (lane >> 3), col = ((lane & 7) ^ swz_mask<SWZ_K, 8>(r)) * 8;
+        ob.goff[j] = (uint32_t)(((r / (32 * NB) * 32 * W + r % 32 * W + r / 32 % NB) * a.ldb + col) * 2);
+    }
     const uint32_t la = lds_addr(lds) + wave * 1024, lb = la + 2 * ASLOT, ls = lds_addr(lds) + 2 * (ASLOT + BSLOT) + wave * 256;
     uint32_t slot;              // of the step to request, 0 or 1
     KFragReader<64> kf;
@@ -154,7 +309,7 @@ __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int 
     do {                                                                                                                      \
         const int ks_ = (m) / (2 * NB), i_ = (m) / NB % 2, j_ = (m) % NB, c_ = PAIR ? j_ * 2 + (HB_) : (HB_) * NB + j_;        \
         __builtin_amdgcn_sched_barrier(0);                                                                                    \
-        acc[(HA) * 2 + i_][c_] = mma_q8<EPI>(A[i_][ks_], B[j_][ks_], acc[(HA) * 2 + i_][c_], sa[(HA) * 2 + i_], sb[(HB_) * NB + j_]); \
+        acc[(HA) * 2 + i_][c_] = mma_q8<TURNED ? EPI_GATED : EPI_PART>(A[i_][ks_], B[j_][ks_], acc[(HA) * 2 + i_][c_], sa[(HA) * 2 + i_], sb[(HB_) * NB + j_]); \
     } while (0)
 #define TFLA_REQUEST(H, r)                                                                                                    \
     do {                                                                                                                      \
@@ -183,8 +338,8 @@ __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int 
         for (int i = 0; i < 4; ++i) na[i] = *reinterpret_cast<const int*>(p + (wm * 128 + i * 32) * 4);
 #pragma unroll
         for (int j = 0; j < 2 * NB; ++j) {
-            const int h = j / NB, r = PAIR ? h * HB + wn * NB * 32 + j % NB * 32 : wn * HB + h * (HB / 2) + j % NB * 32;
-            nb[j] = *reinterpret_cast<const int*>(p + (256 + r) * 4);
+            const int r = (PAIR ? j / NB * HB : 0) + wn * 32 * W + (PAIR ? j % NB : j) * (TURNED ? 32 : 1);
+            nb[j] = *reinterpret_cast<const int*>(p + (256 + r) * 4 + (TURNED ? 0 : l32 * 4 * (W - 1)));
         }
     };
     auto turn = [&]() {
@@ -308,13 +463,15 @@ __global__ void __launch_bounds__(256, 1) gemm_q8_wide_kernel(Q8GemmArgs q, int 
             if (full) q8_gated_epilogue<true>(q, drow, dcol, wm, wn, acc, lane, meet);
             else q8_gated_epilogue<false>(q, drow, dcol, wm, wn, acc, lane, meet);
         } else {
-            full = wave_epilogue<bf16_t, EPI, PAIR, 4, 2 * NB>(a, done, drow, dcol + wn * (PAIR ? NB * 32 : NB * 64), acc, lane);
+            const int col = dcol + wn * 32 * W;
+            full = drow + 128 <= a.M && col + 32 * W <= a.N;
+            if (full) q8_epilogue<EPI, PAIR, 2 * NB, true>(a, done, drow, col, acc, lane);
+            else q8_epilogue<EPI, PAIR, 2 * NB, false>(a, done, drow, col, acc, lane);
         }
         if (!more) break;
-        // the requests are older than the epilogue's operations, so its last stores need not have arrived.  Of a whole tile every lane
-        // stores 4 x 2 NB blocks in 16 bytes of two rows, partial results in 16 words, or a pair's codes in 4 x 4 pieces, at the least.
-        constexpr int STORES = EPI == EPI_GATED ? 16 : 4 * 2 * NB * (EPI == EPI_PART ? 16 : 2), NEWER = 8;
-        static_assert(STORES >= NEWER, "what may be under way is stores alone");
+        // the requests are older than the epilogue's operations, so its last stores need not have arrived: of a whole tile every lane stores
+        // 4 x 16 pieces at the least, a gate's codes 4 x 4.
+        constexpr int NEWER = EPI == EPI_GATED ? 16 : 32;
         if (full) wait_vmcnt<NEWER>();
         else wait_vmcnt<0>();
     }
