@@ -33,7 +33,7 @@ UNITS = [("api.hip", "api.o", []), ("gates.hip", "gates.o", []), ("step.hip", "s
     # matrix products: operand layouts 0 - 2, two products in one launch 3, + 4 for fp32
     ("gemm_inst.hip", "gemm%d.o" % l, ["-DTFLA_GEMM=%d" % l]) for l in range(8)] + [
     # products in 8 bits, by what follows them
-    ("q8_gemm_inst.hip", "q8_gemm%d.o" % v, ["-DTFLA_Q8=%d" % v]) for v in range(5)]
+    ("q8_gemm_inst.hip", "q8_gemm%d.o" % v, ["-DTFLA_Q8=%d" % v]) for v in range(6)]
 
 
 def _compile(unit):

@@ -34,7 +34,7 @@ FwdLayout fwd_layout(int M, int K, int N, bool pair, bool x_off, bool w_off) {
     FwdLayout l{};
     l.move_x = moved(K, x_off);
     l.move_w = moved(K, w_off);
-    l.rows = q8_rows_applies(M);
+    l.rows = q8_rows_applies(M, N, K, pair, l.move_x || l.move_w);
     Carver c(nullptr);
     if (l.rows) {       // that kernel reads the codes where they are
         l.move_x = l.move_w = false;
@@ -47,7 +47,7 @@ FwdLayout fwd_layout(int M, int K, int N, bool pair, bool x_off, bool w_off) {
             if (pair) { l.w1 = c.off; c.take(N * up16(K)); }
         }
     }
-    l.join = pair && (l.rows || !q8_gate_inside(l.plan));
+    l.join = pair && (l.rows || !q8_gate_inside(l.plan.bn, l.plan.split));
     l.part = c.off;
     if (l.plan.split > 1 || l.join) c.take((size_t)l.plan.split * (pair ? 2 : 1) * M * (((size_t)N + 7) & ~(size_t)7) * sizeof(float));
     l.bytes = c.off;
@@ -147,8 +147,10 @@ int product_bwd(const void* x, const void* const (&wqt)[2], const void* const (&
     uint8_t* ws = u8(workspace);
     const bool want_dw = dw[0] || dw[1], want_db = db[0] || db[1];
     const long Np = up16(N), Mp = up16(M);
+    const bool one = blocks(M) == 1;         // (block of rows: its sums are the results)
+    Q8Sums sums{reinterpret_cast<float*>(ws + l.dbpart), (int)blocks(M), want_db && !one ? P : 0, N, {db[0], db[1]}};
     if (M > 0 && (dx || want_dw || want_db)) {
-        Q8TileArgs a{};
+        Q8TileArgs a{}, b{};
         a.x = dy; a.z = z; a.u = u; a.M = M; a.N = N; a.act = act; a.dtype = TFLA_BF16; a.rows = 1;
         a.mode = pair ? Q8_PAIR : (act != TFLA_ACT_NONE ? Q8_ACT : Q8_VALUES);
         for (int p = 0; p < P; ++p) {
@@ -156,46 +158,44 @@ int product_bwd(const void* x, const void* const (&wqt)[2], const void* const (&
             if (dx) { o.q = ws + l.dz[p]; o.s = ws + l.s[p]; o.ldq = Np; o.lds = M; o.wq = (int)Np; }
             if (want_dw) { o.qt = ws + l.dzt[p]; o.st = ws + l.st[p]; o.ldt = Mp; o.ldst = N; o.wt = (int)Mp; }
         }
-        const bool one = blocks(M) == 1;
-        if (want_db && !one) { a.part = reinterpret_cast<float*>(ws + l.dbpart); a.ldp = N; }
+        if (sums.planes) { a.part = reinterpret_cast<float*>(ws + l.dbpart); a.ldp = N; }
         if (one) { a.db[0] = db[0]; a.db[1] = db[1]; }
-        Q8TileArgs b{};
         if (want_dw) {      // x along the tokens
             b.x = x; b.M = M; b.N = K; b.dtype = TFLA_BF16; b.rows = 1; b.mode = Q8_VALUES;
             Q8Out& o = b.out[0];
             o.qt = ws + l.xt; o.st = ws + l.sx; o.ldt = Mp; o.ldst = K; o.wt = (int)Mp;
         }
-        TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, b, s));
-    }
-    if (want_db && blocks(M) != 1)
-        TFLA_LAUNCH(K_ACT_BWD, launch_sum_rows(reinterpret_cast<float*>(ws + l.dbpart), (int)blocks(M), (long)P * N, N, N, db[0], db[1], s));
-    if (dx && M > 0) {
-        Q8GemmArgs q{};
-        operands(q, Np, N, M, K, N);
-        q.lsa = M; q.lsb = blocks(K); q.shb = 7;
         Q8RepackArgs rp{};
         rp.cols = N; rp.ldd = Np;
+        for (int p = 0; p < P && dx && l.move_w; ++p) rp.add(u8(wqt[p]), ws + l.w[p], K);
+        TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, b, rp, s));
+    }
+    Q8GemmArgs qx{}, qw{};
+    if (dx && M > 0) {
+        operands(qx, Np, N, M, K, N);
+        qx.lsa = M; qx.lsb = blocks(K); qx.shb = 7;
         for (int p = 0; p < P; ++p) {
-            q.g.A[p] = ws + l.dz[p]; q.sa[p] = ws + l.s[p];
-            q.g.B[p] = wqt[p]; q.sb[p] = u8(wt_scale[p]);
-            if (l.move_w) {
-                rp.add(u8(wqt[p]), ws + l.w[p], K);
-                q.g.B[p] = ws + l.w[p]; q.g.ldb = Np / 2;
-            }
+            qx.g.A[p] = ws + l.dz[p]; qx.sa[p] = ws + l.s[p];
+            qx.g.B[p] = l.move_w ? ws + l.w[p] : u8(wqt[p]); qx.sb[p] = u8(wt_scale[p]);
         }
-        if (rp.count > 0) TFLA_LAUNCH(K_ACT_BWD, launch_q8_repack(rp, s));
-        q.g.segs = P; q.g.out[0] = dx; q.g.split = l.plan_dx.split; q.g.part = reinterpret_cast<float*>(ws + l.part);
-        TFLA_LAUNCH(K_GEMM, launch_q8_gemm(q, l.plan_dx, EPI_STORE, s));
+        if (l.move_w) qx.g.ldb = Np / 2;
+        qx.g.segs = P; qx.g.out[0] = dx; qx.g.split = l.plan_dx.split; qx.g.part = reinterpret_cast<float*>(ws + l.part);
     }
     if (want_dw) {
-        Q8GemmArgs q{};
-        operands(q, Mp, Mp, N, K, M);
-        q.lsa = N; q.lsb = K; q.shb = 0;
-        for (int p = 0; p < P; ++p) { q.g.A[p] = ws + l.dzt[p]; q.sa[p] = ws + l.st[p]; q.g.out[p] = dw[p]; }
-        q.g.B[0] = ws + l.xt; q.sb[0] = q.sb[1] = ws + l.sx;
-        q.g.batch = P; q.g.split = l.plan_dw.split; q.g.part = reinterpret_cast<float*>(ws + l.part);
-        TFLA_LAUNCH(K_GEMM, launch_q8_gemm(q, l.plan_dw, EPI_STORE, s));
+        operands(qw, Mp, Mp, N, K, M);
+        qw.lsa = N; qw.lsb = K; qw.shb = 0;
+        for (int p = 0; p < P; ++p) { qw.g.A[p] = ws + l.dzt[p]; qw.sa[p] = ws + l.st[p]; qw.g.out[p] = dw[p]; }
+        qw.g.B[0] = ws + l.xt; qw.sb[0] = qw.sb[1] = ws + l.sx;
+        qw.g.batch = P; qw.g.split = l.plan_dw.split; qw.g.part = reinterpret_cast<float*>(ws + l.part);
     }
+    if (qx.g.M > 0 && qw.g.M > 0 && q8_both_applies(l.plan_dx, l.plan_dw, M, K, N, pair)) {
+        qx.g.split = qw.g.split = 1;
+        TFLA_LAUNCH(K_GEMM, launch_q8_both(qx, qw, sums, s));
+        return TFLA_OK;
+    }
+    if (want_db && !one) TFLA_LAUNCH(K_ACT_BWD, launch_sum_rows(sums.part, sums.rows, (long)P * N, N, N, db[0], db[1], s));
+    if (qx.g.M > 0) TFLA_LAUNCH(K_GEMM, launch_q8_gemm(qx, l.plan_dx, EPI_STORE, s));
+    if (qw.g.M > 0) TFLA_LAUNCH(K_GEMM, launch_q8_gemm(qw, l.plan_dw, EPI_STORE, s));
     return TFLA_OK;
 }
 
@@ -227,7 +227,7 @@ int tfla_q8_quant(const void* x, int M, int K, int dtype, int rows, void* q, voi
     Q8TileArgs a{};
     a.x = x; a.M = M; a.N = K; a.dtype = dtype; a.rows = rows; a.mode = Q8_VALUES;
     a.out[0] = {u8(q), u8(scale), u8(qt), u8(scale_t), K, rows == 1 ? M : blocks(M), M, rows == 1 ? K : blocks(K), K, M};
-    TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, {}, s));
+    TFLA_LAUNCH(K_ACT_BWD, launch_q8_tiles(a, {}, {}, s));
     return TFLA_OK;
 }
 

@@ -39,7 +39,8 @@ template <int AR, int BR, int NW, bool PAIR> struct ScaleStream {
             const int r = (ofa ? q : q - AR / 64) * 64, m = PAIR && !ofa ? r / (BR / 2) : 0;
             const int sh = ofa ? 0 : a.shb;
             const long first = ofa ? row0 + r : (long)col0 + r - m * (BR / 2), extent = ofa ? a.g.M : a.g.N, ld = ofa ? a.lsa : a.lsb;
-            const uint8_t* p = ofa ? a.sa[second ? 1 : w.b] : a.sb[PAIR ? m : (second ? 1 : 0)];
+            // (members by constant indices: with others the compiler keeps the arguments in memory, where a descriptor cannot be)
+            const uint8_t* p = ofa ? (second || w.b ? a.sa[1] : a.sa[0]) : ((PAIR ? m != 0 : second) ? a.sb[1] : a.sb[0]);
             const uint64_t b = reinterpret_cast<uint64_t>(p) + (uint64_t)(block * ld + (first >> sh));
             d[j][0] = (uint32_t)b;
             d[j][1] = (uint32_t)(b >> 32) & 0xffffu;
@@ -73,12 +74,15 @@ template <bool PAIR, int STRIDE> struct Q8StepStream {
     StepStream<PAIR, STRIDE> st;
     template <typename OA, typename OB, typename SC>
     __device__ __forceinline__ void find(const Q8GemmArgs& a, const GemmWork& w, long row0, int col0, OA& oa, OB& ob, SC& sc, int tid) {
-        st.find(a.g, w, row0, col0, oa, ob, tid);
-        scales(a, w, row0, col0, sc, tid);
-    }
-    template <typename SC> __device__ __forceinline__ void scales(const Q8GemmArgs& a, const GemmWork& w, long row0, int col0, SC& sc, int tid) {
         const bool on = st.at < st.k_end, second = st.at >= st.ksteps;
-        sc.set(a, w, row0, col0, on ? (second ? st.at - st.ksteps : st.at) : 0, second, on, tid);
+        const int block = on ? (second ? st.at - st.ksteps : st.at) : 0;
+        const void* pa = second || w.b ? a.g.A[1] : a.g.A[0];
+        const void* pb = second && !PAIR ? a.g.B[1] : a.g.B[0];
+        oa.set(pa, pa, a.g.lda, row0, a.g.M, a.g.K, block * 64, on, tid);
+        ob.set(pb, PAIR ? a.g.B[1] : pb, a.g.ldb, col0, a.g.N, a.g.K, block * 64, on, tid);
+        sc.set(a, w, row0, col0, block, second, on, tid);
+        const int seg_end = second ? 2 * st.ksteps : st.ksteps, whole = seg_end - (a.g.K % 64 != 0);
+        st.change = !on ? 0x7fffffff : min(st.k_end, st.at < whole ? whole : seg_end);
     }
     template <typename OA, typename OB, typename SC>
     __device__ __forceinline__ void next(const Q8GemmArgs& a, const GemmWork& w, long row0, int col0, OA& oa, OB& ob, SC& sc, int tid) {
@@ -91,18 +95,19 @@ template <bool PAIR, int STRIDE> struct Q8StepStream {
 };
 
 // Tile BM x BN, WM x WN wavefronts, S LDS stages, KG groups of wavefronts: as gemm_bf16.
+template <int BM, int BN, int WM, int WN, int S, int KG, bool PAIR> constexpr int gemm_q8_lds = KG * S * ((BM + BN) * 128 + ScaleStream<BM, BN, WM * WN, PAIR>::BYTES);
 template <int BM, int BN, int WM, int WN, int S, int KG, bool PAIR, int EPI>
-__global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_q8_kernel(Q8GemmArgs a, int tms, int tns) {
+__device__ __forceinline__ void gemm_q8(const Q8GemmArgs& a, int tms, int tns, unsigned id, unsigned total, char* lds) {
     constexpr int NT = WM * WN * 64, TM = BM / WM, TN = BN / WN, MB = TM / 32, NB = TN / 32, BNO = PAIR ? BN / 2 : BN;
     typedef ScaleStream<BM, BN, WM * WN, PAIR> Scales;
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128, TILES = ABYTES + BBYTES, STAGE = TILES + Scales::BYTES;
     constexpr int JOIN = (KG - 1) * WM * WN * MB * NB * 4096;
     static_assert(JOIN <= KG * S * STAGE, "the groups' results fit the stages");
-    __shared__ __align__(1024) char lds[KG * S * STAGE];
+    static_assert(KG * S * STAGE == gemm_q8_lds<BM, BN, WM, WN, S, KG, PAIR>, "the stages");
     const int tid = threadIdx.x % NT, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const int wm = wave / WN, wn = wave % WN, l32 = lane & 31;
-    const GemmWork w = gemm_work(xcd_range(blockIdx.x, gridDim.x), tms, tns, a.g.split);
+    const GemmWork w = gemm_work(xcd_range(id, total), tms, tns, a.g.split);
     const long row0 = (long)w.tm * BM;
     const int col0 = w.tn * BNO;
 
@@ -193,6 +198,32 @@ __global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_q8_kernel(Q8GemmArgs 
         for (int p = 0; p < KG - 1; ++p) join_add<MB, NB>(area, acc, p * WM * WN + wave, lane);
     }
     wave_epilogue<bf16_t, EPI, PAIR, MB, NB>(a.g, w, row0 + wm * TM, col0 + wn * (PAIR ? TN / 2 : TN), acc, lane);
+}
+
+template <int BM, int BN, int WM, int WN, int S, int KG, bool PAIR, int EPI>
+__global__ void __launch_bounds__(KG* WM* WN * 64, 2) gemm_q8_kernel(Q8GemmArgs a, int tms, int tns) {
+    __shared__ __align__(1024) char lds[gemm_q8_lds<BM, BN, WM, WN, S, KG, PAIR>];
+    gemm_q8<BM, BN, WM, WN, S, KG, PAIR, EPI>(a, tms, tns, blockIdx.x, gridDim.x, lds);
+}
+
+// Both products of a small backward pass in one launch, those with the longer contraction first, and behind them the column sums of the
+// bias gradients.  n: workgroups of the first product, of both, and all.
+template <int KG, int S>
+__global__ void __launch_bounds__(KG * 256, 2) gemm_q8_both_kernel(Q8GemmArgs x, Q8GemmArgs w, Q8Both n, Q8Sums sums) {
+    __shared__ __align__(1024) char lds[gemm_q8_lds<64, 64, 2, 2, S, KG, false>];
+    const unsigned i = blockIdx.x;
+    if (i < n.first) gemm_q8<64, 64, 2, 2, S, KG, false, EPI_STORE>(x, n.tms[0], n.tns[0], i, n.first, lds);
+    else if (i < n.both) gemm_q8<64, 64, 2, 2, S, KG, false, EPI_STORE>(w, n.tms[1], n.tns[1], i - n.first, n.both - n.first, lds);
+    else {
+        const int c = (i - n.both) * (KG * 256) + threadIdx.x, p = c / sums.n, col = c % sums.n;
+        float* out = p == 0 ? sums.out[0] : sums.out[1];
+        if (p >= sums.planes || !out) return;
+        const float* from = sums.part + c;
+        float s = 0.0f;
+#pragma unroll 8
+        for (int r = 0; r < sums.rows; ++r) s += from[(long)r * sums.planes * sums.n];
+        out[col] = s;
+    }
 }
 
 }  // namespace tfla

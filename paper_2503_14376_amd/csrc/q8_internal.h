@@ -25,8 +25,9 @@ struct Q8TileArgs {
     float* part; float* db[2];
     long M; int N; long ldp; int act, dtype, mode, rows;
 };
-// b: plain values in the same launch, none where b.M is 0
-hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s);
+struct Q8RepackArgs;
+// b: plain values in the same launch, none where b.M is 0; rp: copies in the same launch
+hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s);
 
 // y = norm(x + residual), its codes and scales; sum, y, rstd, mean may be NULL
 struct Q8NormArgs : RowNormArgs {
@@ -55,6 +56,11 @@ struct Q8GemmArgs {
 };
 // (a pair: EPI_GATED where q8_gate_inside, otherwise EPI_PART, which leaves the parts to launch_q8_gated_join)
 hipError_t launch_q8_gemm(const Q8GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);
+// column sums of (rows, planes, n) partial sums, in the order of the rows; either result may be NULL
+struct Q8Sums { const float* part; int rows, planes, n; float* out[2]; };
+struct Q8Both { unsigned first, both; int tms[2], tns[2]; };
+// both products of a small backward pass (whole ones, where q8_both_applies) and the sums (planes 0: none) in one launch
+hipError_t launch_q8_both(const Q8GemmArgs& x, const Q8GemmArgs& w, const Q8Sums& sums, hipStream_t s);
 hipError_t launch_q8_rows(const Q8GemmArgs& a, hipStream_t s);
 // h = act(a) u of a pair whose products lie in g.part (split parts of two planes), its codes and scales; stores a, u, h where wanted
 hipError_t launch_q8_gated_join(const Q8GemmArgs& a, hipStream_t s);

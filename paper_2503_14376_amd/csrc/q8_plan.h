@@ -4,7 +4,17 @@
 
 namespace tfla {
 
-// Tiles of 256 x 256 to 64 x 64 (pairs: 64 x 128); a step of the contraction is 128 codes.
+// Whether a pair's kernel forms h and its codes: a tile of 256 x 256 holds the 128 columns of a scale, all of their contraction.
+inline bool q8_gate_inside(int bn, int split) { return bn == 256 && split == 1; }
+
+// How a product is cut: the tile and the number of parts with the shortest time by a model as gemm_plan's, with steps of 128 codes.  Fitted to
+// 2500 times of 260 random products (33 to 8192 rows, 64 to 8192 columns, contractions of 128 to 8192; pairs, two segments, two at a
+// time): 8 % off in the mean, and what it picks is 1.3 % above the best of all choices on average, 23 % at most.  In us:
+//   256 x 256   8.7 + n (t (0.97 + 0.43 min(1, w / 256)) + 4.6)      (a pair with its gate inside: 11.2 in place of 4.6)
+//   256 x 128   6.6 + n (t (0.66 + 0.16 min(1, w / 256)) + 4.5)
+//   128 x 128   6.1 + t (0.43 + 0.28 w / 256) up to 256 workgroups, 7 + n (0.45 t + 0.5) + 1.5 max(0, n - 2) above
+//   64 x 64     5.6 + 0.193 t n + 1.2 max(0, n - 2)                  (pairs: 64 x 128, 0.396 t n)
+//   joining the parts, or a pair's gate outside   3.1 + (bytes written and read again) / 7 MB per us
 inline GemmPlan q8_plan(long M, int N, int K, int segs, int batch, int pair) {
     struct Tile { int bm, bn; };
     static constexpr Tile tiles[] = {{256, 256}, {256, 128}, {128, 128}, {64, 64}};
@@ -16,23 +26,32 @@ inline GemmPlan q8_plan(long M, int N, int K, int segs, int batch, int pair) {
         for (int split = 1; split <= 32 && (split == 1 || (all >= 4 * split && cells * split <= 1024)); split += split < 4 ? 1 : split / 2) {
             const double w = cells * split, t = (all + split - 1) / split, part = w < 256 ? w / 256 : 1, n = (double)(long)((w + 255) / 256);
             const double more = n > 2 ? n - 2 : 0;
+            const bool inside = pair && q8_gate_inside(bn, split);
             double us;
-            if (bn == 256) us = 8 + n * (t * (1.0 + 0.45 * part) + 4);
-            else if (bm == 256) us = 7 + n * (t * (0.63 + 0.31 * part) + 2);
-            else if (bm == 128) us = n < 2 ? 5 + t * (0.42 + 0.15 * part) : 6 + 0.49 * t * n + 1.5 * more;
-            else us = 4.8 + (pair ? 0.34 : 0.177) * t * n + 0.9 * more;
-            if (split > 1) us += 4.2 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
+            if (bn == 256) us = 8.7 + n * (t * (0.97 + 0.43 * part) + (inside ? 11.2 : 4.6));
+            else if (bm == 256) us = 6.6 + n * (t * (0.66 + 0.16 * part) + 4.5);
+            else if (bm == 128) us = n < 2 ? 6.1 + t * (0.43 + 0.28 * part) : 7 + n * (0.45 * t + 0.5) + 1.5 * more;
+            else us = 5.6 + (pair ? 0.396 : 0.193) * t * n + 1.2 * more;
+            if (split > 1 || (pair && !inside)) us += 3.1 + 8.0 * split * (pair ? 2 : batch) * (double)M * N / 7e6;
             if (best.bm == 0 || us < best.us) best = {bm, bn, split, us};
         }
     }
     return best;
 }
-// Whether a pair's kernel forms h and its codes: a tile of 256 x 256 holds the 128 columns of a scale, all of their contraction.
-inline bool q8_gate_inside(const GemmPlan& p) { return p.bn == 256 && p.split == 1; }
+
+// ---- both products of a small backward pass in one launch ------------------------------------------
+// dx and dw in tiles of 64 x 64, undivided, and the bias gradients' sums with them: a launch saved (3.4 us of the host's time, 2 of the GPU's; two
+// with sums), and the items of one product fill what the other leaves of the CUs' time, where by an estimate that is no slower.
+inline bool q8_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K, int N, int pair) {
+    auto up = [](long v, int by) { return (v + by - 1) / by; };
+    const long segs = pair ? 2 : 1, nx = up(M, 64) * up(K, 64), nw = up(N, 64) * up(K, 64) * segs, tx = up(N, 128) * segs, tw = up(M, 128);
+    const double share = (nx * tx + nw * tw) / 256.0, longest = tx > tw ? tx : tw, chain = (nx + nw > 256 ? 0.4 : 0.2) * longest;
+    const double us = 7.5 + (0.25 * share > chain ? 0.25 * share : chain);
+    return us <= x.us + w.us - 4;
+}
 
 // ---- few rows -----------------------------------------------------------------------------------
 constexpr int Q8_ROWS_MAX = 32;
-inline bool q8_rows_applies(long M) { return M <= Q8_ROWS_MAX; }
 // Slices as in gemm_plan.h, wherever the rows of x leave room for them: a block of work is 16 / slices rows of weights.  A slice's pieces of
 // 128 codes go round the wavefronts, `ahead` of them per wavefront in flight, so that few places stay empty: a place without a piece costs
 // what one with a piece does (4 tokens through a pair of 10944 x 4096, 8 pieces a slice: four wavefronts with two pieces 18.4 us, with four
@@ -52,6 +71,17 @@ inline Q8RowsPlan q8_rows_plan(long M, int N, int K) {
     p.hold = p.waves <= 8 && p.ahead == 2 && two == 1 && p.blocks > most;
     p.grid = p.hold ? most : p.blocks;
     return p;
+}
+// Whether this kernel takes a product or the tiles do: by estimates of both, here rounds of blocks at 30 GB/s per CU (one round: 39).  Calls,
+// here and there: 4096 x 4096, 8 rows 8.2 and 10.7 us, 32 rows 9.5 and 10.8; 4096 x 10944, 32 rows 15.5 and 14.4; pair of 10944 x 4096, 8
+// rows 22.5 and 22.2, 16 rows 28.7 and 22.5.  copies: operands that the tiles cannot read in place.
+inline bool q8_rows_applies(long M, int N, int K, int pair, bool copies) {
+    if (M <= 4 || M > Q8_ROWS_MAX) return M <= 4;
+    if (copies) return true;
+    const Q8RowsPlan p = q8_rows_plan(M, N, K);
+    const double bytes = (double)(16 / p.slices * (pair ? 2 : 1) + M) * K;
+    const double here = 1.8 + (p.blocks + 255) / 256 * bytes / (p.blocks <= 256 ? 39e3 : 30e3) + (pair ? 3.1 : 0);
+    return here <= q8_plan(M, N, K, 1, 1, pair).us;
 }
 
 }  // namespace tfla

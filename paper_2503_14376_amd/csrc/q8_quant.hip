@@ -241,9 +241,33 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
     }
 }
 
-// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0).  A pair's two
+// Rows of bytes at any address to rows of ldd bytes: block x of `across` of them, 16 bytes a lane
+constexpr int COPIES = 256;         // workgroups of a launch's copies, at most
+__device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block, unsigned blocks) {
+    const int per = (int)(a.ldd >> 4);
+    for (int q = 0; q < a.count; ++q) {
+        const long all = a.rows[q] * per;
+        for (long i = (long)block * NT + threadIdx.x; i < all; i += (long)blocks * NT) {
+            const long r = i / per;
+            const int c = (int)(i % per) * 16;
+            const uint8_t* p = a.src[q] + r * a.cols + c;
+            u32x4 w = {0u, 0u, 0u, 0u};
+            if (c + 16 <= a.cols) __builtin_memcpy(&w, p, 16);
+            else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (c + e < a.cols) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+            }
+            *reinterpret_cast<u32x4*>(a.dst[q] + r * a.ldd + c) = w;
+        }
+    }
+}
+__global__ void __launch_bounds__(NT) q8_repack_kernel(Q8RepackArgs a) { q8_repack(a, blockIdx.x, gridDim.x); }
+
+// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.  A pair's two
 // gradients of a tile are two workgroups that read the same tensors at about the same time on the same XCD (ids 8 apart).
-template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, unsigned na) {
+template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp, unsigned na,
+                                                                                              unsigned nb) {
     __shared__ __align__(16) TileMemory<typename Kept<DT, MODE>::type> m;
     const unsigned i = blockIdx.x;
     if (i < na) {
@@ -251,26 +275,11 @@ template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 
         const unsigned tile = MODE == Q8_PAIR ? (i >> 4) * 8 + (i & 7) : i;
         if (MODE == Q8_PAIR && tile >= across * (unsigned)((a.M + TILE - 1) / TILE)) return;
         q8_tile<DT, MODE, ACT>(a, tile / across, tile % across, MODE == Q8_PAIR ? (i >> 3) & 1 : 0, m);
+    } else if (i >= na + nb) {
+        q8_repack(rp, i - na - nb, gridDim.x - na - nb);
     } else {
         const unsigned across = (b.N + TILE - 1) / TILE;
         q8_tile<DT, Q8_VALUES, ACT_NONE>(b, (i - na) / across, (i - na) % across, 0, m);
-    }
-}
-
-__global__ void __launch_bounds__(256) q8_repack_kernel(Q8RepackArgs a) {
-    const int c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 16, q = blockIdx.z;
-    if (c >= a.ldd) return;
-    const long step = (long)gridDim.x * 4;
-    for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows[q]; r += step) {
-        const uint8_t* p = a.src[q] + r * a.cols + c;
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (c + 16 <= a.cols) __builtin_memcpy(&w, p, 16);
-        else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (c + e < a.cols) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
-        }
-        *reinterpret_cast<u32x4*>(a.dst[q] + r * a.ldd + c) = w;
     }
 }
 
@@ -317,34 +326,36 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
 }
 
 unsigned tiles_of(const Q8TileArgs& a) { return (unsigned)((a.M + TILE - 1) / TILE * ((a.N + TILE - 1) / TILE)); }
-template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
-    const unsigned na = MODE == Q8_PAIR ? (tiles_of(a) + 7) / 8 * 16 : tiles_of(a), nb = tiles_of(b);
-    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb), dim3(NT), 0, s, a, b, na);
+unsigned copies_of(const Q8RepackArgs& a) {
+    long all = 0;
+    for (int q = 0; q < a.count; ++q) all += a.rows[q] * (a.ldd >> 4);
+    const long n = (all + 4 * NT - 1) / (4 * NT);
+    return (unsigned)(n < COPIES ? n : COPIES);
 }
-template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
-    if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, s);
-    else if (a.act == ACT_GELU) tiles<bf16_t, MODE, ACT_GELU>(a, b, s);
-    else if (a.act == ACT_RELU) tiles<bf16_t, MODE, ACT_RELU>(a, b, s);
-    else tiles<bf16_t, MODE, ACT_NONE>(a, b, s);
+template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
+    const unsigned na = MODE == Q8_PAIR ? (tiles_of(a) + 7) / 8 * 16 : tiles_of(a), nb = tiles_of(b);
+    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb + copies_of(rp)), dim3(NT), 0, s, a, b, rp, na, nb);
+}
+template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
+    if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, rp, s);
+    else if (a.act == ACT_GELU) tiles<bf16_t, MODE, ACT_GELU>(a, b, rp, s);
+    else if (a.act == ACT_RELU) tiles<bf16_t, MODE, ACT_RELU>(a, b, rp, s);
+    else tiles<bf16_t, MODE, ACT_NONE>(a, b, rp, s);
 }
 
 }  // namespace
 
-hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, hipStream_t s) {
-    if (a.dtype != 1) tiles<float, Q8_VALUES, ACT_NONE>(a, b, s);
-    else if (a.mode == Q8_PAIR) by_act<Q8_PAIR>(a, b, s);
-    else if (a.mode == Q8_ACT) by_act<Q8_ACT>(a, b, s);
-    else tiles<bf16_t, Q8_VALUES, ACT_NONE>(a, b, s);
+hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
+    if (a.dtype != 1) tiles<float, Q8_VALUES, ACT_NONE>(a, b, rp, s);
+    else if (a.mode == Q8_PAIR) by_act<Q8_PAIR>(a, b, rp, s);
+    else if (a.mode == Q8_ACT) by_act<Q8_ACT>(a, b, rp, s);
+    else tiles<bf16_t, Q8_VALUES, ACT_NONE>(a, b, rp, s);
     return hipGetLastError();
 }
 
 hipError_t launch_q8_repack(const Q8RepackArgs& a, hipStream_t s) {
     if (a.count == 0) return hipSuccess;
-    long most = 1;
-    for (int q = 0; q < a.count; ++q) most = a.rows[q] > most ? a.rows[q] : most;
-    const long n = (most + 3) / 4;
-    const dim3 grid((unsigned)(n < 1024 ? n : 1024), (unsigned)((a.ldd + 1023) / 1024), a.count);
-    hipLaunchKernelGGL(q8_repack_kernel, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(q8_repack_kernel, dim3(copies_of(a)), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
 

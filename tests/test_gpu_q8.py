@@ -244,7 +244,7 @@ def few_values(gen, R, C, most=2):
     return (v * torch.randint(-1, 2, (R, C), generator=gen, device="cuda")).to(BF16)
 
 
-LARGE = [(300, 200, 260), (1000, 1100, 1365), (4100, 2600, 2000), (2000, 4200, 2600), (4096, 4096, 2048)]
+LARGE = [(40, 100, 72), (300, 200, 260), (515, 1030, 700), (1500, 300, 2000), (1000, 1100, 1365), (4100, 2600, 2000), (2000, 4200, 2600), (4096, 4096, 2048)]
 
 
 @pytest.mark.parametrize("M,K,N", LARGE)
