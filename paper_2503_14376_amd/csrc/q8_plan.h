@@ -46,8 +46,8 @@ inline bool q8_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K,
     auto up = [](long v, int by) { return (v + by - 1) / by; };
     const long segs = pair ? 2 : 1, nx = up(M, 64) * up(K, 64), nw = up(N, 64) * up(K, 64) * segs, tx = up(N, 128) * segs, tw = up(M, 128);
     const double share = (nx * tx + nw * tw) / 256.0, longest = tx > tw ? tx : tw, chain = (nx + nw > 256 ? 0.4 : 0.2) * longest;
-    const double us = 7.5 + (0.25 * share > chain ? 0.25 * share : chain);
-    return us <= x.us + w.us - 4;
+    const double us = 7.5 + (0.31 * share > chain ? 0.31 * share : chain);
+    return us <= x.us + w.us + 2;
 }
 
 // ---- few rows -----------------------------------------------------------------------------------
