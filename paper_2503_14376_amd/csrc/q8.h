@@ -22,15 +22,17 @@ __device__ __forceinline__ uint32_t q8_scale(uint32_t most) {
     const int b = (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u);
     return (uint32_t)(b > 0 ? b : 0);
 }
-// 2^-e
-__device__ __forceinline__ float q8_inverse(uint32_t scale) { return __builtin_bit_cast(float, (254u - scale) << 23); }
-// four values times inv -> four codes
-__device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+// 2^e as the conversions take it: of its bits they read the exponent alone, so that the byte 0 (2^-127) needs no denormal
+__device__ __forceinline__ float q8_power(uint32_t scale) { return __builtin_bit_cast(float, scale << 23); }
+// four values times 2^-e -> four codes
+__device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d, float power) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, power, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, power, true));
 }
-__device__ __forceinline__ u32x2 q8_codes8(const float (&v)[8], float inv) {
-    return u32x2{q8_codes(v[0], v[1], v[2], v[3], inv), q8_codes(v[4], v[5], v[6], v[7], inv)};
+__device__ __forceinline__ u32x2 q8_codes8(const float (&v)[8], float power) {
+    return u32x2{q8_codes(v[0], v[1], v[2], v[3], power), q8_codes(v[4], v[5], v[6], v[7], power)};
 }
 __device__ __forceinline__ uint32_t q8_magnitude8(const float (&v)[8]) {
     uint32_t m = 0;

@@ -35,25 +35,6 @@ template <int ACT> __device__ __forceinline__ float act_fine(float z, float& slo
     } else return act_both<float>(z, ACT, slope);
 }
 
-// maximum (sum) over the lanes 16 and 32 apart, which hold other rows of the same columns
-__device__ __forceinline__ uint32_t rows_max(uint32_t x) {
-    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const uint32_t p0 = p[0], p1 = p[1], y = max(p0, p1);
-    const auto q = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    const uint32_t q0 = q[0], q1 = q[1];
-    return max(q0, q1);
-}
-__device__ __forceinline__ float rows_sum(float x) {
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const unsigned p0 = p[0], p1 = p[1];
-    const float y = __builtin_bit_cast(float, p0) + __builtin_bit_cast(float, p1);
-    const unsigned w = __builtin_bit_cast(unsigned, y);
-    const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    const unsigned q0 = q[0], q1 = q[1];
-    return __builtin_bit_cast(float, q0) + __builtin_bit_cast(float, q1);
-}
-
 // A tile's values, for what has to wait for its scale: bf16 where they are bf16, else fp32.  A row's columns are turned by 32 bytes from one
 // block of 16 rows to the next, so that the transposed reads, 8 columns of 8 such blocks at a time, meet no bank twice.
 template <typename VT> struct TileValues {
@@ -63,8 +44,7 @@ template <typename VT> struct TileValues {
 };
 template <typename VT> struct TileMemory {
     TileValues<VT> values;
-    float colsum[WAVES][TILE];
-    uint32_t colmax[TILE];
+    uint32_t most[WAVES];
 };
 template <typename DT, int MODE> struct Kept { typedef float type; };
 template <> struct Kept<bf16_t, Q8_VALUES> { typedef bf16_t type; };
@@ -91,24 +71,34 @@ __device__ __forceinline__ void into_place(Vec8<float>& x, int shift) {
     if (shift >= 8) x.zero();
 }
 
-// Tile (bx, by) of matrix p.  Thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r, r + 32, r + 64, r + 96: what a row
-// needs is done there, from registers; what a column needs is kept in LDS until the column's scale is known.  All rows are requested at once.
-// Where an activation follows, their loop is not unrolled (a switch picks the registers): code that a workgroup runs through once is waited
-// for line by line (unrolled, 28 KB, a pair of 1000 x 1365 took 32 us).
-template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline__ void q8_tile(const Q8TileArgs& a, int bx, int by, int p, MEM& m) {
+// magnitudes of N values, of which what is not finite does not count, and the largest of them
+template <int N> __device__ __forceinline__ uint32_t largest(const float (&v)[N]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = max(most, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+    if (__any(most >= 0x7f800000u)) {       // (rare)
+        most = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) most = max(most, q8_magnitude(v[e]));
+    }
+    return most;
+}
+
+// Tile (bx, by).  By rows, thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r, r + 32, r + 64, r + 96: what a row needs is
+// done there, from registers, and the values are left in LDS for what a block or a column needs.  By columns, a thread takes 16 rows of a
+// column, eight neighbouring lanes all of it, so that neither scales nor sums need LDS.  A pair's second gradient waits in registers: a pair's
+// backward 8192 x 10944 takes 196 us (4.6 TB/s of its 898 MB; 265 with a tile of workgroups for each gradient, which computes the activation twice
+// and by rows from LDS), a weight of 10944 x 4096 with its transpose 39.5 (4.6 TB/s).  Small matrices pay for the unrolled rows, whose instructions
+// every workgroup fetches once (1000 x 1365 pair 16 -> 18).
+template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline__ void q8_tile(const Q8TileArgs& a, int bx, int by, MEM& m) {
     typedef typename Kept<DT, MODE>::type VT;
     typedef TileValues<VT> Values;
-    constexpr int ROWS = TILE / RPI;
-    static_assert(ROWS == 4, "the cases of the switch below");
-    const int t = threadIdx.x, g = t & 15, wave = t >> 6;
+    constexpr int ROWS = TILE / RPI, P = MODE == Q8_PAIR ? 2 : 1;
+    const int t = threadIdx.x, g = t & 15;
     const long r0 = (long)bx * TILE;
     const int c0 = by * TILE, c = c0 + g * 8, left = a.N - c;
-    const Q8Out& o = a.out[p];
-    float* db = a.part ? a.part + ((long)bx * (MODE == Q8_PAIR ? 2 : 1) + p) * a.ldp : a.db[p];
-    const bool blocks = a.rows > 1, columns = o.qt != nullptr, keep = columns || blocks;
+    const bool blocks = a.rows > 1;
     VT* const kept = reinterpret_cast<VT*>(&m);
-    if (t < TILE) m.colmax[t] = 0;
-    __syncthreads();
     Vec8<DT> x[ROWS], z[ROWS], u[ROWS];
     const int behind = left >= 8 ? 0 : min(8 - left, 8);      // by how much a read ends behind the row
     if (a.N >= 8) {
@@ -117,10 +107,7 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
             const long row = min(r0 + (t >> 4) + k * RPI, a.M - 1), at = row * a.N + min(c, a.N - 8);
             x[k].load(a.x, at);
             if constexpr (MODE != Q8_VALUES) z[k].load(a.z, at);
-            if constexpr (MODE == Q8_PAIR) {
-                if (p == 0) u[k].load(a.u, at);
-                else u[k].zero();
-            }
+            if constexpr (MODE == Q8_PAIR) u[k].load(a.u, at);
         }
     } else {
 #pragma unroll
@@ -128,158 +115,142 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
             const long row = min(r0 + (t >> 4) + k * RPI, a.M - 1);
             x[k] = load8<DT>(a.x, row * a.N + c, left);
             if constexpr (MODE != Q8_VALUES) z[k] = load8<DT>(a.z, row * a.N + c, left);
-            if constexpr (MODE == Q8_PAIR) u[k] = load8<DT>(a.u, row * a.N + c, p == 0 ? left : 0);
+            if constexpr (MODE == Q8_PAIR) u[k] = load8<DT>(a.u, row * a.N + c, left);
         }
     }
-    uint32_t cm[8];
-    float cs[8];
+    float second[MODE == Q8_PAIR ? ROWS : 1][8];
+    uint32_t all = 0;
+    auto keep = [&](int i, const float (&v)[8]) {
+        VT* d = kept + Values::place(i, g * 8);
+        if constexpr (sizeof(VT) == 4) {
+            *reinterpret_cast<f32x4*>(d) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(d + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    };
+    auto codes = [&](const Q8Out& o, int i, const float (&v)[8]) {
+        const uint32_t most = largest(v);
+        all = max(all, most);
+        if (!o.q || blocks) return;
+        const long row = r0 + i;
+        const uint32_t s = q8_scale(lanes_max<16>(most));
+        if (row < a.M) {
+            q8_store8(o.q + row * o.ldq + c, q8_codes8(v, q8_power(s)), o.wq - c);
+            if (g == 0) o.s[(long)by * o.lds + row] = (uint8_t)s;
+        }
+    };
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { cm[e] = 0; cs[e] = 0.0f; }
-    auto take = [&](int i, Vec8<DT> xk, Vec8<DT> zk, Vec8<DT> uk) {
+    for (int k = 0; k < ROWS; ++k) {
+        const int i = (t >> 4) + k * RPI;
         // (rows behind the last one have read it again)
         const int shift = r0 + i < a.M ? (a.N >= 8 ? behind : 0) : 8;
         if (__any(shift > 0)) {
-            into_place(xk, shift);
-            if constexpr (MODE != Q8_VALUES) into_place(zk, shift);
-            if constexpr (MODE == Q8_PAIR) into_place(uk, shift);
+            into_place(x[k], shift);
+            if constexpr (MODE != Q8_VALUES) into_place(z[k], shift);
+            if constexpr (MODE == Q8_PAIR) into_place(u[k], shift);
         }
         float v[8];
-        xk.get(v);
-        if constexpr (sizeof(VT) == 2) {
-            if (keep) *reinterpret_cast<u32x4*>(kept + Values::place(i, g * 8)) = xk.w;
-        }
+        x[k].get(v);
+        if constexpr (sizeof(VT) == 2) *reinterpret_cast<u32x4*>(kept + Values::place(i, g * 8)) = x[k].w;
         if constexpr (MODE != Q8_VALUES) {
             float zf[8], uf[8];
-            zk.get(zf);
-            if (MODE == Q8_PAIR && p == 0) uk.get(uf);
+            z[k].get(zf);
+            if constexpr (MODE == Q8_PAIR) u[k].get(uf);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float slope;
                 const float value = act_fine<ACT>(zf[e], slope);
-                if (MODE == Q8_PAIR) v[e] = p > 0 ? v[e] * value : v[e] * uf[e] * slope;
-                else v[e] *= slope;
+                if constexpr (MODE == Q8_PAIR) {
+                    second[k][e] = v[e] * value;
+                    v[e] *= uf[e];
+                }
+                v[e] *= slope;
             }
         }
-        uint32_t w[8], most = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[e] = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
-            most = max(most, w[e]);
+        codes(a.out[0], i, v);
+        keep(i, v);
+        if constexpr (MODE == Q8_PAIR) {
+            codes(a.out[1], i, second[k]);
+            // (row after row, so that the registers do for two workgroups on a CU)
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (__any(most >= 0x7f800000u)) {       // (rare: what is not finite does not count)
-            most = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = w[e] < 0x7f800000u ? w[e] : 0u;
-                most = max(most, w[e]);
-            }
-        }
-        const long row = r0 + i;
-        if (o.q && !blocks) {
-            const uint32_t s = q8_scale(lanes_max<16>(most));
-            if (row < a.M) {
-                q8_store8(o.q + row * o.ldq + c, q8_codes8(v, q8_inverse(s)), o.wq - c);
-                if (g == 0) o.s[(long)by * o.lds + row] = (uint8_t)s;
-            }
-        }
-        if constexpr (sizeof(VT) == 4) {
-            if (keep) {
-                float* d = kept + Values::place(i, g * 8);
-                *reinterpret_cast<f32x4*>(d) = f32x4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4*>(d + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cm[e] = max(cm[e], w[e]);
-            cs[e] += v[e];
-        }
-    };
-    if constexpr (MODE == Q8_VALUES) {
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) take((t >> 4) + k * RPI, x[k], z[k], u[k]);
-    } else {
-        int rows = ROWS;
-        asm("" : "+s"(rows));
-#pragma unroll 1
-        for (int k = 0; k < rows; ++k) {
-            Vec8<DT> xk, zk, uk;
-#define TFLA_PICK(K)                                    \
-    case K:                                             \
-        xk = x[K];                                      \
-        zk = z[K];                                      \
-        if constexpr (MODE == Q8_PAIR) uk = u[K];       \
-        break;
-            switch (k) {
-                TFLA_PICK(0) TFLA_PICK(1) TFLA_PICK(2) TFLA_PICK(3)
-                default: __builtin_unreachable();
-            }
-#undef TFLA_PICK
-            take((t >> 4) + k * RPI, xk, zk, uk);
-        }
-    }
-    if (keep) {
-        // (the largest of a set does not depend on the order in which the wavefronts come)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cm[e] = rows_max(cm[e]);
-            if ((t & 48) == 0) atomicMax(&m.colmax[g * 8 + e], cm[e]);
-        }
-    }
-    if (db) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cs[e] = rows_sum(cs[e]);
-            if ((t & 48) == 0) m.colsum[wave][g * 8 + e] = cs[e];
-        }
-    }
-    __syncthreads();
-    if (db && t < TILE && c0 + t < a.N) {
-        float s = m.colsum[0][t];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += m.colsum[w][t];
-        db[c0 + t] = s;
     }
     uint32_t whole = 0;         // the scale of a block
     if (blocks) {
-        whole = q8_scale(lanes_max<64>(max(m.colmax[t & 63], m.colmax[64 + (t & 63)])));
+        all = lanes_max<64>(all);
+        if ((t & 63) == 0) m.most[t >> 6] = all;
+    }
+    __syncthreads();
+    if (blocks) {
+        const Q8Out& o = a.out[0];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) whole = max(whole, m.most[w]);
+        whole = q8_scale(whole);
         if (t == 0 && o.q) o.s[(long)by * o.lds + bx] = (uint8_t)whole;
-        if (t == 0 && columns) o.st[(long)bx * o.ldst + by] = (uint8_t)whole;
+        if (t == 0 && o.qt) o.st[(long)bx * o.ldst + by] = (uint8_t)whole;
         if (o.q) {
 #pragma unroll 1
             for (int i = t >> 4; i < TILE && r0 + i < a.M; i += RPI) {
                 float v[8];
                 load8<VT>(kept, Values::place(i, g * 8), 8).get(v);
-                q8_store8(o.q + (r0 + i) * o.ldq + c, q8_codes8(v, q8_inverse(whole)), o.wq - c);
+                q8_store8(o.q + (r0 + i) * o.ldq + c, q8_codes8(v, q8_power(whole)), o.wq - c);
             }
         }
     }
-    if (!columns) return;
-    // rows of the transpose: eight pieces of 16 codes each
-#pragma unroll 1
-    for (int i = t; i < TILE * 8; i += NT) {
-        const int col = i >> 3, at = (i & 7) * 16;
-        const long n = o.wt - r0 - at;
-        if (c0 + col >= a.N || n <= 0) continue;
-        const uint32_t s = blocks ? whole : q8_scale(m.colmax[col]);
-        const float inv = q8_inverse(s);
-        const VT* d = kept + Values::place(at, col);        // (whole blocks of 16 rows are turned alike)
-        auto at_row = [&](int r) { return (float)d[r * Values::PITCH]; };
-        uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = q8_codes(at_row(4 * e), at_row(4 * e + 1), at_row(4 * e + 2), at_row(4 * e + 3), inv);
-        uint8_t* to = o.qt + (long)(c0 + col) * o.ldt + r0 + at;
-        if (n >= 16) __builtin_memcpy(to, w, 16);
-        else {
-            for (int e = 0; e < n; ++e) {
-                uint32_t q = w[0];
-                q = e >= 4 ? w[1] : q;
-                q = e >= 8 ? w[2] : q;
-                q = e >= 12 ? w[3] : q;
-                to[e] = (uint8_t)(q >> (8 * (e & 3)));
+    for (int p = 0; p < P; ++p) {
+        const Q8Out& o = a.out[p];
+        float* db = a.part ? a.part + ((long)bx * P + p) * a.ldp : a.db[p];
+        if constexpr (MODE == Q8_PAIR) {
+            if (p > 0) {
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) keep((t >> 4) + k * RPI, second[k]);
+                __syncthreads();
             }
         }
-        if (at == 0 && !blocks) o.st[(long)bx * o.ldst + c0 + col] = (uint8_t)s;
+        if (!o.qt && !db) continue;
+        // rows of the transpose: eight pieces of 16 codes each
+#pragma unroll 1
+        for (int i = t; i < TILE * 8; i += NT) {
+            const int col = i >> 3, at = (i & 7) * 16;
+            const VT* d = kept + Values::place(at, col);        // (whole blocks of 16 rows are turned alike)
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = (float)d[e * Values::PITCH];
+            if (db) {
+                float s = v[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) s += v[e];
+                s = lanes_sum<8>(s);
+                if (at == 0 && c0 + col < a.N) db[c0 + col] = s;
+            }
+            if (!o.qt) continue;
+            uint32_t s = whole;
+            if (!blocks) {
+                uint32_t most = largest(v);
+                most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, true));
+                most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4e, 0xf, 0xf, true));
+                s = q8_scale(max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x141, 0xf, 0xf, true)));
+                if (at == 0 && c0 + col < a.N) o.st[(long)bx * o.ldst + c0 + col] = (uint8_t)s;
+            }
+            const long n = o.wt - r0 - at;
+            if (c0 + col >= a.N || n <= 0) continue;
+            const float power = q8_power(s);
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = q8_codes(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], power);
+            uint8_t* to = o.qt + (long)(c0 + col) * o.ldt + r0 + at;
+            if (n >= 16) __builtin_memcpy(to, w, 16);
+            else {
+                for (int e = 0; e < n; ++e) {
+                    uint32_t q = w[0];
+                    q = e >= 4 ? w[1] : q;
+                    q = e >= 8 ? w[2] : q;
+                    q = e >= 12 ? w[3] : q;
+                    to[e] = (uint8_t)(q >> (8 * (e & 3)));
+                }
+            }
+        }
     }
 }
 
@@ -306,22 +277,19 @@ __device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block,
 }
 __global__ void __launch_bounds__(NT) q8_repack_kernel(Q8RepackArgs a) { q8_repack(a, blockIdx.x, gridDim.x); }
 
-// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.  A pair's two
-// gradients of a tile are two workgroups that read the same tensors at about the same time on the same XCD (ids 8 apart).
-template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp, unsigned na,
-                                                                                              unsigned nb) {
+// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.
+template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp,
+                                                                                                                         unsigned na, unsigned nb) {
     __shared__ __align__(16) TileMemory<typename Kept<DT, MODE>::type> m;
     const unsigned i = blockIdx.x;
     if (i < na) {
         const unsigned across = (a.N + TILE - 1) / TILE;
-        const unsigned tile = MODE == Q8_PAIR ? (i >> 4) * 8 + (i & 7) : i;
-        if (MODE == Q8_PAIR && tile >= across * (unsigned)((a.M + TILE - 1) / TILE)) return;
-        q8_tile<DT, MODE, ACT>(a, tile / across, tile % across, MODE == Q8_PAIR ? (i >> 3) & 1 : 0, m);
-    } else if (i >= na + nb) {
-        q8_repack(rp, i - na - nb, gridDim.x - na - nb);
-    } else {
+        q8_tile<DT, MODE, ACT>(a, i / across, i % across, m);
+    } else if (i < na + nb) {
         const unsigned across = (b.N + TILE - 1) / TILE;
-        q8_tile<DT, Q8_VALUES, ACT_NONE>(b, (i - na) / across, (i - na) % across, 0, m);
+        q8_tile<DT, Q8_VALUES, ACT_NONE>(b, (i - na) / across, (i - na) % across, m);
+    } else {
+        q8_repack(rp, i - na - nb, gridDim.x - na - nb);
     }
 }
 
@@ -362,7 +330,7 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
     for (int e = 0; e < 8; ++e) h[e] = e < left ? act_value<bf16_t>(v[0][e], x.act) * v[1][e] : 0.0f;
     const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(h)));
     if (left <= 0) return;
-    q8_store8(a.h.q + m * x.N + n, q8_codes8(h, q8_inverse(s)), left);
+    q8_store8(a.h.q + m * x.N + n, q8_codes8(h, q8_power(s)), left);
     if ((threadIdx.x & 15) == 0) a.h.s[(long)(n / Q8_GROUP) * x.M + m] = (uint8_t)s;
     if (a.hc) store8<bf16_t>(a.hc, m * x.N + n, left, h);
 }
@@ -375,7 +343,7 @@ unsigned copies_of(const Q8RepackArgs& a) {
     return (unsigned)(n < COPIES ? n : COPIES);
 }
 template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
-    const unsigned na = MODE == Q8_PAIR ? (tiles_of(a) + 7) / 8 * 16 : tiles_of(a), nb = tiles_of(b);
+    const unsigned na = tiles_of(a), nb = tiles_of(b);
     hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb + copies_of(rp)), dim3(NT), 0, s, a, b, rp, na, nb);
 }
 template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {

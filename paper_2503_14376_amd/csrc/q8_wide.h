@@ -232,11 +232,11 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const uint32_t s = q8_scale(max(most[r], area[wm][wn ^ 1][(c & 15) + 16 * r]));
-            const float inv = q8_inverse(s);
+            const float power = q8_power(s);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int i = 2 * k + r, l = left(i);
-                if (l > 0) q8_store8(q.h.q + at(i), q8_codes8(v[i], inv), l);
+                if (l > 0) q8_store8(q.h.q + at(i), q8_codes8(v[i], power), l);
             }
             if (wn == 0 && lane < 16 && (FULL || m + 16 * r < a.M)) q.h.s[(long)(col0 >> 7) * a.M + m + 16 * r] = (uint8_t)s;
         }

@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_q8_kernel(Q8NormArg
             if (a.y) store8<DT>(a.y, row * a.D + c, left, y);
             const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(y)));
             if (left > 0) {
-                q8_store8(a.q + row * a.D + c, q8_codes8(y, q8_inverse(s)), left);
+                q8_store8(a.q + row * a.D + c, q8_codes8(y, q8_power(s)), left);
                 if ((t & 15) == 0) a.s[(long)(c / Q8_GROUP) * a.M + row] = (uint8_t)s;
             }
         }
