@@ -9,7 +9,7 @@ namespace tfla {
 
 namespace {
 
-constexpr int TILE = 128, NT = 512, WAVES = NT / 64, RPI = NT / 16;
+constexpr int TILE = 128, NT = 1024, WAVES = NT / 64, RPI = NT / 16;
 
 // act(z) and act'(z) of a bf16 value, to 2^-20 (1 + |z|) of it: of a gradient that is rounded to 8 bits a value next to the border between
 // two codes is worth a sixteenth of itself, so that an error of 2^-13, as the bf16 products' gelu has, would show in dx, dw and the sums.  (The
@@ -84,12 +84,13 @@ template <int N> __device__ __forceinline__ uint32_t largest(const float (&v)[N]
     return most;
 }
 
-// Tile (bx, by).  By rows, thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r, r + 32, r + 64, r + 96: what a row needs is
+// Tile (bx, by).  By rows, thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r and r + 64: what a row needs is
 // done there, from registers, and the values are left in LDS for what a block or a column needs.  By columns, a thread takes 16 rows of a
 // column, eight neighbouring lanes all of it, so that neither scales nor sums need LDS.  A pair's second gradient waits in registers: a pair's
-// backward 8192 x 10944 takes 196 us (4.6 TB/s of its 898 MB; 265 with a tile of workgroups for each gradient, which computes the activation twice
-// and by rows from LDS), a weight of 10944 x 4096 with its transpose 39.5 (4.6 TB/s).  Small matrices pay for the unrolled rows, whose instructions
-// every workgroup fetches once (1000 x 1365 pair 16 -> 18).
+// backward 8192 x 10944 takes 193 us (4.6 TB/s of its 898 MB; 265 with a tile of workgroups for each gradient, which computes the activation twice
+// and by rows from LDS), a weight of 10944 x 4096 with its transpose 39.5 (4.6 TB/s).  512 threads with twice the rows each have as much in flight
+// in a full card, but where there are few tiles, their instructions, which each workgroup fetches once, are twice as many (1000 x 1365: pair
+// 18.0 us against 15.4, fp32 with its transpose 9.4 against 8.6).
 template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline__ void q8_tile(const Q8TileArgs& a, int bx, int by, MEM& m) {
     typedef typename Kept<DT, MODE>::type VT;
     typedef TileValues<VT> Values;
@@ -278,7 +279,7 @@ __device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block,
 __global__ void __launch_bounds__(NT) q8_repack_kernel(Q8RepackArgs a) { q8_repack(a, blockIdx.x, gridDim.x); }
 
 // The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.
-template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, MODE == Q8_VALUES ? 6 : 4) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp,
+template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 8) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp,
                                                                                                                          unsigned na, unsigned nb) {
     __shared__ __align__(16) TileMemory<typename Kept<DT, MODE>::type> m;
     const unsigned i = blockIdx.x;
