@@ -136,6 +136,19 @@ def test_two_streams_at_once(tfla):
             assert torch.equal(y, wy) and all(torch.equal(g[k], wg[k]) for k in wg)
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 4096, 300), (8, 257, 200), (64, 1024, 64), (300, 1000, 333), (513, 2048, 520), (4100, 2600, 2000),
+                                   (40, 4096, 256), (8192, 256, 4096), (4096, 256, 1152)])
+def test_a_projection_may_write_over_its_residual(tfla, M, K, N):
+    print("in place", M, K, N, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(M + K + N)
+    x, w, r = (torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16) for s in ((M, K), (N, K), (M, N)))
+    xq, wq = tfla.q8_quant(x), tfla.q8_quant(w, rows=128)
+    args = xq["q"], xq["scale"], wq["q"], wq["scale"]
+    want = tfla.linear_q8_fwd(*args, residual=r, act=tfla.ACT_SILU)["y"]
+    assert tfla.linear_q8_fwd(*args, residual=r, act=tfla.ACT_SILU, out={"y": r})["y"] is r
+    assert torch.equal(r.view(torch.int16), want.view(torch.int16))
+
+
 def test_the_same_call_gives_the_same_bits(tfla):
     print("bits", flush=True)
     b = FeedForward(tfla, 333, 1024, 1365, 7)
