@@ -17,6 +17,19 @@ __device__ __forceinline__ uint32_t q8_magnitude(float v) {
     const uint32_t u = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
     return u < 0x7f800000u ? u : 0u;
 }
+// The largest of N: by their bits alone, and with the test of each only in a wavefront that holds one that is not finite (of four
+// instructions a value two and a half are saved)
+template <int N> __device__ __forceinline__ uint32_t q8_largest(const float (&v)[N]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = max(most, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+    if (__any(most >= 0x7f800000u)) {
+        most = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) most = max(most, q8_magnitude(v[e]));
+    }
+    return most;
+}
 // scale byte of a group with that magnitude: 448 is 1.75 2^8 (subnormal magnitudes give 0 as they should)
 __device__ __forceinline__ uint32_t q8_scale(uint32_t most) {
     const int b = (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u);
@@ -33,12 +46,6 @@ __device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d,
 }
 __device__ __forceinline__ u32x2 q8_codes8(const float (&v)[8], float power) {
     return u32x2{q8_codes(v[0], v[1], v[2], v[3], power), q8_codes(v[4], v[5], v[6], v[7], power)};
-}
-__device__ __forceinline__ uint32_t q8_magnitude8(const float (&v)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, q8_magnitude(v[e]));
-    return m;
 }
 // the first n (0 .. 8) of eight codes to any address
 __device__ __forceinline__ void q8_store8(uint8_t* p, const u32x2& w, int n) {

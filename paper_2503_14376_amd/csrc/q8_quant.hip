@@ -71,19 +71,6 @@ __device__ __forceinline__ void into_place(Vec8<float>& x, int shift) {
     if (shift >= 8) x.zero();
 }
 
-// magnitudes of N values, of which what is not finite does not count, and the largest of them
-template <int N> __device__ __forceinline__ uint32_t largest(const float (&v)[N]) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) most = max(most, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
-    if (__any(most >= 0x7f800000u)) {       // (rare)
-        most = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) most = max(most, q8_magnitude(v[e]));
-    }
-    return most;
-}
-
 // Tile (bx, by).  By rows, thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r and r + 64: what a row needs is
 // done there, from registers, and the values are left in LDS for what a block or a column needs.  By columns, a thread takes 16 rows of a
 // column, eight neighbouring lanes all of it, so that neither scales nor sums need LDS.  A pair's second gradient waits in registers: a pair's
@@ -129,7 +116,7 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
         }
     };
     auto codes = [&](const Q8Out& o, int i, const float (&v)[8]) {
-        const uint32_t most = largest(v);
+        const uint32_t most = q8_largest(v);
         all = max(all, most);
         if (!o.q || blocks) return;
         const long row = r0 + i;
@@ -228,7 +215,7 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
             if (!o.qt) continue;
             uint32_t s = whole;
             if (!blocks) {
-                uint32_t most = largest(v);
+                uint32_t most = q8_largest(v);
                 most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, true));
                 most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4e, 0xf, 0xf, true));
                 s = q8_scale(max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x141, 0xf, 0xf, true)));
@@ -329,7 +316,7 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
     float h[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = e < left ? act_value<bf16_t>(v[0][e], x.act) * v[1][e] : 0.0f;
-    const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(h)));
+    const uint32_t s = q8_scale(lanes_max<16>(q8_largest(h)));
     if (left <= 0) return;
     q8_store8(a.h.q + m * x.N + n, q8_codes8(h, q8_power(s)), left);
     if ((threadIdx.x & 15) == 0) a.h.s[(long)(n / Q8_GROUP) * x.M + m] = (uint8_t)s;

@@ -214,7 +214,7 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
         uint32_t most[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            uint32_t x = max(q8_magnitude8(v[r]), q8_magnitude8(v[r + 2]));
+            uint32_t x = max(q8_largest(v[r]), q8_largest(v[r + 2]));
             // the other columns of the row are those of the lanes 16 and 32 further
             const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
             const uint32_t p0 = p[0], p1 = p[1];

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_q8_kernel(Q8NormArg
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = e < left ? (x[j][e] - mean) * rstd * g[j][e] + be[j][e] : 0.0f;
             if (a.y) store8<DT>(a.y, row * a.D + c, left, y);
-            const uint32_t s = q8_scale(lanes_max<16>(q8_magnitude8(y)));
+            const uint32_t s = q8_scale(lanes_max<16>(q8_largest(y)));
             if (left > 0) {
                 q8_store8(a.q + row * a.D + c, q8_codes8(y, q8_power(s)), left);
                 if ((t & 15) == 0) a.s[(long)(c / Q8_GROUP) * a.M + row] = (uint8_t)s;
