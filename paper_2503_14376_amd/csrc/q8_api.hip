@@ -114,7 +114,7 @@ int product_fwd(const void* xq, const void* x_scale, const void* const (&wq)[2],
     for (int p = 0; p < 2; ++p) { g.bias[p] = bias[p]; g.z[p] = z[p]; }
     g.residual = residual; g.act = act; g.split = l.plan.split;
     g.part = reinterpret_cast<float*>(ws + l.part);
-    if (pair) { q.h.q = u8(y); q.h.s = u8(y_scale); q.hc = h; q.past = q8_past_caches(M, N, (h != nullptr) + (z[0] != nullptr) + (z[1] != nullptr)); }
+    if (pair) { q.h.q = u8(y); q.h.s = u8(y_scale); q.hc = h; }
     else g.out[0] = y;
     if (l.rows) {
         TFLA_LAUNCH(K_GEMM, launch_q8_rows(q, s));

@@ -53,7 +53,6 @@ struct Q8GemmArgs {
     long lsa, lsb; int shb;            // (rows of A have a scale each)
     int k;
     Q8Out h; void* hc;                 // EPI_GATED: codes and scales of h; hc: h in bf16 or NULL
-    bool past;                         // q8_past_caches, of hc and the pre-activations
 };
 // (a pair: EPI_GATED where q8_gate_inside, otherwise EPI_PART, which leaves the parts to launch_q8_gated_join)
 hipError_t launch_q8_gemm(const Q8GemmArgs& a, const GemmPlan& p, int epi, hipStream_t s);

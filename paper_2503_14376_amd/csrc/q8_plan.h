@@ -6,10 +6,6 @@ namespace tfla {
 
 // Whether a pair's kernel forms h and its codes: a tile of 256 x 256 holds the 128 columns of a scale, all of their contraction.
 inline bool q8_gate_inside(int bn, int split) { return bn == 256 && split == 1; }
-// Whether what a pair keeps for the backward pass (`tensors` of M x N in bf16) goes past the caches: where the last one (256 MB) does not hold it for
-// its reader, it costs the operands their place.  a, u and h kept: 8192 x 4096 x 10944 (538 MB) 677 us, past the caches 652 - 672; 8192 x 2048 x 5504
-// (271 MB) 229, 226; 2048 x 4096 x 10944 (134 MB) 181, 184; 8192 x 1024 x 2752 (135 MB) 84, 88.
-inline bool q8_past_caches(long M, int N, int tensors) { return 2.0 * tensors * M * N > 200e6; }
 
 // How a product is cut: the tile and the number of parts with the shortest time by a model as gemm_plan's, with steps of 128 codes.  Fitted to
 // 2500 times of 260 random products (33 to 8192 rows, 64 to 8192 columns, contractions of 128 to 8192; pairs, two segments, two at a

@@ -155,15 +155,6 @@ __device__ __forceinline__ void q8_epilogue(const GemmArgs& a, const GemmWork& w
     }
 }
 
-// eight values past the caches, or up to seven
-__device__ __forceinline__ void leave8(void* base, long idx, int n, const float (&x)[8]) {
-    typedef u32x4 __attribute__((aligned(2))) any4;
-    Vec8<bf16_t> r;
-    r.set(x);
-    if (n >= 8) __builtin_nontemporal_store(r.w, reinterpret_cast<any4*>(reinterpret_cast<uint16_t*>(base) + idx));
-    else if (n > 0) r.store_tail(base, idx, n);
-}
-
 // A pair's results, 32 rows at a time, in transposed blocks as gemm.h turns them (two columns a lane, as above, are four times the stores: 651 -> 725 us): bias, a and u where wanted, h = act(a) u, its scale and codes.  The 128 columns that share a scale
 // are this tile's: two wavefronts hold 64 each and meet in `meet` (two areas in turn, so that one meeting per 32 rows is enough).
 template <bool FULL>
@@ -189,15 +180,6 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
         const int n = col0 + wn * 64 + (c >> 4) * 16 + 8 * g;
         auto left = [&](int i) { return FULL ? 8 : (m + (i & 1) * 16 < a.M ? min(8, a.N - n - (i >> 1) * 32) : 0); };
         auto at = [&](int i) { return (m + (i & 1) * 16) * a.N + n + (i >> 1) * 32; };
-        auto put = [&](void* to, const float (&x)[4][8]) {
-            if (q.past) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) leave8(to, at(i), left(i), x[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) store8<bf16_t>(to, at(i), left(i), x[i]);
-            }
-        };
         auto ready = [&](float (&x)[4][8], const float* bias, void* keep) {
             if (bias) {
 #pragma unroll
@@ -208,7 +190,10 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
                     for (int e = 0; e < 8; ++e) { x[2 * k][e] += t[e]; x[2 * k + 1][e] += t[e]; }
                 }
             }
-            if (keep) put(keep, x);
+            if (keep) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store8<bf16_t>(keep, at(i), left(i), x[i]);
+            }
         };
         ready(v, a.bias[0], a.z[0]);
         ready(u, a.bias[1], a.z[1]);
@@ -222,7 +207,10 @@ __device__ __forceinline__ void q8_gated_epilogue(const Q8GemmArgs& q, long row0
                     v[i][e] = FULL || e < left(i) ? h : 0.0f;
                 }
         });
-        if (q.hc) put(q.hc, v);
+        if (q.hc) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store8<bf16_t>(q.hc, at(i), left(i), v[i]);
+        }
         uint32_t most[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
