@@ -74,7 +74,7 @@ __device__ __forceinline__ void into_place(Vec8<float>& x, int shift) {
 // Tile (bx, by).  By rows, thread (g = t % 16, r = t / 16) takes the columns 8 g ... of the rows r and r + 64: what a row needs is
 // done there, from registers, and the values are left in LDS for what a block or a column needs.  By columns, a thread takes 16 rows of a
 // column, eight neighbouring lanes all of it, so that neither scales nor sums need LDS.  A pair's second gradient waits in registers: a pair's
-// backward 8192 x 10944 takes 193 us (4.6 TB/s of its 898 MB; 265 with a tile of workgroups for each gradient, which computes the activation twice
+// backward 8192 x 10944 takes 193 us (4.6 TB/s of its 898 MB; 265 with a workgroup for each gradient, which computes the activation twice
 // and by rows from LDS), a weight of 10944 x 4096 with its transpose 39.5 (4.6 TB/s).  512 threads with twice the rows each have as much in flight
 // in a full card, but where there are few tiles, their instructions, which each workgroup fetches once, are twice as many (1000 x 1365: pair
 // 18.0 us against 15.4, fp32 with its transpose 9.4 against 8.6).
