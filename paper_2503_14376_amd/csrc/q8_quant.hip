@@ -242,19 +242,28 @@ template <typename DT, int MODE, int ACT, typename MEM> __device__ __forceinline
     }
 }
 
-// Rows of bytes at any address to rows of ldd bytes: block x of `across` of them, 16 bytes a lane
-constexpr int COPIES = 256;         // workgroups of a launch's copies, at most
-__device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block, unsigned blocks) {
-    const int per = (int)(a.ldd >> 4);
+// Rows of bytes at any address to rows of ldd bytes: block x of `blocks` of THREADS, 16 bytes a lane.  A row's end is read from inside the row, as
+// a tile's (byte by byte, in a branch, a product of 33 x 1365 x 1000 with
+// its copies took 15.6 us, so 10.5).
+template <int THREADS> __device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block, unsigned blocks) {
+    const unsigned per = (unsigned)(a.ldd >> 4);
     for (int q = 0; q < a.count; ++q) {
         const long all = a.rows[q] * per;
-        for (long i = (long)block * NT + threadIdx.x; i < all; i += (long)blocks * NT) {
-            const long r = i / per;
-            const int c = (int)(i % per) * 16;
+        const bool narrow = all < 1l << 32;
+        for (long i = (long)block * THREADS + threadIdx.x; i < all; i += (long)blocks * THREADS) {
+            const long r = narrow ? (long)((unsigned)i / per) : i / per;
+            const int c = (int)(i - r * per) * 16, behind = max(c + 16 - a.cols, 0);      // how far a read goes past the row
             const uint8_t* p = a.src[q] + r * a.cols + c;
             u32x4 w = {0u, 0u, 0u, 0u};
-            if (c + 16 <= a.cols) __builtin_memcpy(&w, p, 16);
-            else {
+            if (a.cols >= 16) {
+                uint64_t d[2];
+                __builtin_memcpy(d, p - behind, 16);
+                uint64_t lo = behind & 8 ? d[1] : d[0], hi = behind & 8 ? 0 : d[1];
+                const int bits = (behind & 7) * 8;
+                lo = lo >> bits | (hi << 1) << (63 - bits);
+                hi >>= bits;
+                w = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+            } else {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (c + e < a.cols) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
@@ -263,7 +272,8 @@ __device__ __forceinline__ void q8_repack(const Q8RepackArgs& a, unsigned block,
         }
     }
 }
-__global__ void __launch_bounds__(NT) q8_repack_kernel(Q8RepackArgs a) { q8_repack(a, blockIdx.x, gridDim.x); }
+constexpr int COPY = 256;
+__global__ void __launch_bounds__(COPY) q8_repack_kernel(Q8RepackArgs a) { q8_repack<COPY>(a, blockIdx.x, gridDim.x); }
 
 // The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.
 template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 8) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp,
@@ -277,7 +287,7 @@ template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 
         const unsigned across = (b.N + TILE - 1) / TILE;
         q8_tile<DT, Q8_VALUES, ACT_NONE>(b, (i - na) / across, (i - na) % across, m);
     } else {
-        q8_repack(rp, i - na - nb, gridDim.x - na - nb);
+        q8_repack<NT>(rp, i - na - nb, gridDim.x - na - nb);
     }
 }
 
@@ -325,15 +335,16 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
 }
 
 unsigned tiles_of(const Q8TileArgs& a) { return (unsigned)((a.M + TILE - 1) / TILE * ((a.N + TILE - 1) / TILE)); }
-unsigned copies_of(const Q8RepackArgs& a) {
+// workgroups of a launch's copies: a piece a thread, up to as many as the chip holds (beside a quantisation half of them)
+unsigned copies_of(const Q8RepackArgs& a, int threads, unsigned most) {
     long all = 0;
-    for (int q = 0; q < a.count; ++q) all += a.rows[q] * (a.ldd >> 4);
-    const long n = (all + 4 * NT - 1) / (4 * NT);
-    return (unsigned)(n < COPIES ? n : COPIES);
+    for (int q = 0; q < a.count; ++q) all = max(all, a.rows[q] * (a.ldd >> 4));
+    const long n = (all + threads - 1) / threads;
+    return n < most ? (unsigned)n : most;
 }
 template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
     const unsigned na = tiles_of(a), nb = tiles_of(b);
-    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb + copies_of(rp)), dim3(NT), 0, s, a, b, rp, na, nb);
+    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb + copies_of(rp, NT, 256)), dim3(NT), 0, s, a, b, rp, na, nb);
 }
 template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
     if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, rp, s);
@@ -354,7 +365,7 @@ hipError_t launch_q8_tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8Rep
 
 hipError_t launch_q8_repack(const Q8RepackArgs& a, hipStream_t s) {
     if (a.count == 0) return hipSuccess;
-    hipLaunchKernelGGL(q8_repack_kernel, dim3(copies_of(a)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(q8_repack_kernel, dim3(copies_of(a, COPY, 2048)), dim3(COPY), 0, s, a);
     return hipGetLastError();
 }
 
