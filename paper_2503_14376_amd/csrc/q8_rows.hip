@@ -12,13 +12,13 @@ namespace tfla {
 namespace {
 
 // 32 codes of a row: 16 at k, 16 at k + 64 (so that an access reads 64 consecutive bytes of each row); left: codes from k on that exist
-struct Codes32 {
+template <bool ODD> struct Codes32 {
     i32x8 w;
     __device__ __forceinline__ void load(const uint8_t* p) {
         __builtin_memcpy(&w, p, 16);
         __builtin_memcpy(reinterpret_cast<char*>(&w) + 16, p + 64, 16);
     }
-    __device__ __forceinline__ void load_tail(const uint8_t* p, int left) {
+    __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t*) {
         uint32_t t[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -34,11 +34,45 @@ struct Codes32 {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = (int)t[e];
     }
+    __device__ __forceinline__ i32x8 codes(int) const { return w; }
+};
+// ... of a row at any address (ODD).  What is read are whole words of four bytes, one more than there are codes for, and moved by the row's place in its
+// first word when the codes are wanted (16 bytes at an odd address are many accesses: 16 x 4095 through 4096 rows 18.7 us, so 10.6).  Such a
+// word may hold up to three bytes before or behind the row, which count for nothing; one without a byte of the row is not read.
+template <> struct Codes32<true> {
+    uint32_t d[2][5];
+    __device__ __forceinline__ void load(const uint8_t* p) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            __builtin_memcpy(d[h], __builtin_assume_aligned(reinterpret_cast<const void*>((at & ~(uintptr_t)3) + h * 64), 4), 16);
+            d[h][4] = *reinterpret_cast<const uint32_t*>(((at + 15) & ~(uintptr_t)3) + h * 64);
+        }
+    }
+    // (words behind the end are read at `row`, so that no branch holds the others up, and cleared)
+    __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t* row) {
+        const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 3);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 5; ++j) {
+                const int n = left > h * 64 ? min(left - h * 64, 16) + shift - 4 * j : 0;       // bytes of the word that are the row's or before it
+                const uintptr_t from = reinterpret_cast<uintptr_t>(n > 0 ? p - shift + h * 64 + 4 * j : row) & ~(uintptr_t)3;
+                const uint32_t v = *reinterpret_cast<const uint32_t*>(from);
+                d[h][j] = n <= 0 ? 0u : (n >= 4 ? v : v & ((1u << 8 * n) - 1));
+            }
+    }
+    __device__ __forceinline__ i32x8 codes(int shift) const {
+        i32x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (int)__builtin_amdgcn_alignbyte(d[e / 4][e % 4 + 1], d[e / 4][e % 4], (uint32_t)shift);
+        return w;
+    }
 };
 
 // MB blocks of 16 rows of x, NW wavefronts, U pieces of 128 codes in flight per wavefront, SL slices, HOLD: as gemm_rows_kernel.
 // A pair's products go to the partial planes, for its gate and the codes of 128 columns at a time are formed in a second launch.
-template <int MB, int SL, bool PAIR, int NW, int U, bool HOLD>
+template <int MB, int SL, bool PAIR, int NW, int U, bool HOLD, bool ODD>
 __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int blocks) {
     constexpr int P = PAIR ? 2 : 1, RB = 16 / SL, LD = RB + 4;
     static_assert(SL == 1 || MB == 1, "slices take one block of rows");
@@ -55,19 +89,29 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
         xm[i] = min(i * 16 + r % RB, a.M - 1);
         xrow[i] = (long)xm[i] * q.k;
     }
-    Codes32 w[U][P], x[U][MB];
+    Codes32<ODD> w[U][P], x[U][MB];
     int ws[U][P], xs[U][MB];
+    // a row's place in its first word
+    int wshift[P] = {}, xshift[MB] = {};
+    if constexpr (ODD) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) xshift[i] = (int)(reinterpret_cast<uintptr_t>(xp + xrow[i]) & 3);
+    }
     // piece c0 + u NW of this lane's slice
     auto fetch = [&](int c0, int n0, bool with_w, bool with_x) {
         // rows behind the last one read it again: their results are not stored
-        const long wrow = (long)min(n0 + r % RB, a.N - 1) * q.k + g * 16;
+        const long wrow = (long)min(n0 + r % RB, a.N - 1) * q.k;
+        if constexpr (ODD) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) wshift[p] = (int)((reinterpret_cast<uintptr_t>(a.B[p]) + wrow) & 3);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = c0 + u * NW, kb = slice * ps + c;
             if ((SL - 1) * ps + c < full && c < ps) {
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    if (with_w) w[u][p].load(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + (long)kb * 128);
+                    if (with_w) w[u][p].load(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + g * 16 + (long)kb * 128);
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
                     if (with_x) x[u][i].load(xp + xrow[i] + (long)kb * 128);
@@ -75,10 +119,10 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
                 const int left = c < ps ? q.k - kb * 128 - g * 16 : 0;
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    if (with_w) w[u][p].load_tail(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + (long)kb * 128, left);
+                    if (with_w) w[u][p].load_tail(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + g * 16 + (long)kb * 128, left, reinterpret_cast<const uint8_t*>(a.B[p]) + wrow);
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
-                    if (with_x) x[u][i].load_tail(xp + xrow[i] + (long)kb * 128, left);
+                    if (with_x) x[u][i].load_tail(xp + xrow[i] + (long)kb * 128, left, xp - g * 16 + xrow[i]);
             }
             const int ks = min(kb, pieces - 1);
 #pragma unroll
@@ -109,7 +153,8 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
                 for (int p = 0; p < P; ++p)
 #pragma unroll
                     for (int i = 0; i < MB; ++i)
-                        acc[p][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[u][p].w, x[u][i].w, acc[p][i], 0, 0, 0, ws[u][p], 0, xs[u][i]);
+                        acc[p][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[u][p].codes(wshift[p]), x[u][i].codes(xshift[i]), acc[p][i], 0, 0, 0,
+                                                                                                  ws[u][p], 0, xs[u][i]);
             if (HOLD) break;
         }
         if (HOLD && block + (int)gridDim.x < blocks) fetch(wave, n0 + gridDim.x * RB, true, false);
@@ -151,27 +196,36 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
     }
 }
 
-template <int MB, int SL, bool PAIR, int NW> void launch(const Q8GemmArgs& a, const Q8RowsPlan& p, hipStream_t s) {
+// (rows at odd addresses are not held over blocks: their words are more, and so are the registers)
+template <int MB, int SL, bool PAIR, int NW> void launch(const Q8GemmArgs& a, const Q8RowsPlan& p, bool odd, hipStream_t s) {
+    const dim3 threads(NW * 64);
+    if (odd) {
+        if (p.ahead == 2) hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, false, true>), dim3(p.blocks), threads, 0, s, a, p.blocks);
+        else hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 1, false, true>), dim3(p.blocks), threads, 0, s, a, p.blocks);
+        return;
+    }
     if constexpr (NW <= 8) {
         if (p.hold) {
-            hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, true>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+            hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, true, false>), dim3(p.grid), threads, 0, s, a, p.blocks);
             return;
         }
     }
-    if (p.ahead == 2) hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
-    else hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 1, false>), dim3(p.grid), dim3(NW * 64), 0, s, a, p.blocks);
+    if (p.ahead == 2) hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, false, false>), dim3(p.grid), threads, 0, s, a, p.blocks);
+    else hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 1, false, false>), dim3(p.grid), threads, 0, s, a, p.blocks);
 }
-template <int MB, int SL, bool PAIR> void go(const Q8GemmArgs& a, const Q8RowsPlan& p, hipStream_t s) {
-    if (p.waves == 4) launch<MB, SL, PAIR, 4>(a, p, s);
-    else if (p.waves == 8) launch<MB, SL, PAIR, 8>(a, p, s);
-    else launch<MB, SL, PAIR, 16>(a, p, s);
+template <int MB, int SL, bool PAIR> void go(const Q8GemmArgs& a, const Q8RowsPlan& p, bool odd, hipStream_t s) {
+    if (p.waves == 4) launch<MB, SL, PAIR, 4>(a, p, odd, s);
+    else if (p.waves == 8) launch<MB, SL, PAIR, 8>(a, p, odd, s);
+    else launch<MB, SL, PAIR, 16>(a, p, odd, s);
 }
 template <bool PAIR> void by_rows(const Q8GemmArgs& a, hipStream_t s) {
     const Q8RowsPlan p = q8_rows_plan(a.g.M, a.g.N, a.k);
-    if (p.slices == 4) go<1, 4, PAIR>(a, p, s);
-    else if (p.slices == 2) go<1, 2, PAIR>(a, p, s);
-    else if (p.row_blocks == 1) go<1, 1, PAIR>(a, p, s);
-    else go<2, 1, PAIR>(a, p, s);
+    const uintptr_t all = reinterpret_cast<uintptr_t>(a.g.A[0]) | reinterpret_cast<uintptr_t>(a.g.B[0]) | (PAIR ? reinterpret_cast<uintptr_t>(a.g.B[1]) : 0);
+    const bool odd = ((all | (uintptr_t)a.k) & 3) != 0;
+    if (p.slices == 4) go<1, 4, PAIR>(a, p, odd, s);
+    else if (p.slices == 2) go<1, 2, PAIR>(a, p, odd, s);
+    else if (p.row_blocks == 1) go<1, 1, PAIR>(a, p, odd, s);
+    else go<2, 1, PAIR>(a, p, odd, s);
 }
 
 }  // namespace

@@ -129,6 +129,16 @@ def test_operands_off_16_bytes(tfla, off, M, K, N, pair):
         backward(tfla, generator(N), pair, M, N, K, 1, off[1])
 
 
+@pytest.mark.parametrize("M", [1, 4, 5, 8, 9, 16, 17, 32])
+@pytest.mark.parametrize("K,N,off", [(1, 20, (0, 0)), (2, 7, (1, 3)), (3, 40, (2, 1)), (5, 33, (0, 2)), (15, 16, (3, 0)), (127, 130, (0, 0)), (129, 64, (0, 1)),
+                                     (333, 70, (2, 0)), (1365, 129, (0, 0)), (2049, 140, (5, 2)), (4099, 24, (0, 0)), (4096, 24, (1, 2))])
+@pytest.mark.parametrize("pair", [False, True])
+def test_few_rows_at_odd_addresses(tfla, M, K, N, off, pair):
+    """the first and last words of a row hold bytes of its neighbours or of nothing"""
+    print("odd", M, K, N, off, pair, flush=True)
+    forward(tfla, generator(M * K), pair, M, K, N, 1, off)
+
+
 @pytest.mark.parametrize("rows", [1, 128])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("M,K", [(1, 5), (7, 7), (128, 128), (130, 1365), (300, 264), (129, 8)])
