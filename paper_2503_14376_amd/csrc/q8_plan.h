@@ -58,7 +58,7 @@ constexpr int Q8_ROWS_MAX = 32;
 // 37.2; through 4096 x 10944, 22 pieces: eight wavefronts with one 11.0, with two 13.3).  hold: a wavefront's share of x is one turn, and
 // there are more blocks than the chip runs at a time.
 struct Q8RowsPlan { int row_blocks, slices, waves, ahead, blocks, grid; bool hold; };
-inline Q8RowsPlan q8_rows_plan(long M, int N, int K) {
+inline Q8RowsPlan q8_rows_plan(long M, int N, int K, int pair) {
     Q8RowsPlan p{};
     p.row_blocks = M <= 16 ? 1 : 2;
     p.slices = M <= 4 ? 4 : (M <= 8 ? 2 : 1);
@@ -69,6 +69,10 @@ inline Q8RowsPlan q8_rows_plan(long M, int N, int K) {
     p.ahead = 2 * two <= one ? 2 : 1;
     const int most = 256 * (p.waves == 4 ? 4 : 2);
     p.hold = p.waves <= 8 && p.ahead == 2 && two == 1 && p.blocks > most;
+    // three turns as one, x held: 4 tokens through 10944 x 5504 17.9 us, so 14.4; not where x is a row or two (13.3, 14.7), for pairs (28.3, 30.8), where
+    // the slices lack more than two pieces (10944 x 4104: 15.3, 18.4) or blocks are few (4096 x 10944: 10.9, 12.0)
+    const int all = (K + 127) / 128;
+    if (p.slices == 4 && M > 2 && !pair && p.waves <= 8 && one == 3 && p.blocks > 2 * most && 4 * pieces - all <= 2) { p.ahead = 3; p.hold = true; }
     p.grid = p.hold ? most : p.blocks;
     return p;
 }
@@ -78,7 +82,7 @@ inline Q8RowsPlan q8_rows_plan(long M, int N, int K) {
 inline bool q8_rows_applies(long M, int N, int K, int pair, bool copies) {
     if (M <= 4 || M > Q8_ROWS_MAX) return M <= 4;
     if (copies) return true;
-    const Q8RowsPlan p = q8_rows_plan(M, N, K);
+    const Q8RowsPlan p = q8_rows_plan(M, N, K, pair);
     const double bytes = (double)(16 / p.slices * (pair ? 2 : 1) + M) * K;
     const double here = 1.8 + (p.blocks + 255) / 256 * bytes / (p.blocks <= 256 ? 39e3 : 30e3) + (pair ? 3.1 : 0);
     return here <= q8_plan(M, N, K, 1, 1, pair).us;

@@ -18,7 +18,24 @@ template <bool ODD> struct Codes32 {
         __builtin_memcpy(&w, p, 16);
         __builtin_memcpy(reinterpret_cast<char*>(&w) + 16, p + 64, 16);
     }
-    __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t*) {
+    // (k: the row's length, a multiple of four.  Without branches, which would have one load wait for another, a row's end is read from inside
+    // the row and moved, what does not exist at its beginning: 8 tokens through 10944 x 4104 15.2 us, so 12.7.  Of four slices only one ends with
+    // the row, and its lanes' reads cost more than the branch: pair, 4 x 10944 x 10944 50 us, without branches 55)
+    template <bool BRANCHES> __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t* row, int k) {
+        if (!BRANCHES && k >= 16) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = left - h * 64, behind = n >= 16 || n <= 0 ? 0 : 16 - n;
+                u32x4 v;
+                __builtin_memcpy(&v, n > 0 ? p + h * 64 - behind : row, 16);
+                const bool eight = (behind & 8) != 0, four = (behind & 4) != 0;
+                v = u32x4{eight ? v[2] : v[0], eight ? v[3] : v[1], eight ? 0 : v[2], eight ? 0 : v[3]};
+                v = u32x4{four ? v[1] : v[0], four ? v[2] : v[1], four ? v[3] : v[2], four ? 0 : v[3]};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[h * 4 + e] = n > 0 ? (int)v[e] : 0;
+            }
+            return;
+        }
         uint32_t t[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -50,7 +67,7 @@ template <> struct Codes32<true> {
         }
     }
     // (words behind the end are read at `row`, so that no branch holds the others up, and cleared)
-    __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t* row) {
+    template <bool BRANCHES> __device__ __forceinline__ void load_tail(const uint8_t* p, int left, const uint8_t* row, int) {
         const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 3);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -119,10 +136,12 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
                 const int left = c < ps ? q.k - kb * 128 - g * 16 : 0;
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    if (with_w) w[u][p].load_tail(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + g * 16 + (long)kb * 128, left, reinterpret_cast<const uint8_t*>(a.B[p]) + wrow);
+                    if (with_w)
+                        w[u][p].template load_tail<HOLD || SL == 4>(reinterpret_cast<const uint8_t*>(a.B[p]) + wrow + g * 16 + (long)kb * 128, left,
+                                                         reinterpret_cast<const uint8_t*>(a.B[p]) + wrow, q.k);
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
-                    if (with_x) x[u][i].load_tail(xp + xrow[i] + (long)kb * 128, left, xp - g * 16 + xrow[i]);
+                    if (with_x) x[u][i].template load_tail<HOLD || SL == 4>(xp + xrow[i] + (long)kb * 128, left, xp - g * 16 + xrow[i], q.k);
             }
             const int ks = min(kb, pieces - 1);
 #pragma unroll
@@ -199,6 +218,14 @@ __global__ void __launch_bounds__(NW * 64) q8_rows_kernel(Q8GemmArgs q, int bloc
 // (rows at odd addresses are not held over blocks: their words are more, and so are the registers)
 template <int MB, int SL, bool PAIR, int NW> void launch(const Q8GemmArgs& a, const Q8RowsPlan& p, bool odd, hipStream_t s) {
     const dim3 threads(NW * 64);
+    if constexpr (NW <= 8) {
+        if constexpr (SL == 4 && !PAIR) {
+            if (p.ahead == 3 && !odd) {
+                hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 3, true, false>), dim3(p.grid), threads, 0, s, a, p.blocks);
+                return;
+            }
+        }
+    }
     if (odd) {
         if (p.ahead == 2) hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 2, false, true>), dim3(p.blocks), threads, 0, s, a, p.blocks);
         else hipLaunchKernelGGL((q8_rows_kernel<MB, SL, PAIR, NW, 1, false, true>), dim3(p.blocks), threads, 0, s, a, p.blocks);
@@ -219,7 +246,7 @@ template <int MB, int SL, bool PAIR> void go(const Q8GemmArgs& a, const Q8RowsPl
     else launch<MB, SL, PAIR, 16>(a, p, odd, s);
 }
 template <bool PAIR> void by_rows(const Q8GemmArgs& a, hipStream_t s) {
-    const Q8RowsPlan p = q8_rows_plan(a.g.M, a.g.N, a.k);
+    const Q8RowsPlan p = q8_rows_plan(a.g.M, a.g.N, a.k, PAIR);
     const uintptr_t all = reinterpret_cast<uintptr_t>(a.g.A[0]) | reinterpret_cast<uintptr_t>(a.g.B[0]) | (PAIR ? reinterpret_cast<uintptr_t>(a.g.B[1]) : 0);
     const bool odd = ((all | (uintptr_t)a.k) & 3) != 0;
     if (p.slices == 4) go<1, 4, PAIR>(a, p, odd, s);

@@ -15,8 +15,10 @@ extern "C" void product_kernels(int backward, int pair, long M, int K, int N, ch
     *to = 0;
     if (!backward) {
         if (q8_rows_applies(M, N, K, pair, K % 16 != 0)) {
-            const Q8RowsPlan p = q8_rows_plan(M, N, K);
-            sprintf(to, "rows%s blocks %d slices %d waves %d ahead %d%s\n", pair ? " pair" : "", p.row_blocks, p.slices, p.waves, p.ahead, p.hold ? " hold" : "");
+            const Q8RowsPlan p = q8_rows_plan(M, N, K, pair);
+            const bool odd = K % 4 != 0;
+            sprintf(to, "rows%s blocks %d slices %d waves %d ahead %d%s\n", pair ? " pair" : "", p.row_blocks, p.slices, p.waves,
+                    odd && p.ahead == 3 ? 1 : p.ahead, odd ? " odd" : (p.hold ? " hold" : ""));
             return;
         }
         const GemmPlan p = q8_plan(M, N, K, 1, 1, pair);
