@@ -7,6 +7,17 @@ namespace tfla {
 // Whether a pair's kernel forms h and its codes: a tile of 256 x 256 holds the 128 columns of a scale, all of their contraction.
 inline bool q8_gate_inside(int bn, int split) { return bn == 256 && split == 1; }
 
+// ---- the quantiser's tiles ------------------------------------------------------------------------
+// A workgroup of 1024 threads per tile of 128 x 128.  The runtime starts fewer than 2^32 threads along an axis, and matrices of 2^36 values have
+// 2^22 tiles: what is more than Q8_LAUNCH workgroups follows in further launches (a multiple of eight, so that workgroup i of all of them goes on
+// running on XCD i % 8).
+constexpr int Q8_TILE = 128, Q8_TILE_THREADS = 1024;
+constexpr unsigned Q8_LAUNCH = 1u << 21;
+inline unsigned q8_tiles(long M, long N) { return (unsigned)((M + Q8_TILE - 1) / Q8_TILE * ((N + Q8_TILE - 1) / Q8_TILE)); }
+// workgroups of the launch that begins with workgroup `first` of `all`
+inline unsigned q8_launch(unsigned first, unsigned all) { return all - first < Q8_LAUNCH ? all - first : Q8_LAUNCH; }
+
+// ---- tiles of products ------------------------------------------------------------------------------
 // How a product is cut: the tile and the number of parts with the shortest time by a model as gemm_plan's, with steps of 128 codes.  Fitted to
 // 2500 times of 260 random products (33 to 8192 rows, 64 to 8192 columns, contractions of 128 to 8192; pairs, two segments, two at a
 // time): 8 % off in the mean, and what it picks is 1.3 % above the best of all choices on average, 23 % at most.  In us:

@@ -9,7 +9,7 @@ namespace tfla {
 
 namespace {
 
-constexpr int TILE = 128, NT = 1024, WAVES = NT / 64, RPI = NT / 16;
+constexpr int TILE = Q8_TILE, NT = Q8_TILE_THREADS, WAVES = NT / 64, RPI = NT / 16;
 
 // act(z) and act'(z) of a bf16 value, to 2^-20 (1 + |z|) of it: of a gradient that is rounded to 8 bits a value next to the border between
 // two codes is worth a sixteenth of itself, so that an error of 2^-13, as the bf16 products' gelu has, would show in dx, dw and the sums.  (The
@@ -280,11 +280,12 @@ __global__ void __launch_bounds__(COPY) q8_repack_kernel(Q8RepackArgs a) { q8_re
 // 40.5, ranges 44.6).
 __device__ __forceinline__ unsigned tile_of(const Q8TileArgs& a, unsigned i, unsigned n) { return a.N % 64 ? xcd_range(i, n) : i; }
 
-// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies.
+// The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies: of all of
+// these workgroups the ones from `first` on.
 template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 8) q8_tiles_kernel(Q8TileArgs a, Q8TileArgs b, Q8RepackArgs rp,
-                                                                                                                         unsigned na, unsigned nb) {
+                                                                                                   unsigned na, unsigned nb, unsigned copies, unsigned first) {
     __shared__ __align__(16) TileMemory<typename Kept<DT, MODE>::type> m;
-    const unsigned i = blockIdx.x;
+    const unsigned i = first + blockIdx.x;
     if (i < na) {
         const unsigned across = (a.N + TILE - 1) / TILE, t = tile_of(a, i, na);
         q8_tile<DT, MODE, ACT>(a, t / across, t % across, m);
@@ -292,7 +293,7 @@ template <typename DT, int MODE, int ACT> __global__ void __launch_bounds__(NT, 
         const unsigned across = (b.N + TILE - 1) / TILE, t = tile_of(b, i - na, nb);
         q8_tile<DT, Q8_VALUES, ACT_NONE>(b, t / across, t % across, m);
     } else {
-        q8_repack<NT>(rp, i - na - nb, gridDim.x - na - nb);
+        q8_repack<NT>(rp, i - na - nb, copies);
     }
 }
 
@@ -339,7 +340,6 @@ __global__ void __launch_bounds__(256) q8_gated_join_kernel(Q8GemmArgs a) {
     if (a.hc) store8<bf16_t>(a.hc, m * x.N + n, left, h);
 }
 
-unsigned tiles_of(const Q8TileArgs& a) { return (unsigned)((a.M + TILE - 1) / TILE * ((a.N + TILE - 1) / TILE)); }
 // workgroups of a launch's copies: a piece a thread, up to as many as the chip holds (beside a quantisation half of them)
 unsigned copies_of(const Q8RepackArgs& a, int threads, unsigned most) {
     long all = 0;
@@ -348,8 +348,9 @@ unsigned copies_of(const Q8RepackArgs& a, int threads, unsigned most) {
     return n < most ? (unsigned)n : most;
 }
 template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
-    const unsigned na = tiles_of(a), nb = tiles_of(b);
-    hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(na + nb + copies_of(rp, NT, 256)), dim3(NT), 0, s, a, b, rp, na, nb);
+    const unsigned na = q8_tiles(a.M, a.N), nb = q8_tiles(b.M, b.N), copies = copies_of(rp, NT, 256), all = na + nb + copies;
+    for (unsigned first = 0; first < all; first += q8_launch(first, all))
+        hipLaunchKernelGGL((q8_tiles_kernel<DT, MODE, ACT>), dim3(q8_launch(first, all)), dim3(NT), 0, s, a, b, rp, na, nb, copies, first);
 }
 template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
     if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, rp, s);

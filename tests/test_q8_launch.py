@@ -1,0 +1,36 @@
+"""The runtime starts fewer than 2^32 threads along an axis.  At the largest sizes that the calls in 8 bits accept, no launch asks for more: the
+rules (csrc/q8_plan.h, the header that the library is built with) compiled for the host."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from tests.test_block_plan import CSRC, HERE
+
+LIMIT = 1 << 32
+
+
+@pytest.fixture(scope="module")
+def probe(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("launch") / "q8_launch.so")
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, os.path.join(HERE, "q8_launch_probe.cpp"), "-o", so])
+    return ctypes.CDLL(so)
+
+
+@pytest.mark.parametrize("more", [0, 1, 256, (1 << 14) + 256, 1 << 22])
+@pytest.mark.parametrize("M,N", [(1, 1), (128, 129), (1 << 24, 3968), (1 << 24, 3969), (1 << 24, 4096), (1 << 18, 1 << 18), (1 << 16, 1 << 20), (1 << 21, 1 << 15),
+                                 ((1 << 24) - 1, 4095), ((1 << 21) - 5, (1 << 15) - 200)])
+def test_tiles(probe, M, N, more):
+    """all workgroups, in order, in launches that the runtime accepts; each begins at a multiple of eight, as XCDs are counted"""
+    ask = probe.tile_launches
+    ask.argtypes = [ctypes.c_long, ctypes.c_long, ctypes.c_uint, ctypes.POINTER(ctypes.c_long), ctypes.POINTER(ctypes.c_long)]
+    first, threads = (ctypes.c_long * 64)(), (ctypes.c_long * 64)()
+    n = ask(M, N, more, first, threads)
+    at = 0
+    for i in range(n):
+        assert first[i] == at and at % 8 == 0 and 0 < threads[i] < LIMIT
+        at += threads[i] // 1024
+    assert at == -(-M // 128) * -(-N // 128) + more
+    if at < 1 << 21:
+        assert n == 1
