@@ -52,10 +52,12 @@ inline GemmPlan q8_plan(long M, int N, int K, int segs, int batch, int pair) {
 
 // ---- both products of a small backward pass in one launch ------------------------------------------
 // dx and dw in tiles of 64 x 64, undivided, and the bias gradients' sums with them: a launch saved (3.4 us of the host's time, 2 of the GPU's; two
-// with sums), and the items of one product fill what the other leaves of the CUs' time, where by an estimate that is no slower.
+// with sums), and the items of one product fill what the other leaves of the CUs' time, where by an estimate that is no slower.  (Weights of close to
+// 2^36 elements with a few tokens are 2^24 tiles of 256 threads, 2^32: the runtime does not start that many, two products of larger tiles do.)
 inline bool q8_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K, int N, int pair) {
     auto up = [](long v, int by) { return (v + by - 1) / by; };
     const long segs = pair ? 2 : 1, nx = up(M, 64) * up(K, 64), nw = up(N, 64) * up(K, 64) * segs, tx = up(N, 128) * segs, tw = up(M, 128);
+    if ((nx + nw + up(N * segs, 256)) * 256 >> 32) return false;
     const double share = (nx * tx + nw * tw) / 256.0, longest = tx > tw ? tx : tw, chain = (nx + nw > 256 ? 0.4 : 0.2) * longest;
     const double us = 7.5 + (0.31 * share > chain ? 0.31 * share : chain);
     return us <= x.us + w.us + 2;

@@ -1,4 +1,5 @@
-"""Calls in 8 bits of so many tiles that one launch cannot start them all (2^32 threads): 2^22 tiles of 128 x 128 values.  Tensors are zero but in
+"""Calls in 8 bits of so many tiles that one launch cannot start them all (2^32 threads): 2^22 tiles of 128 x 128 values, 2^24
+of 64 x 64 results.  Tensors are zero but in
 some rows, at both ends and round the places where a launch ends; outputs hold other bytes before the call."""
 import pytest
 import torch
@@ -70,3 +71,29 @@ def test_bias_gradient(tfla):  # noqa: F811
     db = torch.full((N,), float("nan"), device="cuda")
     tfla.linear_q8_bwd(None, None, None, dy, want_dx=False, want_dw=False, want_db=True, out={"db": db})
     assert torch.equal(db, few.to(F64).sum(0).to(F32))
+
+
+def test_one_token_back_through_the_largest_weights(tfla):  # noqa: F811
+    """dx and dw in one launch would be 2^24 tiles"""
+    K = N = 1 << 18
+    room(210)
+    print("largest weights", K, N, flush=True)
+    at = some_rows(K)
+    wt, few = torch.zeros((K, N), dtype=torch.uint8, device="cuda"), whole(3, len(at), N, BF16, 1)
+    codes = few.to(E4M3).view(torch.uint8)                  # (0 and +-1 are codes)
+    for i, k in enumerate(at):
+        wt[k].copy_(codes[i])
+    scale = torch.full((N // 128, K // 128), 127, dtype=torch.uint8, device="cuda").view(E8M0)
+    x, dy = torch.zeros((1, K), dtype=BF16, device="cuda"), torch.zeros((1, N), dtype=BF16, device="cuda")
+    rows = torch.tensor(at, device="cuda")
+    x[:, rows], dy[:, rows] = whole(4, 1, len(at), BF16), whole(5, 1, len(at), BF16)
+    dw = torch.full((N, K), float("nan"), dtype=BF16, device="cuda")
+    o = tfla.linear_q8_bwd(x, wt.view(E4M3), scale, dy, want_db=True, out={"dw": dw})
+    assert torch.equal(o["dx"][:, rows], (dy.to(F64) @ few.to(F64).t()).to(BF16))
+    o["dx"][:, rows] = 0
+    assert not bool(o["dx"].any()) and torch.equal(o["db"], dy[0].float())
+    for n in at:
+        assert torch.equal(dw[n], dy[0, n] * x[0]), n
+        dw[n] = 0
+    for lo in range(0, N, 1 << 14):
+        assert not bool(dw[lo:lo + (1 << 14)].any()), lo

@@ -1,6 +1,7 @@
 """The runtime starts fewer than 2^32 threads along an axis.  At the largest sizes that the calls in 8 bits accept, no launch asks for more: the
 rules (csrc/q8_plan.h, the header that the library is built with) compiled for the host."""
 import ctypes
+import itertools
 import os
 import subprocess
 
@@ -34,3 +35,24 @@ def test_tiles(probe, M, N, more):
     assert at == -(-M // 128) * -(-N // 128) + more
     if at < 1 << 21:
         assert n == 1
+
+
+def sizes(most):
+    """powers of two up to the limit and what lies next to them"""
+    return sorted({n for p in range(0, most + 1, 2) for n in (1 << p, (1 << p) + 1, (3 << p) // 2) if n <= 1 << most} | {1 << most, (1 << most) - 1})
+
+
+@pytest.mark.parametrize("backward,pair", itertools.product((0, 1), (0, 1)))
+def test_products(probe, backward, pair):
+    ask = probe.product_threads
+    ask.argtypes, ask.restype = [ctypes.c_int] * 2 + [ctypes.c_long] + [ctypes.c_int] * 2, ctypes.c_long
+    worst = (0,)
+    for M, K, N in itertools.product(sizes(21 if backward else 24), sizes(20), sizes(20)):
+        if max(M * K, M * N, N * K) <= 1 << 36:
+            worst = max(worst, (ask(backward, pair, M, K, N), M, K, N))
+    # the weights' size limit itself, in every proportion
+    for i in range(1 << 16, (1 << 20) + 1, 997):
+        for K, N in ((i, (1 << 36) // i), ((1 << 36) // i, i)):
+            if max(K, N) <= 1 << 20:
+                worst = max(worst, *((ask(backward, pair, M, K, N), M, K, N) for M in (1, 5, 40, 64, 128)))
+    assert worst[0] < LIMIT, worst
