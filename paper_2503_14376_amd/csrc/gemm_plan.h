@@ -79,6 +79,7 @@ inline bool gemm_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int 
     if (x.split != 1 || w.split != 1) return false;
     if (dtype != 1) return x.bm == w.bm && x.bm <= 64;
     const BothSteps b = both_steps(M, K, N, pair);
+    if (b.items >> 24) return false;        // (of 256 threads each: the runtime starts fewer than 2^32)
     const double share = b.sum / 256.0, chain = (b.items > 256 ? 0.4 : 0.2) * b.longest;
     const double us = b.wide() ? 9 + 0.225 * share : 7.5 + (0.29 * share > chain ? 0.29 * share : chain);
     return us <= x.us + w.us + 6;

@@ -1,4 +1,4 @@
-// How many threads the calls in 8 bits start at once, by the rules that the library itself is built with.  Compiled by the tests with the host
+// How many threads the residual block's calls start at once, by the rules that the library itself is built with.  Compiled by the tests with the host
 // compiler.
 #include "q8_plan.h"
 
@@ -39,4 +39,10 @@ extern "C" int tile_launches(long M, long N, unsigned more, long* first, long* t
         threads[n++] = (long)q8_launch(at, all) * Q8_TILE_THREADS;
     }
     return n;
+}
+
+// work items of 256 threads of a backward call's products in one launch, those of bf16; 0: two launches
+extern "C" long both_items(int pair, long M, int K, int N) {
+    const GemmPlan x = gemm_plan(M, K, N, pair ? 2 : 1, 1, 0, 1), w = gemm_plan(N, K, M, 1, pair ? 2 : 1, 0, 1);
+    return gemm_both_applies(x, w, M, K, N, pair, 1) ? both_steps(M, K, N, pair).items : 0;
 }

@@ -1,5 +1,6 @@
-"""The runtime starts fewer than 2^32 threads along an axis.  At the largest sizes that the calls in 8 bits accept, no launch asks for more: the
-rules (csrc/q8_plan.h, the header that the library is built with) compiled for the host."""
+"""The runtime starts fewer than 2^32 threads along an axis.  At the largest sizes that the calls in 8 bits accept, no launch asks for more, nor
+does the launch of both backward products in bf16: the rules (csrc/q8_plan.h, gemm_plan.h, the headers that the library is built with) compiled
+for the host."""
 import ctypes
 import itertools
 import os
@@ -56,3 +57,11 @@ def test_products(probe, backward, pair):
             if max(K, N) <= 1 << 20:
                 worst = max(worst, *((ask(backward, pair, M, K, N), M, K, N) for M in (1, 5, 40, 64, 128)))
     assert worst[0] < LIMIT, worst
+
+
+@pytest.mark.parametrize("pair", (0, 1))
+def test_both_products_in_bf16(probe, pair):
+    ask = probe.both_items
+    ask.argtypes, ask.restype = [ctypes.c_int, ctypes.c_long, ctypes.c_int, ctypes.c_int], ctypes.c_long
+    most = max(ask(pair, M, K, N) for M, K, N in itertools.product(sizes(24), sizes(20), sizes(20)) if max(M * K, M * N, N * K) <= 1 << 36)
+    assert 0 < most < LIMIT // 256
