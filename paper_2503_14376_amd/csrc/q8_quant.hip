@@ -355,8 +355,8 @@ template <typename DT, int MODE, int ACT> void tiles(const Q8TileArgs& a, const 
 template <int MODE> void by_act(const Q8TileArgs& a, const Q8TileArgs& b, const Q8RepackArgs& rp, hipStream_t s) {
     if (a.act == ACT_SILU) tiles<bf16_t, MODE, ACT_SILU>(a, b, rp, s);
     else if (a.act == ACT_GELU) tiles<bf16_t, MODE, ACT_GELU>(a, b, rp, s);
-    else if (a.act == ACT_RELU) tiles<bf16_t, MODE, ACT_RELU>(a, b, rp, s);
-    else tiles<bf16_t, MODE, ACT_NONE>(a, b, rp, s);
+    else if (MODE == Q8_ACT || a.act == ACT_RELU) tiles<bf16_t, MODE, ACT_RELU>(a, b, rp, s);
+    else if constexpr (MODE == Q8_PAIR) tiles<bf16_t, MODE, ACT_NONE>(a, b, rp, s);     // (a single product without an activation: Q8_VALUES)
 }
 
 }  // namespace
