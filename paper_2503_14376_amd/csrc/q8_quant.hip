@@ -15,8 +15,8 @@ constexpr int TILE = Q8_TILE, NT = Q8_TILE_THREADS, WAVES = NT / 64, RPI = NT / 
 // two codes is worth a sixteenth of itself, so that an error of 2^-13, as the bf16 products' gelu has, would show in dx, dw and the sums.  (The
 // library's functions for fp32 bound the pass instead: gated pair backward, 8192 x 10944, 406 us.)
 // silu: sigma by the hardware's exponential and reciprocal.  gelu: Phi(-|z|) = exp(-z^2 / 2) h(|z|), h = t P(t), t = 1 / (1 + c |z|), P of
-// degree 8 fitted to the smallest relative error over |z| <= 14.5 (2^-25.1, evaluated in fp32 2^-21.3; beyond, exp(-z^2 / 2)
-// leaves fp32).  z^2 is exact.
+// degree 8 fitted to the smallest relative error over |z| <= 14.5 (with these constants in fp32 2^-24.3, evaluated in fp32 2^-21.3, with a
+// reciprocal one unit off 2^-20.3; beyond, exp(-z^2 / 2) leaves fp32).  z^2 is exact.
 template <int ACT> __device__ __forceinline__ float act_fine(float z, float& slope) {
     if constexpr (ACT == ACT_SILU) {
         const float g = __builtin_amdgcn_rcpf(1.0f + fast_exp2(-1.44269504f * z));
