@@ -566,8 +566,8 @@ def _rows(x, name, b16, f32):
     t = x.dtype
     shape = x.shape
     dev = x.get_device()
-    if t != b16 and t != f32:
-        raise ValueError("%s must be bfloat16 or float32 (got %s)" % (name, t))
+    if t != b16 and t != f32:       # (f32 is b16 where a call takes that type alone)
+        raise ValueError("%s must be bfloat16%s (got %s)" % (name, "" if f32 is b16 else " or float32", t))
     if len(shape) != 2 or dev < 0 or not x.is_contiguous():
         raise ValueError("%s must be a contiguous device tensor of two dimensions" % name)
     return BF16 if t == b16 else F32, shape[0], shape[1], dev
