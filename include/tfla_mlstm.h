@@ -347,7 +347,8 @@ TFLA_API int tfla_gated_bwd(const void* x, const void* w_gate, const void* w_up,
  *    bfloat16, rounded once; biases, their gradients and row statistics are float.
  *  - Sizes, M = 0, alignment, order of execution, overlap and workspaces: as for the residual block above; in backward calls M is at most
  *    2^21.  The products work on rows of codes that are multiples of 16 bytes at 16-byte addresses; other operands are copied into the workspace first (`unaligned`:
- *    non-zero if codes or x are not at a 16-byte address).  Calls of few tokens read rows of any alignment in place.
+ *    non-zero if codes of the call are not at a 16-byte address; the other tensors are read at any).  Calls of few tokens read rows of codes of
+ *    any alignment in place.
  *
  * tfla_q8_quant: x (M, K) in `dtype` -> q (M, K) and scale, and / or those of the transpose, qt (K, M) and scale_t.  rows = 1: a group is 128
  * columns of a row (of the transpose: 128 rows of a column); rows = 128: blocks, for both.  Either pair of outputs may be NULL.
