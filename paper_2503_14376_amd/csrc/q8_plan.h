@@ -65,7 +65,9 @@ inline bool q8_both_applies(const GemmPlan& x, const GemmPlan& w, long M, int K,
 
 // ---- few rows -----------------------------------------------------------------------------------
 constexpr int Q8_ROWS_MAX = 32;
-// Slices as in gemm_plan.h, wherever the rows of x leave room for them: a block of work is 16 / slices rows of weights.  A slice's pieces of
+// Slices as in gemm_plan.h, wherever the rows of x leave room for them: a block of work is 16 / slices rows of weights (one token through
+// 10944 x 4096 11.3 us, in one slice 14.3, 8 tokens 13.3 and 15.2; through 4096 x 4096, where the host's time is most of it, 7.2 and 7.3,
+// 7.9 and 7.9; 4 tokens there 7.8 and 7.6).  A slice's pieces of
 // 128 codes go round the wavefronts, `ahead` of them per wavefront in flight, so that few places stay empty: a place without a piece costs
 // what one with a piece does (4 tokens through a pair of 10944 x 4096, 8 pieces a slice: four wavefronts with two pieces 18.4 us, with four
 // 37.2; through 4096 x 10944, 22 pieces: eight wavefronts with one 11.0, with two 13.3).  hold: a wavefront's share of x is one turn, and

@@ -276,8 +276,8 @@ constexpr int COPY = 256;
 __global__ void __launch_bounds__(COPY) q8_repack_kernel(Q8RepackArgs a) { q8_repack<COPY>(a, blockIdx.x, gridDim.x); }
 
 // Which tile workgroup i takes.  Rows of codes that are no multiple of 64 bytes: neighbours share cache lines, and an XCD takes a range of them, so that it
-// writes whole ones (16384 x 4097 33.0 us, one after another 46.8; with the transpose 45.3, 59.6).  Otherwise one after another (10944 x 4096
-// 40.5, ranges 44.6).
+// writes whole ones (16384 x 4097, four matrices in turn, 46.0 us, one after another 56.6; with the transpose 61.3, 79.4).  Otherwise one after
+// another (16384 x 4096 38.5, in ranges 46.4; 10944 x 4096 with its transpose 40.3, 44.3).
 __device__ __forceinline__ unsigned tile_of(const Q8TileArgs& a, unsigned i, unsigned n) { return a.N % 64 ? xcd_range(i, n) : i; }
 
 // The tiles of a, those of a row of tiles next to each other, then the tiles of b (plain values; none where b.M is 0), then copies: of all of

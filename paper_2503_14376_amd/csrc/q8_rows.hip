@@ -1,8 +1,9 @@
 // Products of few rows of codes with a whole matrix of weights in 8 bits (tokens being generated), as gemm_rows.hip does them for
 // bf16: one read of the weights bounds them, straight into the operand registers of v_mfma_scale_f32_16x16x128_f8f6f4, whose step is
 // the 128 codes that share a scale.  Rows may start at any address.
-// Measured: 1 token through 4096 x 4096 8.3 us with the host's time (kernel 7.5; 16.8 MB, of which a first load takes 2 us to arrive), 4 through a
-// pair of 10944 x 4096 18.9 (4.7 TB/s), its gate 4.0.
+// Measured: 1 token through 4096 x 4096 with bias and residual 8.2 us with the host's time (kernel 7.5; 16.8 MB, of which a first load takes 2 us
+// to arrive), 4 through a pair of 10944 x 4096 18.9 (4.7 TB/s), its gate 4.0.  Scratch: pairs at odd addresses with sixteen wavefronts and two
+// pieces in flight (17 to 32 rows 37 registers, 5 to 8 rows 4).
 #include "gemm_epilogue.h"
 #include "q8.h"
 #include "q8_internal.h"

@@ -157,7 +157,8 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_fwd_kernel(RowNormA
 
 // y = norm(x + residual) in 8 bits: the sum is formed once, in fp32, for the statistics and for y, and rounded only where it is stored.
 // Sixteen lanes hold 128 columns side by side, the group of a scale.  Memory-bound: 16384 x 4096 in bf16 with a residual and the sum 88.5 us for
-// 470 MB (5.3 TB/s); 2999 x 1365 in fp32 15.5, of whose rows every access is split.
+// 470 MB (5.3 TB/s).  Rows that do not begin at multiples of 16 bytes are read and written by split accesses: 16384 x 4097 131 us, 2999 x 1365 in
+// fp32 15.5.  Rows of more than 8192 columns leave 11 (bf16) or 19 (fp32) registers in scratch.
 template <typename DT, int T, int J>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) rownorm_q8_kernel(Q8NormArgs a) {
     constexpr int G = T < 256 ? 256 / T : 1;            // rows at a time
